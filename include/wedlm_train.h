@@ -1,8 +1,8 @@
 /*
- * wedlm_train.h -- C ABI of the training-time attention of WeDLM (arXiv
- * 2512.22737, Sec. 4.2 "Dual-Stream Masking") on MI355X (gfx950): the
- * forward of attention over a clean memory stream and a block-wise
- * reordered prediction stream.
+ * wedlm_train.h -- C ABI of the training-time operators of WeDLM (arXiv
+ * 2512.22737, Sec. 4.2 "Dual-Stream Masking") on MI355X (gfx950): attention
+ * over a clean memory stream and a block-wise reordered prediction stream,
+ * forward and backward.
  *
  * Conventions of wedlm.h hold (device pointers owned by the caller, bf16 as
  * uint16_t bits, nothing allocated or synchronised, enqueued on `stream`,
@@ -54,6 +54,40 @@ int wedlm_dual_stream_attn(const uint16_t* q, const uint16_t* k,
                            float softmax_scale, uint16_t* out, float* lse,
                            void* workspace, size_t workspace_bytes,
                            void* stream);
+
+/* Bytes of workspace wedlm_dual_stream_attn_backward needs (0: unsupported
+ * shape). */
+size_t wedlm_dual_stream_attn_backward_workspace_size(int32_t n_seq, int32_t L,
+                                                      int32_t block,
+                                                      int32_t Hq, int32_t Hkv,
+                                                      int32_t D);
+
+/*
+ * wedlm_dual_stream_attn_backward -- gradients of wedlm_dual_stream_attn:
+ * from dout, the gradient of its out, those of q, k and v.  The
+ * probabilities are computed again from q, k and lse.
+ * In:
+ *   q, k, v, softmax_scale and the sizes as in the forward call; out and lse
+ *   as it wrote them; dout [n_seq, 2L, Hq, D] bf16.  Values must be finite.
+ * Out:
+ *   dq [n_seq, 2L, Hq, D], dk, dv [n_seq, 2L, Hkv, D] bf16 (overwritten; the
+ *   gradients of a kv head are summed over its query heads).  They must not
+ *   overlap the inputs or each other.
+ * Products take bf16 operands (the probabilities and the scores' gradients
+ * are rounded to it) with fp32 sums, in an order that the sizes fix: the
+ * result does not depend on the run.
+ * Limits: those of the forward.
+ * workspace: wedlm_dual_stream_attn_backward_workspace_size() bytes, 256-byte
+ * aligned (each row's normaliser and output product; fp32 partial sums where
+ * few key tiles are split); its contents on entry do not matter.  Two calls
+ * that overlap in time must not share a workspace.
+ */
+int wedlm_dual_stream_attn_backward(
+    const uint16_t* q, const uint16_t* k, const uint16_t* v,
+    const uint16_t* out, const float* lse, const uint16_t* dout, int32_t n_seq,
+    int32_t L, int32_t block, int32_t Hq, int32_t Hkv, int32_t D,
+    float softmax_scale, uint16_t* dq, uint16_t* dk, uint16_t* dv,
+    void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

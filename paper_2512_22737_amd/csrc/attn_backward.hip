@@ -1,0 +1,588 @@
+// Backward pass of the dual-stream training attention (Sec. 4.2): from the
+// output's gradient to those of q, k and v, with the probabilities computed
+// again from q, k and the forward's normaliser.
+//
+// For a row i and the keys j it sees (scale s, o and lse of the forward):
+//   P_ij = exp(s q_i.k_j - lse_i)        dP_ij = do_i . v_j
+//   D_i  = do_i . o_i                    dS_ij = P_ij (dP_ij - D_i)
+//   dq_i = s sum_j dS_ij k_j             dk_j  = s sum_i dS_ij q_i
+//                                        dv_j  = sum_i P_ij do_i
+// where the sums over i run over the G = Hq/Hkv query heads of the kv head
+// too.  Memory row p sees memory keys 0..p; prediction row p (block
+// start f = p / block * block) sees memory keys 0..f-1 and prediction keys
+// f..p.  In both directions the visible ones are an interval: every mask is
+// two comparisons.
+//
+// Two kernels, each accumulating in registers what it owns, so that nothing
+// is added atomically and the result does not depend on the run:
+//   dq:    a wave owns 64 rows of one head and walks the keys.  It also
+//          writes D_i and lse_i, laid out for the second kernel.
+//   dk/dv: a wave owns 64 keys of one kv head and walks the rows of all its
+//          heads.
+// S and dP are formed in both, seven products instead of the five that a
+// pass with shared accumulators needs.
+// MFMA: v_mfma_f32_32x32x16_bf16.  The score tile has the streamed rows
+// (keys in dq, query rows in dk/dv) as its M dimension and the owned ones as
+// N, so a lane holds 16 scores of one owned row, eight at a time contiguous
+// (key_of_row), which is the operand layout of the second product: P and dS
+// go from accumulators to operands in registers.  The second product's other
+// operand is read from the same LDS tile by columns (ds_read_b64_tr_b16).
+// Each operand read from LDS feeds two MFMAs (the wave's two 32-row groups).
+// P and dS are rounded to bf16 for the second products, as the forward
+// rounds P; all sums are fp32.
+#include "common.h"
+#include "wedlm_train.h"
+
+using namespace wedlm;
+
+namespace {
+
+constexpr int kRows = 32;             // streamed rows of an LDS tile
+constexpr int kOwn = 64;              // rows or keys that a wave owns
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kKeysPerWg = kWaves * kOwn;
+constexpr float kLog2e = 1.4426950408889634f;
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+struct BwdArgs {
+  const uint16_t* q;      // [n_seq, 2L, Hq, D]
+  const uint16_t* k;      // [n_seq, 2L, Hkv, D]
+  const uint16_t* v;
+  const uint16_t* out;    // [n_seq, 2L, Hq, D]
+  const float* lse;       // [n_seq, 2L, Hq]
+  const uint16_t* dout;
+  uint16_t* dq;
+  uint16_t* dk;
+  uint16_t* dv;
+  float* ld;              // [n_seq, Hq, 2, T, 2, 32]: lse (log2 units), D
+  float* part;            // [2 (dk, dv)][nsplit][n_seq, L, Hkv, D], or null
+  int n_seq, L, block, Hq, Hkv, G, T, nsplit;
+  float scale, scale_log2;
+};
+
+// LDS tile of 32 rows of D bf16: 16-byte chunk c of row r sits in slot
+// c ^ swz(r) of its row.  swz takes all values over rows that share a bank
+// phase (16 rows of one chunk, a row read, hit different banks) and its high
+// bits differ over four consecutive rows (so do a column read's).
+template <int D>
+struct RowTile {
+  static constexpr int bytes = kRows * D * 2;
+  static constexpr int chunks = D / 8;
+  __device__ static __forceinline__ int swz(int r) {
+    return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3)
+                    : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  }
+  __device__ static __forceinline__ int off(int r, int c) {
+    return r * 2 * D + ((c ^ swz(r)) << 4);
+  }
+};
+
+// Row of the streamed tile in MFMA row m: bits 2 and 3 swapped, so that
+// output element e of a lane (hf = lane / 32) is row 16 (e / 8) + 8 hf + e % 8.
+__device__ __forceinline__ int row_of_m(int m) {
+  return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1);
+}
+
+__device__ __forceinline__ bf16x8_t load8(const uint16_t* p) {
+  return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u16x8_t*>(p));
+}
+
+// Rows as the first operand: lane's row, values 16 kk + 8 hf .. + 7.
+template <int D>
+__device__ __forceinline__ bf16x8_t row_frag(const char* tile, int kk) {
+  const int l = lane_id();
+  return load8(reinterpret_cast<const uint16_t*>(
+      tile + RowTile<D>::off(row_of_m(l & 31), 2 * kk + (l >> 5))));
+}
+
+// Columns: lane's column 32 m + lane % 32, rows 16 h + 8 hf .. + 7.
+template <int D>
+__device__ __forceinline__ bf16x8_t col_frag(const char* tile, int h, int m) {
+  const int l = lane_id(), i = l & 15;
+  const int c = 4 * m + 2 * ((l >> 4) & 1) + ((i & 3) >> 1);
+  s16x4_t x[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int r = 16 * h + 8 * (l >> 5) + 4 * j + (i >> 2);
+    x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_s16x4_t*)(tile + RowTile<D>::off(r, c) + (i & 1) * 8));
+  }
+  return __builtin_bit_cast(
+      bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A tile of rows first .. first+31 of a [.., rows, heads, D] array (base: row
+// 0 of one head, stride in elements) into LDS; rows past the last one re-read
+// it.
+template <int D>
+__device__ __forceinline__ void stage(const uint16_t* base, int64_t stride,
+                                      int first, int last, char* tile) {
+  constexpr int C = RowTile<D>::chunks;
+#pragma unroll
+  for (int u = 0; u < kRows * C / kThreads; ++u) {
+    const int i = threadIdx.x + u * kThreads;
+    const int r = i / C, c = i % C;
+    *reinterpret_cast<u16x8_t*>(tile + RowTile<D>::off(r, c)) =
+        *reinterpret_cast<const u16x8_t*>(base + min(first + r, last) * stride +
+                                          c * 8);
+  }
+}
+
+__device__ __forceinline__ floatx16_t mfma(bf16x8_t a, bf16x8_t b,
+                                           floatx16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// dq: workgroup = four units (64-position chunk, head) of one stream and kv
+// head, one per wave; the longest first.
+template <int D>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(1)))
+void dq_kernel(BwdArgs a) {
+  constexpr int NK = D / 16, NM = D / 32;
+  using T = RowTile<D>;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * T::bytes];
+  char* kt = smem;
+  char* vt = smem + T::bytes;
+  const int chunks = (a.L + kOwn - 1) / kOwn;
+  const int groups = (chunks * a.G + kWaves - 1) / kWaves;
+  int wg = blockIdx.x;
+  const int kvh = wg % a.Hkv;
+  wg /= a.Hkv;
+  const int stream = wg & 1;
+  wg >>= 1;
+  const int grp = groups - 1 - wg % groups;
+  const int sq = wg / groups;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = lane_id(), col = lane & 31, hf = lane >> 5;
+  const int last_unit = chunks * a.G - 1;
+  const int unit = min(grp * kWaves + wave, last_unit);
+  const bool live = grp * kWaves + wave <= last_unit;
+  const int p0 = unit / a.G * kOwn;
+  const int head = kvh * a.G + unit % a.G;
+  const int64_t row0 = (static_cast<int64_t>(sq) * 2 + stream) * a.L;
+
+  bf16x8_t qf[2][NK], dof[2][NK];
+  float lse2[2], delta[2];
+  int lo[2], hi[2];         // memory: keys below lo; own stream: see own()
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int p = p0 + 32 * b + col;
+    const int pc = min(p, a.L - 1);
+    const int64_t o = ((row0 + pc) * a.Hq + head) * D;
+    float d = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      const int at = kk * 16 + hf * 8;
+      qf[b][kk] = load8(a.q + o + at);
+      dof[b][kk] = load8(a.dout + o + at);
+      const bf16x8_t of = load8(a.out + o + at);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        d += static_cast<float>(dof[b][kk][e]) * static_cast<float>(of[e]);
+    }
+    d += __shfl_xor(d, 32);
+    const float l2 = a.lse[(row0 + pc) * a.Hq + head] * kLog2e;
+    lse2[b] = l2;
+    delta[b] = d;
+    if (live && hf == 0 && p < a.T * kRows) {
+      float* ld = a.ld + ((((static_cast<int64_t>(sq) * a.Hq + head) * 2 +
+                            stream) * a.T + p / kRows) * 2) * kRows + col;
+      ld[0] = p < a.L ? l2 : 0.f;
+      ld[kRows] = p < a.L ? d : 0.f;
+    }
+    lo[b] = stream ? pc / a.block * a.block : 0;
+    hi[b] = pc + 1;
+  }
+  floatx16_t acc[2][NM];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int m = 0; m < NM; ++m) acc[b][m] = floatx16_t{};
+
+  // one key tile (keys j0 .. j0+31 of a stream); key j is seen if
+  // b0 <= j < b1 of its row
+  auto tile = [&](int j0, const int (&b0)[2], const int (&b1)[2]) {
+    floatx16_t s[2] = {}, dp[2] = {};
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      const bf16x8_t f = row_frag<D>(kt, kk);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) s[b] = mfma(f, qf[b][kk], s[b]);
+    }
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      const bf16x8_t f = row_frag<D>(vt, kk);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) dp[b] = mfma(f, dof[b][kk], dp[b]);
+    }
+    bf16x8_t ds[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int j = j0 + 16 * (e >> 3) + 8 * hf + (e & 7);
+        const float x = j >= b0[b] && j < b1[b] ? s[b][e] : kNegInf;
+        const float p = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(x, a.scale_log2, -lse2[b]));
+        ds[b][e >> 3][e & 7] = static_cast<__bf16>(p * (dp[b][e] - delta[b]));
+      }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int m = 0; m < NM; ++m) {
+        const bf16x8_t f = col_frag<D>(kt, h, m);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[b][m] = mfma(f, ds[b][h], acc[b][m]);
+      }
+  };
+  const int64_t kstride = static_cast<int64_t>(a.Hkv) * D;
+  auto walk = [&](int from, int to, int key_stream, const int (&b0)[2],
+                  const int (&b1)[2]) {
+    const int64_t base =
+        ((static_cast<int64_t>(sq) * 2 + key_stream) * a.L * a.Hkv + kvh) * D;
+    for (int j0 = from / kRows * kRows; j0 < to; j0 += kRows) {
+      __syncthreads();
+      stage<D>(a.k + base, kstride, j0, a.L - 1, kt);
+      stage<D>(a.v + base, kstride, j0, a.L - 1, vt);
+      __syncthreads();
+      tile(j0, b0, b1);
+    }
+  };
+  // positions of the workgroup's rows
+  const int first = grp * kWaves / a.G * kOwn;
+  const int end = min(a.L, (min(grp * kWaves + kWaves - 1, last_unit) / a.G +
+                            1) * kOwn);
+  const int zero[2] = {0, 0};
+  if (stream) {
+    walk(0, (end - 1) / a.block * a.block, 0, zero, lo);
+    walk(first / a.block * a.block, end, 1, lo, hi);
+  } else {
+    walk(0, end, 0, zero, hi);
+  }
+  if (!live) return;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int p = p0 + 32 * b + col;
+    if (p >= a.L) continue;
+    uint16_t* o = a.dq + ((row0 + p) * a.Hq + head) * D;
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        u16x4_t x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[e] = f32_to_bf16(acc[b][m][4 * g + e] * a.scale);
+        *reinterpret_cast<u16x4_t*>(o + 32 * m + 8 * g + 4 * hf) = x;
+      }
+  }
+}
+
+// dk and dv: workgroup = 256 keys of one stream and kv head; the memory
+// stream's tiles first (they have the long walks), the earliest keys first.
+template <int D>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(1)))
+void dkv_kernel(BwdArgs a) {
+  constexpr int NK = D / 16, NM = D / 32;
+  using T = RowTile<D>;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * T::bytes];
+  __shared__ float ldt[2 * kRows];
+  char* qt = smem;
+  char* dot = smem + T::bytes;
+  const int tiles = (a.L + kKeysPerWg - 1) / kKeysPerWg;
+  const int n_mem = a.n_seq * a.Hkv * tiles * a.nsplit;
+  int wg = blockIdx.x;
+  const int stream = wg >= n_mem ? 1 : 0;
+  if (stream) wg -= n_mem;
+  const int nsplit = stream ? 1 : a.nsplit;
+  const int kvh = wg % a.Hkv;
+  wg /= a.Hkv;
+  const int split = wg % nsplit;
+  wg /= nsplit;
+  const int j0 = wg % tiles * kKeysPerWg;
+  const int sq = wg / tiles;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = lane_id(), col = lane & 31, hf = lane >> 5;
+  const int kw0 = j0 + wave * kOwn;
+
+  bf16x8_t kf[2][NK], vf[2][NK];
+  // rows that see this lane's keys: memory rows key .. L-1 and prediction
+  // rows next .. L-1, or for a prediction key rows key .. next-1 (next: the
+  // block after the key's)
+  int key[2], next[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    key[b] = kw0 + 32 * b + col;
+    const int jc = min(key[b], a.L - 1);
+    next[b] = min(a.L, (jc / a.block + 1) * a.block);
+    const int64_t o =
+        (((static_cast<int64_t>(sq) * 2 + stream) * a.L + jc) * a.Hkv + kvh) * D;
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      kf[b][kk] = load8(a.k + o + kk * 16 + hf * 8);
+      vf[b][kk] = load8(a.v + o + kk * 16 + hf * 8);
+    }
+    if (key[b] >= a.L) key[b] = next[b] = 0x40000000;   // seen by no row
+  }
+  floatx16_t dk[2][NM], dv[2][NM];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int m = 0; m < NM; ++m) dk[b][m] = dv[b][m] = floatx16_t{};
+
+  // one tile of rows p0 .. p0+31; row p sees the lane's key if r0 <= p < r1
+  auto tile = [&](int p0, const int (&r0)[2], const int (&r1)[2]) {
+    floatx16_t s[2] = {}, dp[2] = {};
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      const bf16x8_t f = row_frag<D>(qt, kk);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) s[b] = mfma(f, kf[b][kk], s[b]);
+    }
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      const bf16x8_t f = row_frag<D>(dot, kk);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) dp[b] = mfma(f, vf[b][kk], dp[b]);
+    }
+    bf16x8_t pb[2][2], ds[2][2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int r = 16 * (e >> 3) + 8 * hf + (e & 7);
+      const float l2 = ldt[r], d = ldt[kRows + r];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const float x = p0 + r >= r0[b] && p0 + r < r1[b] ? s[b][e] : kNegInf;
+        const float p =
+            __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale_log2, -l2));
+        pb[b][e >> 3][e & 7] = static_cast<__bf16>(p);
+        ds[b][e >> 3][e & 7] = static_cast<__bf16>(p * (dp[b][e] - d));
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int m = 0; m < NM; ++m) {
+        const bf16x8_t f = col_frag<D>(dot, h, m);
+        const bf16x8_t g = col_frag<D>(qt, h, m);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          dv[b][m] = mfma(f, pb[b][h], dv[b][m]);
+          dk[b][m] = mfma(g, ds[b][h], dk[b][m]);
+        }
+      }
+  };
+  // items: row tiles t from the last down, in each the streams that see the
+  // keys and their heads
+  const int kend = min(a.L, j0 + kKeysPerWg);
+  int t_hi = a.T, t_mid, t_lo = j0 / kRows;
+  if (stream) {
+    t_hi = (min(a.L, ((kend - 1) / a.block + 1) * a.block) + kRows - 1) / kRows;
+    t_mid = t_hi;
+  } else {
+    t_mid = min(t_hi, (j0 / a.block + 1) * a.block / kRows);
+  }
+  const int n1 = (t_hi - t_mid) * 2 * a.G;
+  const int n_items = n1 + (t_mid - t_lo) * a.G;
+  const int it0 = static_cast<int>(static_cast<int64_t>(n_items) * split / nsplit);
+  const int it1 =
+      static_cast<int>(static_cast<int64_t>(n_items) * (split + 1) / nsplit);
+  const int64_t qstride = static_cast<int64_t>(a.Hq) * D;
+  const int zero[2] = {0, 0}, all[2] = {a.L, a.L};
+  for (int it = it0; it < it1; ++it) {
+    int t, sg;
+    if (it < n1) {
+      t = t_hi - 1 - it / (2 * a.G);
+      sg = it % (2 * a.G);
+    } else {
+      t = t_mid - 1 - (it - n1) / a.G;
+      sg = (it - n1) % a.G;
+    }
+    const int row_stream = stream ? 1 : sg / a.G;
+    const int head = kvh * a.G + sg % a.G;
+    const int64_t row0 = (static_cast<int64_t>(sq) * 2 + row_stream) * a.L;
+    const int64_t base = (row0 * a.Hq + head) * D;
+    __syncthreads();
+    stage<D>(a.q + base, qstride, t * kRows, a.L - 1, qt);
+    stage<D>(a.dout + base, qstride, t * kRows, a.L - 1, dot);
+    if (threadIdx.x < 2 * kRows)
+      ldt[threadIdx.x] =
+          a.ld[(((static_cast<int64_t>(sq) * a.Hq + head) * 2 + row_stream) *
+                    a.T + t) * 2 * kRows + threadIdx.x];
+    __syncthreads();
+    if (stream)
+      tile(t * kRows, key, next);
+    else if (row_stream)
+      tile(t * kRows, next, all);
+    else
+      tile(t * kRows, key, all);
+  }
+  (void)zero;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    if (key[b] >= a.L) continue;
+    const int64_t kv = static_cast<int64_t>(a.Hkv) * D;
+    if (nsplit == 1) {
+      const int64_t o =
+          ((static_cast<int64_t>(sq) * 2 + stream) * a.L + key[b]) * kv + kvh * D;
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          u16x4_t x, y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] = f32_to_bf16(dk[b][m][4 * g + e] * a.scale);
+            y[e] = f32_to_bf16(dv[b][m][4 * g + e]);
+          }
+          *reinterpret_cast<u16x4_t*>(a.dk + o + 32 * m + 8 * g + 4 * hf) = x;
+          *reinterpret_cast<u16x4_t*>(a.dv + o + 32 * m + 8 * g + 4 * hf) = y;
+        }
+    } else {
+      const int64_t n = a.n_seq * static_cast<int64_t>(a.L) * kv;
+      float* o = a.part + split * n +
+                 (static_cast<int64_t>(sq) * a.L + key[b]) * kv + kvh * D;
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          floatx4_t x, y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] = dk[b][m][4 * g + e] * a.scale;
+            y[e] = dv[b][m][4 * g + e];
+          }
+          *reinterpret_cast<floatx4_t*>(o + 32 * m + 8 * g + 4 * hf) = x;
+          *reinterpret_cast<floatx4_t*>(o + a.nsplit * n + 32 * m + 8 * g +
+                                        4 * hf) = y;
+        }
+    }
+  }
+}
+
+// dk and dv of the memory keys from the fp32 partials of the splits, added in
+// split order; four values a thread.
+__global__ __launch_bounds__(256) void join_kernel(
+    const float* __restrict__ part, int nsplit, int64_t n, int64_t per_seq,
+    uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  const float* src = part + (blockIdx.y ? nsplit * n : 0) + i;
+  floatx4_t s = *reinterpret_cast<const floatx4_t*>(src);
+  for (int k = 1; k < nsplit; ++k) {
+    const floatx4_t x = *reinterpret_cast<const floatx4_t*>(src + k * n);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += x[e];
+  }
+  u16x4_t o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = f32_to_bf16(s[e]);
+  // memory rows are the first half of each sequence's
+  *reinterpret_cast<u16x4_t*>((blockIdx.y ? dv : dk) + i +
+                              i / per_seq * per_seq) = o;
+}
+
+struct BwdPlan {
+  int T, nsplit;
+  size_t part, total;
+  unsigned dq_grid, dkv_grid;
+};
+
+size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
+
+bool bwd_plan(int n_seq, int L, int block, int Hq, int Hkv, int D,
+              BwdPlan* p) {
+  // the forward's limits
+  if (wedlm_dual_stream_attn_workspace_size(n_seq, L, block, Hq, Hkv, D) == 0)
+    return false;
+  const int G = Hq / Hkv;
+  p->T = (L + kRows - 1) / kRows;
+  const int64_t chunks = (L + kOwn - 1) / kOwn;
+  const int64_t dq = 2 * n_seq * ((chunks * G + kWaves - 1) / kWaves) * Hkv;
+  const int64_t tiles = static_cast<int64_t>(n_seq) * Hkv *
+                        ((L + kKeysPerWg - 1) / kKeysPerWg);
+  // Memory key tiles walk up to L rows of each head, half of that on
+  // average: two workgroups per CU even that out.  With fewer tiles than
+  // that the walks are split, down to four row tiles each.
+  const int64_t longest = 2ll * G * p->T;
+  int64_t ns = (512 + tiles - 1) / tiles;
+  if (ns > longest / 4) ns = longest / 4;
+  if (ns < 1) ns = 1;
+  p->nsplit = static_cast<int>(ns);
+  const int64_t dkv = tiles * (ns + 1);
+  if (dq > 0x7fffffffll || dkv > 0x7fffffffll) return false;
+  p->dq_grid = static_cast<unsigned>(dq);
+  p->dkv_grid = static_cast<unsigned>(dkv);
+  p->part = up256(static_cast<size_t>(n_seq) * Hq * 2 * p->T * 2 * kRows * 4);
+  p->total = p->part;
+  if (ns > 1)
+    p->total += up256(2 * ns * static_cast<size_t>(n_seq) * L * Hkv * D * 4);
+  return true;
+}
+
+}  // namespace
+
+extern "C" size_t wedlm_dual_stream_attn_backward_workspace_size(
+    int32_t n_seq, int32_t L, int32_t block, int32_t Hq, int32_t Hkv,
+    int32_t D) {
+  BwdPlan p;
+  return bwd_plan(n_seq, L, block, Hq, Hkv, D, &p) ? p.total : 0;
+}
+
+extern "C" int wedlm_dual_stream_attn_backward(
+    const uint16_t* q, const uint16_t* k, const uint16_t* v,
+    const uint16_t* out, const float* lse, const uint16_t* dout, int32_t n_seq,
+    int32_t L, int32_t block, int32_t Hq, int32_t Hkv, int32_t D,
+    float softmax_scale, uint16_t* dq, uint16_t* dk, uint16_t* dv,
+    void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k || !v || !out || !lse || !dout || !dq || !dk || !dv)
+    return WEDLM_E_ARG;
+  if (!(softmax_scale > 0.f) || !(softmax_scale < 1e30f)) return WEDLM_E_ARG;
+  BwdPlan p;
+  if (!bwd_plan(n_seq, L, block, Hq, Hkv, D, &p)) return WEDLM_E_SHAPE;
+  if (!workspace || workspace_bytes < p.total) return WEDLM_E_WORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  BwdArgs a{};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.lse = lse;
+  a.dout = dout;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.ld = reinterpret_cast<float*>(ws);
+  a.part = p.nsplit > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr;
+  a.n_seq = n_seq;
+  a.L = L;
+  a.block = block;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.T = p.T;
+  a.nsplit = p.nsplit;
+  a.scale = softmax_scale;
+  a.scale_log2 = softmax_scale * kLog2e;
+  hipLaunchKernelGGL(D == 128 ? dq_kernel<128> : dq_kernel<64>,
+                     dim3(p.dq_grid), dim3(kThreads), 0, st, a);
+  WEDLM_LAUNCH_CHECK();
+  hipLaunchKernelGGL(D == 128 ? dkv_kernel<128> : dkv_kernel<64>,
+                     dim3(p.dkv_grid), dim3(kThreads), 0, st, a);
+  WEDLM_LAUNCH_CHECK();
+  if (p.nsplit > 1) {
+    const int64_t per_seq = static_cast<int64_t>(L) * Hkv * D;
+    const int64_t n = n_seq * per_seq;
+    hipLaunchKernelGGL(join_kernel,
+                       dim3(static_cast<unsigned>((n / 4 + 255) / 256), 2),
+                       dim3(256), 0, st, a.part, p.nsplit, n, per_seq, dk, dv);
+    WEDLM_LAUNCH_CHECK();
+  }
+  return WEDLM_OK;
+}

@@ -102,6 +102,11 @@ def _load():
     lib.wedlm_dual_stream_attn.argtypes = [P, P, P, I32, I32, I32, I32, I32,
                                            I32, F, P, P, P, SZ, P]
     lib.wedlm_dual_stream_attn.restype = ctypes.c_int
+    lib.wedlm_dual_stream_attn_backward_workspace_size.argtypes = [I32] * 6
+    lib.wedlm_dual_stream_attn_backward_workspace_size.restype = SZ
+    lib.wedlm_dual_stream_attn_backward.argtypes = (
+        [P] * 6 + [I32] * 6 + [F] + [P] * 4 + [SZ, P])
+    lib.wedlm_dual_stream_attn_backward.restype = ctypes.c_int
     lib.wedlm_strerror.argtypes = [ctypes.c_int]
     lib.wedlm_strerror.restype = ctypes.c_char_p
     lib.wedlm_version.argtypes = []
@@ -124,7 +129,9 @@ EXPORTED = ["wedlm_reorder", "wedlm_window_attn_workspace_size",
             "wedlm_pack_weights", "wedlm_qk_norm_rope",
             "wedlm_model_workspace_size",
             "wedlm_model_forward", "wedlm_commit_layers",
-            "wedlm_dual_stream_attn_workspace_size", "wedlm_dual_stream_attn"]
+            "wedlm_dual_stream_attn_workspace_size", "wedlm_dual_stream_attn",
+            "wedlm_dual_stream_attn_backward_workspace_size",
+            "wedlm_dual_stream_attn_backward"]
 
 # decoding rules of wedlm_commit_rule (include/wedlm.h)
 RULE_STREAMING, RULE_BLOCK, RULE_ONE_TOKEN = 0, 1, 2
@@ -754,3 +761,38 @@ def wedlm_dual_stream_attn(q, k, v, block: int, out, lse=None, workspace=None,
         _t(workspace, "workspace", _U8), workspace.numel(),
         _stream())
     _check(code, "wedlm_dual_stream_attn")
+
+
+def wedlm_dual_stream_attn_backward_workspace_size(n_seq, L, block, Hq, Hkv,
+                                                   D) -> int:
+    return int(_load().wedlm_dual_stream_attn_backward_workspace_size(
+        n_seq, L, block, Hq, Hkv, D))
+
+
+def wedlm_dual_stream_attn_backward(q, k, v, block: int, out, lse, dout, dq,
+                                    dk, dv, workspace=None,
+                                    softmax_scale: Optional[float] = None
+                                    ) -> None:
+    """Gradients of wedlm_dual_stream_attn: dout [n_seq, 2L, Hq, D] and the
+    forward's inputs, out and lse -> dq like q, dk and dv like k (bf16,
+    overwritten).  A workspace is allocated here if none is given."""
+    n_seq, L2, Hq, D = q.shape
+    Hkv = k.shape[2]
+    L = L2 // 2
+    if softmax_scale is None:
+        softmax_scale = 1.0 / math.sqrt(D)
+    need = wedlm_dual_stream_attn_backward_workspace_size(n_seq, L, block, Hq,
+                                                          Hkv, D)
+    if need == 0:
+        raise WedlmError("unsupported dual-stream shape")
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    qs, ks = (n_seq, 2 * L, Hq, D), (n_seq, 2 * L, Hkv, D)
+    code = _load().wedlm_dual_stream_attn_backward(
+        _t(q, "q", _BF16, qs), _t(k, "k", _BF16, ks), _t(v, "v", _BF16, ks),
+        _t(out, "out", _BF16, qs), _t(lse, "lse", _F32, qs[:3]),
+        _t(dout, "dout", _BF16, qs), n_seq, L, int(block), Hq, Hkv, D,
+        float(softmax_scale), _t(dq, "dq", _BF16, qs),
+        _t(dk, "dk", _BF16, ks), _t(dv, "dv", _BF16, ks),
+        _t(workspace, "workspace", _U8), workspace.numel(), _stream())
+    _check(code, "wedlm_dual_stream_attn_backward")

@@ -1,0 +1,51 @@
+"""Host-side refusals of the training operators (include/wedlm_train.h): no
+call here gets past the validation of its arguments."""
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2512_22737_amd", "libwedlm.so")
+
+pytestmark = pytest.mark.skipif(not os.path.exists(LIB),
+                                reason="libwedlm.so not built")
+
+F = ctypes.c_void_p(0x1000)       # never dereferenced
+
+
+def _lib():
+    from paper_2512_22737_amd import wedlm
+    return wedlm.lib()
+
+
+def refusals(call, args, cases):
+    for at, value, code in cases:
+        bad = list(args)
+        bad[at] = value
+        assert call(*bad) == code, (at, value)
+
+
+def test_attention_backward_workspace():
+    ws = _lib().wedlm_dual_stream_attn_backward_workspace_size
+    assert ws(1, 128, 32, 4, 2, 64) > 0
+    # one split: lse and D of 4 x 2 x 4096 rows of 32 heads
+    assert ws(4, 4096, 32, 32, 8, 128) == 4 * 8192 * 32 * 8
+    for bad in ((0, 128, 32, 4, 2, 64), (1, 100, 32, 4, 2, 64),
+                (1, 128, 96, 4, 2, 64), (1, 128, 32, 4, 2, 96),
+                (1, 128, 32, 5, 2, 64), (1, 128, 0, 4, 2, 64),
+                (1, 24, 8, 4, 2, 64), (1, 128, 32, 0, 0, 64),
+                (4, 65536, 1, 4, 2, 64)):
+        assert ws(*bad) == 0, bad
+
+
+def test_attention_backward_refusals():
+    lib = _lib()
+    need = lib.wedlm_dual_stream_attn_backward_workspace_size(1, 128, 32, 4, 2,
+                                                              64)
+    args = [F] * 6 + [1, 128, 32, 4, 2, 64, 0.125] + [F] * 4 + [need, None]
+    refusals(lib.wedlm_dual_stream_attn_backward, args,
+             [(i, None, -1) for i in (0, 1, 2, 3, 4, 5, 13, 14, 15)] +
+             [(12, 0.0, -1), (12, float("nan"), -1), (12, float("inf"), -1),
+              (7, 120, -2), (8, 33, -2), (9, 3, -2), (11, 32, -2),
+              (16, None, -3), (17, need - 1, -3)])
