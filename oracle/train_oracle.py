@@ -1,6 +1,7 @@
 """Plain fp64 CPU oracle of the training-time gradients (numpy, test
-infrastructure only): the backward pass of the dual-stream attention of
-Sec. 4.2.
+infrastructure only): the backward passes of the dual-stream attention of
+Sec. 4.2, of RMSNorm and of the per-head q/k norm with RoPE, and the masked
+tokens' loss.
 
 Each function takes values that are exact in fp64 (bf16 and fp32 inputs
 widened) and returns the exact gradients with a bound of how far the HIP
@@ -104,3 +105,92 @@ def attn_out_error(q, k, v, vis, scale):
             scale * q[:, h] @ K.T - lse[:, h:h + 1], 0.0)), 0.0)
         err[:, h] = 1.02 * (2 * BF16 * p @ np.abs(V) + BF16 * np.abs(out[:, h]))
     return err
+
+
+def rmsnorm(x, gain, eps):
+    return x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * gain
+
+
+def rmsnorm_backward(x, gain, dy, eps, dy_err=None):
+    """Norms over the last axis -> (dx, dgain), (their bounds).  dgain is
+    summed over all others.  dy_err: how far the kernel's dy may be off.
+
+    fp32: sums of n terms are off by n F32 of their magnitudes' sum (the
+    kernels add pairwise, so log2 n would do), r by the sum of squares'
+    error and three roundings, each product by one."""
+    n, rows = x.shape[-1], x.size // x.shape[-1]
+    if dy_err is None:
+        dy_err = np.zeros_like(dy)
+    r = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    xh, u = x * r, dy * gain
+    m = (u * xh).mean(-1, keepdims=True)
+    dx = r * (u - xh * m)
+    other = tuple(range(x.ndim - 1))
+    dg = (dy * xh).sum(other)
+    rel = F32 * (n / 2 + 6)                       # of r and of xh
+    e_u = np.abs(dy_err * gain) + F32 * np.abs(u)
+    e_m = ((e_u + (rel + F32 * (n + 3)) * np.abs(u)) * np.abs(xh)).mean(
+        -1, keepdims=True)
+    b_x = r * (e_u + np.abs(xh) * (e_m + np.abs(m) * (2 * rel + 6 * F32)) +
+               (rel + 3 * F32) * (np.abs(u) + np.abs(xh * m)))
+    b_g = (np.abs(dy_err * xh) + (rel + F32 * (rows + 3)) *
+           np.abs(dy * xh)).sum(other)
+    return (dx, dg), (1.01 * b_x, 1.01 * b_g)
+
+
+def rotate(x, pos, theta, back=False):
+    """x [M, heads, D] turned by the angles of pos [M] ("rotate half")."""
+    h = x.shape[-1] // 2
+    a = pos[:, None, None] * theta ** (-np.arange(h) / h)
+    c, s = np.cos(a), np.sin(a) * (-1 if back else 1)
+    lo, hi = x[..., :h], x[..., h:]
+    return np.concatenate((lo * c - hi * s, hi * c + lo * s), -1)
+
+
+def qk_norm_rope_backward(x, gain, pos, dy, theta, eps):
+    """x, dy [M, heads, D] of the query or the key heads -> (dx, dgain), (their
+    bounds), dx with its rounding to bf16.  A cosine or sine is rounded to
+    fp32, then two products and a sum: 3 F32 of both terms."""
+    h = x.shape[-1] // 2
+    dz = rotate(dy, pos.astype(np.float64), theta, back=True)
+    lo, hi = np.abs(dy[..., :h]), np.abs(dy[..., h:])
+    e = 3 * F32 * (lo + hi)
+    (dx, dg), (bx, bg) = rmsnorm_backward(x, gain, dz, eps,
+                                          np.concatenate((e, e), -1))
+    return (dx, dg), (bx + BF16 * (np.abs(dx) + bx), bg)
+
+
+def token_loss(logits, target, weight):
+    """logits [R, V], target [R], weight [R] -> (loss, dlogits), (their
+    bounds).  Rows without loss: target outside the row, or weight 0.
+
+    fp32: an exponent x - m and its product with log2 e are off by 2 F32 of
+    their size, v_exp_f32 by a step, a sum of V terms by V F32 of itself at
+    most (thread sums and trees: V / 64 + 16 is above any split), the
+    logarithm by two steps of its size and the sum's relative error."""
+    R, V = logits.shape
+    loss, d = np.zeros(R), np.zeros((R, V))
+    bl, bd = np.zeros(R), np.zeros((R, V))
+    for r in range(R):
+        t, w = target[r], weight[r]
+        if not 0 <= t < V or w == 0:
+            continue
+        m = logits[r].max()
+        if m == -np.inf:
+            loss[r] = w * np.inf
+            continue
+        z = logits[r] - m
+        e = np.exp(z)
+        s = e.sum()
+        a = np.abs(np.where(e > 0, z, 0.0))
+        sum_err = F32 * (V / 64 + 16) + (e * (3 * F32 * a + 2 * F32)).sum() / s
+        loss[r] = w * (np.log(s) - z[t])
+        bl[r] = 1.01 * abs(w) * (sum_err + 3 * F32 * (np.log(s) + 2) + (
+            4 * F32 * abs(z[t]) if z[t] > -np.inf else 0.0))
+        p = e / s
+        d[r] = w * p
+        d[r, t] -= w
+        # v_exp_f32 flushes below 2^-126
+        bd[r] = abs(w) * (p * (sum_err + 3 * F32 * a + 6 * F32) + 2.0 ** -125)
+        bd[r, t] += 2 * F32 * abs(w)
+    return (loss, d), (bl, 1.01 * bd)

@@ -21,7 +21,8 @@ LIB = os.path.join(PKG, "libwedlm.so")
 
 SOURCES = ["reorder.hip", "window_attn.hip", "score.hip", "commit.hip",
            "lm_head.hip", "model.hip", "dual_stream.hip",
-           "attn_backward.hip", "abi.hip"]
+           "attn_backward.hip", "norm_backward.hip",
+           "token_loss.hip", "abi.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -107,6 +107,21 @@ def _load():
     lib.wedlm_dual_stream_attn_backward.argtypes = (
         [P] * 6 + [I32] * 6 + [F] + [P] * 4 + [SZ, P])
     lib.wedlm_dual_stream_attn_backward.restype = ctypes.c_int
+    lib.wedlm_rmsnorm_backward_workspace_size.argtypes = [I32, I32]
+    lib.wedlm_rmsnorm_backward_workspace_size.restype = SZ
+    lib.wedlm_rmsnorm_backward.argtypes = [P, P, P, P, I32, I32, F, P, P, P,
+                                           SZ, P]
+    lib.wedlm_rmsnorm_backward.restype = ctypes.c_int
+    lib.wedlm_qk_norm_rope_backward_workspace_size.argtypes = [I32] * 4
+    lib.wedlm_qk_norm_rope_backward_workspace_size.restype = SZ
+    lib.wedlm_qk_norm_rope_backward.argtypes = (
+        [P] * 7 + [I32] * 4 + [D_, F] + [P] * 4 + [SZ, P])
+    lib.wedlm_qk_norm_rope_backward.restype = ctypes.c_int
+    lib.wedlm_token_loss_workspace_size.argtypes = [I32, I32]
+    lib.wedlm_token_loss_workspace_size.restype = SZ
+    lib.wedlm_token_loss.argtypes = [P, I32, I64, P, P, I32, I32, P, P, P, SZ,
+                                     P]
+    lib.wedlm_token_loss.restype = ctypes.c_int
     lib.wedlm_strerror.argtypes = [ctypes.c_int]
     lib.wedlm_strerror.restype = ctypes.c_char_p
     lib.wedlm_version.argtypes = []
@@ -131,7 +146,11 @@ EXPORTED = ["wedlm_reorder", "wedlm_window_attn_workspace_size",
             "wedlm_model_forward", "wedlm_commit_layers",
             "wedlm_dual_stream_attn_workspace_size", "wedlm_dual_stream_attn",
             "wedlm_dual_stream_attn_backward_workspace_size",
-            "wedlm_dual_stream_attn_backward"]
+            "wedlm_dual_stream_attn_backward",
+            "wedlm_rmsnorm_backward_workspace_size", "wedlm_rmsnorm_backward",
+            "wedlm_qk_norm_rope_backward_workspace_size",
+            "wedlm_qk_norm_rope_backward", "wedlm_token_loss_workspace_size",
+            "wedlm_token_loss"]
 
 # decoding rules of wedlm_commit_rule (include/wedlm.h)
 RULE_STREAMING, RULE_BLOCK, RULE_ONE_TOKEN = 0, 1, 2
@@ -728,7 +747,7 @@ class Decoder:
 
 
 # ---------------------------------------------------------------------------
-# training-time attention (include/wedlm_train.h)
+# training (include/wedlm_train.h)
 # ---------------------------------------------------------------------------
 
 def wedlm_dual_stream_attn_workspace_size(n_seq, L, block, Hq, Hkv, D) -> int:
@@ -796,3 +815,102 @@ def wedlm_dual_stream_attn_backward(q, k, v, block: int, out, lse, dout, dq,
         _t(dk, "dk", _BF16, ks), _t(dv, "dv", _BF16, ks),
         _t(workspace, "workspace", _U8), workspace.numel(), _stream())
     _check(code, "wedlm_dual_stream_attn_backward")
+
+
+def _workspace(workspace, need: int, device):
+    """Address and bytes of a workspace, allocated here if none is given."""
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return _t(workspace, "workspace", _U8), workspace.numel()
+
+
+def wedlm_rmsnorm_backward_workspace_size(M, Hd) -> int:
+    return int(_load().wedlm_rmsnorm_backward_workspace_size(M, Hd))
+
+
+def wedlm_rmsnorm_backward(x, gain, eps: float, dy, dx, dgain=None, dres=None,
+                           workspace=None) -> None:
+    """Gradients of wedlm_rmsnorm: x [M, Hd] fp32, gain [Hd] bf16 and dy
+    [M, Hd] bf16 -> dx [M, Hd] fp32 (plus dres, which may be dx itself),
+    dgain [Hd] fp32 (optional).  A workspace is allocated here if dgain needs
+    one and none is given."""
+    M, Hd = x.shape
+    ws, nbytes = None, 0
+    if dgain is not None:
+        ws, nbytes = _workspace(
+            workspace, wedlm_rmsnorm_backward_workspace_size(M, Hd), x.device)
+    code = _load().wedlm_rmsnorm_backward(
+        _t(x, "x", _F32), _t(gain, "gain", _BF16, (Hd,)),
+        _t(dy, "dy", _BF16, (M, Hd)),
+        _t(dres, "dres", _F32, (M, Hd), allow_none=True), M, Hd, float(eps),
+        _t(dx, "dx", _F32, (M, Hd)),
+        _t(dgain, "dgain", _F32, (Hd,), allow_none=True), ws, nbytes,
+        _stream())
+    _check(code, "wedlm_rmsnorm_backward")
+
+
+def wedlm_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D) -> int:
+    return int(_load().wedlm_qk_norm_rope_backward_workspace_size(M, Hq, Hkv,
+                                                                  D))
+
+
+def wedlm_qk_norm_rope_backward(qkv, q_gain, k_gain, pos_ids,
+                                rope_theta: float, eps: float, dq, dk, dv,
+                                dqkv, dq_gain=None, dk_gain=None,
+                                workspace=None) -> None:
+    """Gradients of wedlm_qk_norm_rope: dq [M, Hq, D], dk, dv [M, Hkv, D] and
+    the forward's inputs -> dqkv like qkv (bf16), dq_gain, dk_gain [D] fp32
+    (optional).  A workspace is allocated here if the gains' gradients need
+    one and none is given."""
+    M, Hq, D = dq.shape
+    Hkv = dk.shape[1]
+    ws, nbytes = None, 0
+    if dq_gain is not None or dk_gain is not None:
+        ws, nbytes = _workspace(
+            workspace,
+            wedlm_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D),
+            qkv.device)
+    rows = (M, (Hq + 2 * Hkv) * D)
+    code = _load().wedlm_qk_norm_rope_backward(
+        _t(qkv, "qkv", _BF16, rows), _t(q_gain, "q_gain", _BF16, (D,)),
+        _t(k_gain, "k_gain", _BF16, (D,)),
+        _t(pos_ids, "pos_ids", _I32, (M,)), _t(dq, "dq", _BF16),
+        _t(dk, "dk", _BF16, (M, Hkv, D)), _t(dv, "dv", _BF16, (M, Hkv, D)), M,
+        Hq, Hkv, D, float(rope_theta), float(eps),
+        _t(dqkv, "dqkv", _BF16, rows),
+        _t(dq_gain, "dq_gain", _F32, (D,), allow_none=True),
+        _t(dk_gain, "dk_gain", _F32, (D,), allow_none=True), ws, nbytes,
+        _stream())
+    _check(code, "wedlm_qk_norm_rope_backward")
+
+
+LOGITS_F32, LOGITS_BF16 = 0, 1
+
+
+def wedlm_token_loss_workspace_size(R, V) -> int:
+    return int(_load().wedlm_token_loss_workspace_size(R, V))
+
+
+def wedlm_token_loss(logits, target, loss, weight=None, dlogits=None,
+                     workspace=None, V: Optional[int] = None) -> None:
+    """logits [R, row_stride] fp32 or bf16, target [R] int32 (negative: no
+    loss), weight [R] fp32 (optional) -> loss [R] fp32 and dlogits like
+    logits (optional; may be logits itself).  V defaults to the last
+    dimension.  A workspace is allocated here if one is needed and none is
+    given."""
+    R, stride = logits.shape
+    V = stride if V is None else V
+    half = logits.dtype == torch.bfloat16
+    types = (torch.bfloat16,) if half else _F32
+    need = wedlm_token_loss_workspace_size(R, V)
+    ws, nbytes = None, 0
+    if need:
+        ws, nbytes = _workspace(workspace, need, logits.device)
+    code = _load().wedlm_token_loss(
+        _t(logits, "logits", types), LOGITS_BF16 if half else LOGITS_F32,
+        stride, _t(target, "target", _I32, (R,)),
+        _t(weight, "weight", _F32, (R,), allow_none=True), R, V,
+        _t(loss, "loss", _F32, (R,)),
+        _t(dlogits, "dlogits", types, (R, stride), allow_none=True), ws,
+        nbytes, _stream())
+    _check(code, "wedlm_token_loss")

@@ -49,3 +49,40 @@ def test_attention_backward_refusals():
              [(12, 0.0, -1), (12, float("nan"), -1), (12, float("inf"), -1),
               (7, 120, -2), (8, 33, -2), (9, 3, -2), (11, 32, -2),
               (16, None, -3), (17, need - 1, -3)])
+
+
+def test_rmsnorm_backward_refusals():
+    lib = _lib()
+    ws = lib.wedlm_rmsnorm_backward_workspace_size
+    assert ws(0, 64) == ws(4, 0) == ws(4, 66) == 0
+    need = ws(3, 64)
+    assert need == 3 * 64 * 4
+    args = [F] * 4 + [3, 64, 1e-6, F, F, F, need, None]
+    refusals(lib.wedlm_rmsnorm_backward, args,
+             [(i, None, -1) for i in (0, 1, 2, 7)] +
+             [(6, 0.0, -1), (6, float("nan"), -1), (4, 0, -2), (5, 2, -2),
+              (5, 66, -2), (9, None, -3), (10, need - 1, -3)])
+
+
+def test_qk_norm_rope_backward_refusals():
+    lib = _lib()
+    ws = lib.wedlm_qk_norm_rope_backward_workspace_size
+    assert ws(0, 4, 2, 64) == ws(3, 4, 2, 96) == ws(3, 4, 0, 64) == 0
+    assert ws(3, 1 << 24, 2, 128) == 0
+    need = ws(3, 4, 2, 64)
+    args = [F] * 7 + [3, 4, 2, 64, 1e6, 1e-6] + [F] * 4 + [need, None]
+    refusals(lib.wedlm_qk_norm_rope_backward, args,
+             [(i, None, -1) for i in (0, 1, 2, 3, 4, 5, 6, 13)] +
+             [(11, 1.0, -1), (12, 0.0, -1), (7, 0, -2), (8, 0, -2),
+              (9, -1, -2), (10, 32, -2), (16, None, -3), (17, need - 1, -3)])
+
+
+def test_token_loss_refusals():
+    lib = _lib()
+    ws = lib.wedlm_token_loss_workspace_size
+    assert ws(0, 64) == ws(4, 0) == ws(-1, -1) == 0
+    need = ws(3, 64)
+    args = [F, 0, 64, F, F, 3, 64, F, F, F, need, None]
+    refusals(lib.wedlm_token_loss, args,
+             [(i, None, -1) for i in (0, 3, 7)] +
+             [(1, 2, -1), (1, -1, -1), (2, 63, -2), (5, 0, -2), (6, 0, -2)])
