@@ -42,8 +42,11 @@ def hipcc() -> str:
 
 
 # per-file flags: the attention's max reductions need no NaN handling
-# (infinities are still honoured; masked scores are -inf)
-FILE_FLAGS = {"window_attn.hip": ["-fno-honor-nans"]}
+# (infinities are still honoured; masked scores are -inf).  Its backward keeps
+# its accumulators in the accumulation registers by itself; there the
+# compiler's MFMAs write plain ones.
+FILE_FLAGS = {"window_attn.hip": ["-fno-honor-nans"],
+              "attn_backward.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _compile(src: str) -> str:

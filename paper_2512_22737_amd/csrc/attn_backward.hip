@@ -42,6 +42,7 @@ constexpr int kOwn = 64;              // rows or keys that a wave owns
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKeysPerWg = kWaves * kOwn;
+constexpr int kSlots = 4;             // ring of tile pairs, three ahead
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -63,20 +64,25 @@ struct BwdArgs {
   float scale, scale_log2;
 };
 
-// LDS tile of 32 rows of D bf16: 16-byte chunk c of row r sits in slot
-// c ^ swz(r) of its row.  swz takes all values over rows that share a bank
-// phase (16 rows of one chunk, a row read, hit different banks) and its high
-// bits differ over four consecutive rows (so do a column read's).
+// LDS tile of 32 rows of D bf16, as it is loaded: one 1 KB load instruction
+// fills a group of 512 / D whole rows, groups are 16 bytes apart.  Chunk c (16
+// bytes) of row i of its group sits in slot c ^ swz(i).  Rows read together
+// (16 rows of one chunk; four rows of 64 bytes by columns) then hit different
+// banks, and the reads of a lane differ by constants but for the exclusive or
+// with its row: few address registers.
 template <int D>
 struct RowTile {
-  static constexpr int bytes = kRows * D * 2;
+  static constexpr int per_group = 512 / D;         // rows: 4 or 8
+  static constexpr int groups = kRows / per_group;
+  static constexpr int group_bytes = 1024 + 16;
+  static constexpr int bytes = groups * group_bytes;
   static constexpr int chunks = D / 8;
-  __device__ static __forceinline__ int swz(int r) {
-    return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3)
-                    : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  __device__ static __forceinline__ int swz(int i) {
+    return D == 128 ? i << 2 : ((i & 2) << 1) | ((i & 4) >> 1);
   }
   __device__ static __forceinline__ int off(int r, int c) {
-    return r * 2 * D + ((c ^ swz(r)) << 4);
+    const int i = r % per_group;
+    return r / per_group * group_bytes + i * 2 * D + ((c ^ swz(i)) << 4);
   }
 };
 
@@ -90,50 +96,120 @@ __device__ __forceinline__ bf16x8_t load8(const uint16_t* p) {
   return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u16x8_t*>(p));
 }
 
-// Rows as the first operand: lane's row, values 16 kk + 8 hf .. + 7.
+// A lane's addresses into a tile.
 template <int D>
-__device__ __forceinline__ bf16x8_t row_frag(const char* tile, int kk) {
-  const int l = lane_id();
-  return load8(reinterpret_cast<const uint16_t*>(
-      tile + RowTile<D>::off(row_of_m(l & 31), 2 * kk + (l >> 5))));
+struct Reader {
+  using T = RowTile<D>;
+  int row[4], col[4];
+  __device__ __forceinline__ Reader() {
+    const int l = lane_id(), i = l & 15, hf = l >> 5;
+    // rows: lane's row, chunks 2 kk + hf; kk / 2 (D = 64: kk) meets the swizzle
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      row[x] = T::off(row_of_m(l & 31), (D == 128 ? 4 : 2) * x + hf);
+    // columns: four rows on four lanes each, 16 columns per 16 lanes; the
+    // block m of 32 columns (D = 64: and the half of eight rows) meets it
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int m = D == 128 ? x : x >> 1, j = D == 128 ? 0 : x & 1;
+      col[x] = T::off(8 * hf + 4 * j + (i >> 2),
+                      4 * m + 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) +
+               (i & 1) * 8;
+    }
+  }
+  // lane's row, values 16 kk + 8 hf .. + 7
+  __device__ __forceinline__ bf16x8_t rows(const char* tile, int kk) const {
+    return load8(reinterpret_cast<const uint16_t*>(
+        tile + (D == 128 ? row[kk >> 1] + (kk & 1) * 32 : row[kk])));
+  }
+  // lane's column 32 m + lane % 32, rows 16 h + 8 hf .. + 7
+  __device__ __forceinline__ bf16x8_t cols(const char* tile, int h,
+                                           int m) const {
+    s16x4_t x[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4_t*)(tile + h * (16 / T::per_group) * T::group_bytes +
+                         (D == 128 ? col[m] + j * T::group_bytes
+                                   : col[2 * m + j])));
+    return __builtin_bit_cast(
+        bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// Loads of a pair of tiles (rows first .. first+31 of two arrays of the same
+// row stride) straight into LDS, the workgroup's waves sharing the groups;
+// rows past the last one re-read it.  kCount load instructions per wave.
+template <int D>
+struct PairLoader {
+  using T = RowTile<D>;
+  static constexpr int kCount = 2 * T::groups / kWaves;
+  int row[kCount], chunk[kCount];    // lane's row, byte in it
+  int wave;
+  __device__ __forceinline__ PairLoader(int wave_) : wave(wave_) {
+#pragma unroll
+    for (int u = 0; u < kCount; ++u) {
+      const int g = (wave * kCount + u) % T::groups;
+      const int i = lane_id() / T::chunks;
+      row[u] = g * T::per_group + i;
+      chunk[u] = ((lane_id() % T::chunks) ^ T::swz(i)) * 16;
+    }
+  }
+  // a, b: first rows; left: rows from there to the last one; dst: LDS address
+  // of the pair
+  __device__ __forceinline__ void load(const uint16_t* a, const uint16_t* b,
+                                       int stride_bytes, int left,
+                                       uint32_t dst) const {
+#pragma unroll
+    for (int u = 0; u < kCount; ++u) {
+      const int g = wave * kCount + u;
+      const int r = min(row[u], left);
+      load_to_lds16<false>(
+          buffer_rsrc(g < T::groups ? a : b, 31 * stride_bytes + 2 * D),
+          static_cast<int>(__umul24(r, stride_bytes)) + chunk[u],
+          __builtin_amdgcn_readfirstlane(dst + g * T::group_bytes));
+    }
+  }
+};
+
+// One dword per lane to LDS: lane l's at lds_addr + 4 l.
+__device__ __forceinline__ void load_to_lds4(i32x4_t rsrc, int voff,
+                                             uint32_t lds_addr) {
+  asm volatile("buffer_load_dword %0, %1, 0 offen lds"
+               :
+               : "v"(voff), "s"(rsrc), "{m0}"(lds_addr));
 }
 
-// Columns: lane's column 32 m + lane % 32, rows 16 h + 8 hf .. + 7.
-template <int D>
-__device__ __forceinline__ bf16x8_t col_frag(const char* tile, int h, int m) {
-  const int l = lane_id(), i = l & 15;
-  const int c = 4 * m + 2 * ((l >> 4) & 1) + ((i & 3) >> 1);
-  s16x4_t x[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int r = 16 * h + 8 * (l >> 5) + 4 * j + (i >> 2);
-    x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (lds_s16x4_t*)(tile + RowTile<D>::off(r, c) + (i & 1) * 8));
-  }
-  return __builtin_bit_cast(
-      bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
-// A tile of rows first .. first+31 of a [.., rows, heads, D] array (base: row
-// 0 of one head, stride in elements) into LDS; rows past the last one re-read
-// it.
-template <int D>
-__device__ __forceinline__ void stage(const uint16_t* base, int64_t stride,
-                                      int first, int last, char* tile) {
-  constexpr int C = RowTile<D>::chunks;
-#pragma unroll
-  for (int u = 0; u < kRows * C / kThreads; ++u) {
-    const int i = threadIdx.x + u * kThreads;
-    const int r = i / C, c = i % C;
-    *reinterpret_cast<u16x8_t*>(tile + RowTile<D>::off(r, c)) =
-        *reinterpret_cast<const u16x8_t*>(base + min(first + r, last) * stride +
-                                          c * 8);
-  }
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((lds_void_t*)p));
 }
 
 __device__ __forceinline__ floatx16_t mfma(bf16x8_t a, bf16x8_t b,
                                            floatx16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// acc += a b with the accumulator in the accumulation registers throughout:
+// with the score tiles in plain registers neither file overflows (left to
+// itself the compiler moves hundreds of accumulators per tile).  It does not
+// know that this is an MFMA, so the two wait states after a VALU write of an
+// operand are here, and drain() before anything else reads an accumulator.
+__device__ __forceinline__ void mfma_acc(floatx16_t& acc, bf16x8_t a,
+                                         bf16x8_t b) {
+  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0"
+               : "+a"(acc)
+               : "v"(a), "v"(b));
+}
+
+// The accumulators of the last mfma_acc() are written (18 wait states).
+template <int N>
+__device__ __forceinline__ void drain(floatx16_t (&acc)[2][N]) {
+  asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc[0][0]));
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int m = 0; m < N; ++m) asm volatile("" : "+a"(acc[b][m]));
 }
 
 // dq: workgroup = four units (64-position chunk, head) of one stream and kv
@@ -144,9 +220,8 @@ __attribute__((amdgpu_waves_per_eu(1)))
 void dq_kernel(BwdArgs a) {
   constexpr int NK = D / 16, NM = D / 32;
   using T = RowTile<D>;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * T::bytes];
-  char* kt = smem;
-  char* vt = smem + T::bytes;
+  constexpr int kPair = 2 * T::bytes;
+  __shared__ __attribute__((aligned(1024))) char smem[kSlots * kPair];
   const int chunks = (a.L + kOwn - 1) / kOwn;
   const int groups = (chunks * a.G + kWaves - 1) / kWaves;
   int wg = blockIdx.x;
@@ -203,66 +278,94 @@ void dq_kernel(BwdArgs a) {
 #pragma unroll
     for (int m = 0; m < NM; ++m) acc[b][m] = floatx16_t{};
 
-  // one key tile (keys j0 .. j0+31 of a stream); key j is seen if
-  // b0 <= j < b1 of its row
-  auto tile = [&](int j0, const int (&b0)[2], const int (&b1)[2]) {
+  const Reader<D> rd;
+  // one key tile: keys j0 .. j0+31 of the memory stream, or of the rows' own
+  auto tile = [&](const char* kt, int j0, bool own, bool mask) {
+    const char* vt = kt + T::bytes;
     floatx16_t s[2] = {}, dp[2] = {};
+    bf16x8_t f[NK];
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      const bf16x8_t f = row_frag<D>(kt, kk);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) s[b] = mfma(f, qf[b][kk], s[b]);
-    }
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      const bf16x8_t f = row_frag<D>(vt, kk);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) dp[b] = mfma(f, dof[b][kk], dp[b]);
-    }
-    bf16x8_t ds[2][2];
+    for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(kt, kk);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
+      for (int kk = 0; kk < NK; ++kk) s[b] = mfma(f[kk], qf[b][kk], s[b]);
+    if (mask) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = j0 + 16 * (e >> 3) + 8 * hf + (e & 7);
+          const int from = own ? lo[b] : 0, to = own || !stream ? hi[b] : lo[b];
+          s[b][e] = j >= from && j < to ? s[b][e] : kNegInf;
+        }
+    }
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(vt, kk);
+    bf16x8_t ds[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) dp[b] = mfma(f[kk], dof[b][kk], dp[b]);
+#pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int j = j0 + 16 * (e >> 3) + 8 * hf + (e & 7);
-        const float x = j >= b0[b] && j < b1[b] ? s[b][e] : kNegInf;
         const float p = __builtin_amdgcn_exp2f(
-            __builtin_fmaf(x, a.scale_log2, -lse2[b]));
+            __builtin_fmaf(s[b][e], a.scale_log2, -lse2[b]));
         ds[b][e >> 3][e & 7] = static_cast<__bf16>(p * (dp[b][e] - delta[b]));
       }
+    }
+    bf16x8_t g[2][NM];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int m = 0; m < NM; ++m) {
-        const bf16x8_t f = col_frag<D>(kt, h, m);
+      for (int m = 0; m < NM; ++m) g[h][m] = rd.cols(kt, h, m);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) acc[b][m] = mfma(f, ds[b][h], acc[b][m]);
-      }
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+          mfma_acc(acc[b][m], g[h][m], ds[b][h]);
   };
-  const int64_t kstride = static_cast<int64_t>(a.Hkv) * D;
-  auto walk = [&](int from, int to, int key_stream, const int (&b0)[2],
-                  const int (&b1)[2]) {
-    const int64_t base =
-        ((static_cast<int64_t>(sq) * 2 + key_stream) * a.L * a.Hkv + kvh) * D;
-    for (int j0 = from / kRows * kRows; j0 < to; j0 += kRows) {
-      __syncthreads();
-      stage<D>(a.k + base, kstride, j0, a.L - 1, kt);
-      stage<D>(a.v + base, kstride, j0, a.L - 1, vt);
-      __syncthreads();
-      tile(j0, b0, b1);
-    }
-  };
-  // positions of the workgroup's rows
+  // tiles: memory keys from 0, then for prediction rows their own blocks'
   const int first = grp * kWaves / a.G * kOwn;
   const int end = min(a.L, (min(grp * kWaves + kWaves - 1, last_unit) / a.G +
                             1) * kOwn);
-  const int zero[2] = {0, 0};
-  if (stream) {
-    walk(0, (end - 1) / a.block * a.block, 0, zero, lo);
-    walk(first / a.block * a.block, end, 1, lo, hi);
-  } else {
-    walk(0, end, 0, zero, hi);
+  const int n_mem =
+      ((stream ? (end - 1) / a.block * a.block : end) + kRows - 1) / kRows;
+  const int own0 = first / a.block * a.block / kRows;
+  const int n = n_mem + (stream ? (end + kRows - 1) / kRows - own0 : 0);
+  const int stride = a.Hkv * D * 2;
+  const int64_t kv0 = static_cast<int64_t>(sq) * 2 * a.L;
+  const PairLoader<D> ld(wave);
+  const uint32_t lds0 = lds_address(smem);
+  auto fetch = [&](int i) {
+    const int ic = min(i, n - 1);
+    const bool own = ic >= n_mem;
+    const int j0 = (own ? own0 + ic - n_mem : ic) * kRows;
+    const int64_t o = ((kv0 + (own ? a.L : 0) + j0) * a.Hkv + kvh) * D;
+    ld.load(a.k + o, a.v + o, stride, a.L - 1 - j0,
+            lds0 + (i % kSlots) * kPair);
+  };
+  // memory keys that all of the wave's rows see
+  const int full = stream ? p0 / a.block * a.block : p0 + 1;
+#pragma unroll
+  for (int i = 0; i < kSlots - 1; ++i) fetch(i);
+  for (int i = 0; i < n; ++i) {
+    // this wave's loads of tile i, then everybody's; the barrier also frees
+    // the slot of tile i - 1
+    wait_vmcnt<(kSlots - 2) * PairLoader<D>::kCount>();
+    __syncthreads();
+    fetch(i + kSlots - 1);
+    const char* kt = smem + (i % kSlots) * kPair;
+    const bool own = i >= n_mem;
+    const int j0 = (own ? own0 + i - n_mem : i) * kRows;
+    // (a tile that this wave's rows do not see is computed all the same, P = 0:
+    // the waves are in step, and a branch around the accumulators costs copies)
+    tile(kt, j0, own, own || j0 + kRows > full);
   }
+  wait_vmcnt<0>();      // surplus loads land before the LDS is given up
+  drain(acc);
   if (!live) return;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
@@ -290,10 +393,11 @@ __attribute__((amdgpu_waves_per_eu(1)))
 void dkv_kernel(BwdArgs a) {
   constexpr int NK = D / 16, NM = D / 32;
   using T = RowTile<D>;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * T::bytes];
-  __shared__ float ldt[2 * kRows];
-  char* qt = smem;
-  char* dot = smem + T::bytes;
+  constexpr int kPair = 2 * T::bytes;
+  constexpr int kSlot = kPair + 2 * kRows * 4;     // rows' lse and D behind
+  __shared__ __attribute__((aligned(1024))) char smem[kSlots * kSlot];
+  // V of the workgroup's keys, in tiles of 32
+  __shared__ __attribute__((aligned(1024))) char vsm[kKeysPerWg / kRows * T::bytes];
   const int tiles = (a.L + kKeysPerWg - 1) / kKeysPerWg;
   const int n_mem = a.n_seq * a.Hkv * tiles * a.nsplit;
   int wg = blockIdx.x;
@@ -310,7 +414,7 @@ void dkv_kernel(BwdArgs a) {
   const int lane = lane_id(), col = lane & 31, hf = lane >> 5;
   const int kw0 = j0 + wave * kOwn;
 
-  bf16x8_t kf[2][NK], vf[2][NK];
+  bf16x8_t kf[2][NK];
   // rows that see this lane's keys: memory rows key .. L-1 and prediction
   // rows next .. L-1, or for a prediction key rows key .. next-1 (next: the
   // block after the key's)
@@ -325,7 +429,9 @@ void dkv_kernel(BwdArgs a) {
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       kf[b][kk] = load8(a.k + o + kk * 16 + hf * 8);
-      vf[b][kk] = load8(a.v + o + kk * 16 + hf * 8);
+      *reinterpret_cast<u16x8_t*>(vsm + (2 * wave + b) * T::bytes +
+                                  T::off(col, 2 * kk + hf)) =
+          *reinterpret_cast<const u16x8_t*>(a.v + o + kk * 16 + hf * 8);
     }
     if (key[b] >= a.L) key[b] = next[b] = 0x40000000;   // seen by no row
   }
@@ -335,50 +441,80 @@ void dkv_kernel(BwdArgs a) {
 #pragma unroll
     for (int m = 0; m < NM; ++m) dk[b][m] = dv[b][m] = floatx16_t{};
 
-  // one tile of rows p0 .. p0+31; row p sees the lane's key if r0 <= p < r1
-  auto tile = [&](int p0, const int (&r0)[2], const int (&r1)[2]) {
+  const Reader<D> rd;
+  // the wave's V as the second operand: lane's key, rows in plain order
+  int vrow[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+    vrow[x] = T::off(col, (D == 128 ? 4 : 2) * x + hf) + 2 * wave * T::bytes;
+  auto vfrag = [&](int b, int kk) {
+    return load8(reinterpret_cast<const uint16_t*>(
+        vsm + b * T::bytes +
+        (D == 128 ? vrow[kk >> 1] + (kk & 1) * 32 : vrow[kk])));
+  };
+  // one tile of rows p0 .. p0+31
+  auto tile = [&](const char* qt, int p0, bool pred, bool mask) {
+    const char* dot = qt + T::bytes;
+    const float* ldt = reinterpret_cast<const float*>(qt + kPair) + 8 * hf;
     floatx16_t s[2] = {}, dp[2] = {};
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
-      const bf16x8_t f = row_frag<D>(qt, kk);
+      const bf16x8_t f = rd.rows(qt, kk);
 #pragma unroll
       for (int b = 0; b < 2; ++b) s[b] = mfma(f, kf[b][kk], s[b]);
     }
+    if (mask) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int p = p0 + 16 * (e >> 3) + 8 * hf + (e & 7);
+          const int from = pred ? next[b] : key[b];
+          const int to = stream ? next[b] : a.L;
+          s[b][e] = p >= from && p < to ? s[b][e] : kNegInf;
+        }
+    }
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
-      const bf16x8_t f = row_frag<D>(dot, kk);
+      const bf16x8_t f = rd.rows(dot, kk);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) dp[b] = mfma(f, vf[b][kk], dp[b]);
+      for (int b = 0; b < 2; ++b) dp[b] = mfma(f, vfrag(b, kk), dp[b]);
     }
     bf16x8_t pb[2][2], ds[2][2];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int r = 16 * (e >> 3) + 8 * hf + (e & 7);
-      const float l2 = ldt[r], d = ldt[kRows + r];
+      const float l2 = ldt[16 * (e >> 3) + (e & 7)];
+      const float d = ldt[kRows + 16 * (e >> 3) + (e & 7)];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const float x = p0 + r >= r0[b] && p0 + r < r1[b] ? s[b][e] : kNegInf;
         const float p =
-            __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale_log2, -l2));
+            __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], a.scale_log2, -l2));
         pb[b][e >> 3][e & 7] = static_cast<__bf16>(p);
         ds[b][e >> 3][e & 7] = static_cast<__bf16>(p * (dp[b][e] - d));
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int m = 0; m < NM; ++m) {
-        const bf16x8_t f = col_frag<D>(dot, h, m);
-        const bf16x8_t g = col_frag<D>(qt, h, m);
+        const bf16x8_t f = rd.cols(dot, h, m);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          dv[b][m] = mfma(f, pb[b][h], dv[b][m]);
-          dk[b][m] = mfma(g, ds[b][h], dk[b][m]);
-        }
+        for (int b = 0; b < 2; ++b) mfma_acc(dv[b][m], f, pb[b][h]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int m = 0; m < NM; ++m) {
+        const bf16x8_t f = rd.cols(qt, h, m);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) mfma_acc(dk[b][m], f, ds[b][h]);
       }
   };
   // items: row tiles t from the last down, in each the streams that see the
-  // keys and their heads
+  // keys (memory, prediction) and their heads.  Every workgroup of a kv head
+  // starts at the same rows, which they then find in the L2
   const int kend = min(a.L, j0 + kKeysPerWg);
   int t_hi = a.T, t_mid, t_lo = j0 / kRows;
   if (stream) {
@@ -392,37 +528,66 @@ void dkv_kernel(BwdArgs a) {
   const int it0 = static_cast<int>(static_cast<int64_t>(n_items) * split / nsplit);
   const int it1 =
       static_cast<int>(static_cast<int64_t>(n_items) * (split + 1) / nsplit);
-  const int64_t qstride = static_cast<int64_t>(a.Hq) * D;
-  const int zero[2] = {0, 0}, all[2] = {a.L, a.L};
-  for (int it = it0; it < it1; ++it) {
+  // an item: its row tile and (stream, head of the group)
+  struct Item {
     int t, sg;
-    if (it < n1) {
-      t = t_hi - 1 - it / (2 * a.G);
-      sg = it % (2 * a.G);
-    } else {
-      t = t_mid - 1 - (it - n1) / a.G;
-      sg = (it - n1) % a.G;
+  };
+  auto item_at = [&](int it) {
+    return it < n1 ? Item{t_hi - 1 - it / (2 * a.G), it % (2 * a.G)}
+                   : Item{t_mid - 1 - (it - n1) / a.G, (it - n1) % a.G};
+  };
+  auto next_item = [&](Item x) {
+    ++x.sg;
+    if (x.sg == (x.t >= t_mid ? 2 * a.G : a.G)) {
+      x.sg = 0;
+      --x.t;
     }
-    const int row_stream = stream ? 1 : sg / a.G;
-    const int head = kvh * a.G + sg % a.G;
-    const int64_t row0 = (static_cast<int64_t>(sq) * 2 + row_stream) * a.L;
-    const int64_t base = (row0 * a.Hq + head) * D;
-    __syncthreads();
-    stage<D>(a.q + base, qstride, t * kRows, a.L - 1, qt);
-    stage<D>(a.dout + base, qstride, t * kRows, a.L - 1, dot);
-    if (threadIdx.x < 2 * kRows)
-      ldt[threadIdx.x] =
-          a.ld[(((static_cast<int64_t>(sq) * a.Hq + head) * 2 + row_stream) *
-                    a.T + t) * 2 * kRows + threadIdx.x];
-    __syncthreads();
-    if (stream)
-      tile(t * kRows, key, next);
-    else if (row_stream)
-      tile(t * kRows, next, all);
-    else
-      tile(t * kRows, key, all);
+    return x;
+  };
+  const PairLoader<D> loader(wave);
+  const uint32_t lds0 = lds_address(smem);
+  const int stride = a.Hq * D * 2;
+  Item ahead = item_at(it0);
+  int n_ahead = it0;
+  auto fetch = [&](int slot) {
+    const int rs = stream || ahead.sg >= a.G ? 1 : 0;
+    const int head = kvh * a.G + (ahead.sg >= a.G ? ahead.sg - a.G : ahead.sg);
+    const int p0 = ahead.t * kRows;
+    const int64_t o =
+        (((static_cast<int64_t>(sq) * 2 + rs) * a.L + p0) * a.Hq + head) * D;
+    const uint32_t dst = lds0 + slot * kSlot;
+    loader.load(a.q + o, a.dout + o, stride, a.L - 1 - p0, dst);
+    // every wave the same 256 bytes, so that all wait for as many loads
+    const float* l = a.ld + (((static_cast<int64_t>(sq) * a.Hq + head) * 2 + rs) *
+                                 a.T + ahead.t) * 2 * kRows;
+    load_to_lds4(buffer_rsrc(l, 2 * kRows * 4), lane * 4,
+                 __builtin_amdgcn_readfirstlane(dst + kPair));
+    // past the end: the last item again, into a slot that nobody reads
+    if (++n_ahead < it1) ahead = next_item(ahead);
+  };
+  const int kwl = min(kw0 + kOwn, a.L) - 1;         // the wave's last key
+  const int next_hi = (kwl / a.block + 1) * a.block;
+  if (it0 < it1) {
+#pragma unroll
+    for (int i = 0; i < kSlots - 1; ++i) fetch(i);
   }
-  (void)zero;
+  Item cur = item_at(it0);
+  for (int it = it0, i = 0; it < it1; ++it, ++i) {
+    wait_vmcnt<(kSlots - 2) * (PairLoader<D>::kCount + 1)>();
+    __syncthreads();
+    fetch((i + kSlots - 1) % kSlots);
+    const char* qt = smem + i % kSlots * kSlot;
+    const int p0 = cur.t * kRows;
+    // a mask unless every row sees all keys of the wave
+    const bool pred = cur.sg >= a.G;        // prediction rows, memory keys
+    tile(qt, p0, pred,
+         stream || p0 < (pred ? next_hi : kwl) || p0 + kRows > a.L ||
+             kw0 + kOwn > a.L);
+    cur = next_item(cur);
+  }
+  wait_vmcnt<0>();      // surplus loads land before the LDS is given up
+  drain(dv);
+  drain(dk);
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     if (key[b] >= a.L) continue;
