@@ -42,7 +42,7 @@ constexpr int kOwn = 64;              // rows or keys that a wave owns
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKeysPerWg = kWaves * kOwn;
-constexpr int kSlots = 4;             // ring of tile pairs, three ahead
+constexpr int kSlots = 6;             // ring of tile pairs, five ahead
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -58,7 +58,7 @@ struct BwdArgs {
   uint16_t* dq;
   uint16_t* dk;
   uint16_t* dv;
-  float* ld;              // [n_seq, Hq, 2, T, 2, 32]: lse (log2 units), D
+  float* ld;              // [n_seq, Hq, 2, T, 2, 32]: -lse (log2 units), -D
   float* part;            // [2 (dk, dv)][nsplit][n_seq, L, Hkv, D], or null
   int n_seq, L, block, Hq, Hkv, G, T, nsplit;
   float scale, scale_log2;
@@ -137,38 +137,34 @@ struct Reader {
   }
 };
 
-// Loads of a pair of tiles (rows first .. first+31 of two arrays of the same
-// row stride) straight into LDS, the workgroup's waves sharing the groups;
-// rows past the last one re-read it.  kCount load instructions per wave.
+// Loads of a pair of tiles (32 rows of two arrays of the same row stride)
+// straight into LDS: of four waves two take the first array, two the second.
+// kCount load instructions per wave; rows past the last one re-read it.
 template <int D>
 struct PairLoader {
   using T = RowTile<D>;
   static constexpr int kCount = 2 * T::groups / kWaves;
-  int row[kCount], chunk[kCount];    // lane's row, byte in it
-  int wave;
-  __device__ __forceinline__ PairLoader(int wave_) : wave(wave_) {
-#pragma unroll
-    for (int u = 0; u < kCount; ++u) {
-      const int g = (wave * kCount + u) % T::groups;
-      const int i = lane_id() / T::chunks;
-      row[u] = g * T::per_group + i;
-      chunk[u] = ((lane_id() % T::chunks) ^ T::swz(i)) * 16;
-    }
+  const uint16_t* src;
+  int stride;                        // bytes
+  int row, chunk;                    // lane's first row and its chunk, bytes
+  uint32_t lds;                      // where the wave's share of a pair goes
+  __device__ __forceinline__ PairLoader(const uint16_t* a, const uint16_t* b,
+                                        int stride_elements, int wave,
+                                        uint32_t lds0)
+      : src(wave < kWaves / 2 ? a : b), stride(stride_elements * 2),
+        lds(lds0 + wave * kCount * T::group_bytes) {
+    const int i = lane_id() / T::chunks;
+    row = (wave * kCount % T::groups * T::per_group + i) * stride;
+    chunk = ((lane_id() % T::chunks) ^ T::swz(i)) * 16;
   }
-  // a, b: first rows; left: rows from there to the last one; dst: LDS address
-  // of the pair
-  __device__ __forceinline__ void load(const uint16_t* a, const uint16_t* b,
-                                       int stride_bytes, int left,
+  // instruction u: o elements from the arrays' starts to the tile's first row,
+  // left rows from there to the last one; dst: bytes from lds0 to the pair
+  __device__ __forceinline__ void load(int u, int64_t o, int left,
                                        uint32_t dst) const {
-#pragma unroll
-    for (int u = 0; u < kCount; ++u) {
-      const int g = wave * kCount + u;
-      const int r = min(row[u], left);
-      load_to_lds16<false>(
-          buffer_rsrc(g < T::groups ? a : b, 31 * stride_bytes + 2 * D),
-          static_cast<int>(__umul24(r, stride_bytes)) + chunk[u],
-          __builtin_amdgcn_readfirstlane(dst + g * T::group_bytes));
-    }
+    load_to_lds16<false>(buffer_rsrc(src + o, 31 * stride + 2 * D),
+                         min(row + u * T::per_group * stride, left * stride) +
+                             chunk,
+                         lds + dst + u * T::group_bytes);
   }
 };
 
@@ -193,14 +189,36 @@ __device__ __forceinline__ floatx16_t mfma(bf16x8_t a, bf16x8_t b,
 // acc += a b with the accumulator in the accumulation registers throughout:
 // with the score tiles in plain registers neither file overflows (left to
 // itself the compiler moves hundreds of accumulators per tile).  It does not
-// know that this is an MFMA, so the two wait states after a VALU write of an
-// operand are here, and drain() before anything else reads an accumulator.
+// know that this is an MFMA: operands that the VALU wrote go through
+// settle() first, and drain() comes before anything else reads an
+// accumulator.
 __device__ __forceinline__ void mfma_acc(floatx16_t& acc, bf16x8_t a,
                                          bf16x8_t b) {
-  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0"
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0"
                : "+a"(acc)
                : "v"(a), "v"(b));
 }
+
+// Two wait states between VALU writes of operands and an MFMA's read.
+__device__ __forceinline__ void settle(bf16x8_t (&x)[2]) {
+  asm volatile("s_nop 1" : "+v"(x[0]), "+v"(x[1]));
+}
+
+// The value is computed here, not sunk past the next branch.
+__device__ __forceinline__ void here(float& x) { asm volatile("" : "+v"(x)); }
+
+// Lane index, computed where it stands (no register from outside the loop).
+__device__ __forceinline__ int lane_here() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0"
+               : "=v"(l));
+  return l;
+}
+
+// Ends a step: what is written before it is issued before it.  The tiles are
+// written as steps of one MFMA and the vector work and LDS reads that run
+// under it (32 cycles, room for seven other instructions).
+__device__ __forceinline__ void step() { __builtin_amdgcn_sched_barrier(0); }
 
 // The accumulators of the last mfma_acc() are written (18 wait states).
 template <int N>
@@ -266,8 +284,8 @@ void dq_kernel(BwdArgs a) {
     if (live && hf == 0 && p < a.T * kRows) {
       float* ld = a.ld + ((((static_cast<int64_t>(sq) * a.Hq + head) * 2 +
                             stream) * a.T + p / kRows) * 2) * kRows + col;
-      ld[0] = p < a.L ? l2 : 0.f;
-      ld[kRows] = p < a.L ? d : 0.f;
+      ld[0] = p < a.L ? -l2 : 0.f;
+      ld[kRows] = p < a.L ? -d : 0.f;
     }
     lo[b] = stream ? pc / a.block * a.block : 0;
     hi[b] = pc + 1;
@@ -278,55 +296,6 @@ void dq_kernel(BwdArgs a) {
 #pragma unroll
     for (int m = 0; m < NM; ++m) acc[b][m] = floatx16_t{};
 
-  const Reader<D> rd;
-  // one key tile: keys j0 .. j0+31 of the memory stream, or of the rows' own
-  auto tile = [&](const char* kt, int j0, bool own, bool mask) {
-    const char* vt = kt + T::bytes;
-    floatx16_t s[2] = {}, dp[2] = {};
-    bf16x8_t f[NK];
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(kt, kk);
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) s[b] = mfma(f[kk], qf[b][kk], s[b]);
-    if (mask) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = j0 + 16 * (e >> 3) + 8 * hf + (e & 7);
-          const int from = own ? lo[b] : 0, to = own || !stream ? hi[b] : lo[b];
-          s[b][e] = j >= from && j < to ? s[b][e] : kNegInf;
-        }
-    }
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(vt, kk);
-    bf16x8_t ds[2][2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) dp[b] = mfma(f[kk], dof[b][kk], dp[b]);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float p = __builtin_amdgcn_exp2f(
-            __builtin_fmaf(s[b][e], a.scale_log2, -lse2[b]));
-        ds[b][e >> 3][e & 7] = static_cast<__bf16>(p * (dp[b][e] - delta[b]));
-      }
-    }
-    bf16x8_t g[2][NM];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int m = 0; m < NM; ++m) g[h][m] = rd.cols(kt, h, m);
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int m = 0; m < NM; ++m)
-          mfma_acc(acc[b][m], g[h][m], ds[b][h]);
-  };
   // tiles: memory keys from 0, then for prediction rows their own blocks'
   const int first = grp * kWaves / a.G * kOwn;
   const int end = min(a.L, (min(grp * kWaves + kWaves - 1, last_unit) / a.G +
@@ -335,34 +304,132 @@ void dq_kernel(BwdArgs a) {
       ((stream ? (end - 1) / a.block * a.block : end) + kRows - 1) / kRows;
   const int own0 = first / a.block * a.block / kRows;
   const int n = n_mem + (stream ? (end + kRows - 1) / kRows - own0 : 0);
-  const int stride = a.Hkv * D * 2;
-  const int64_t kv0 = static_cast<int64_t>(sq) * 2 * a.L;
-  const PairLoader<D> ld(wave);
-  const uint32_t lds0 = lds_address(smem);
-  auto fetch = [&](int i) {
-    const int ic = min(i, n - 1);
-    const bool own = ic >= n_mem;
-    const int j0 = (own ? own0 + ic - n_mem : ic) * kRows;
-    const int64_t o = ((kv0 + (own ? a.L : 0) + j0) * a.Hkv + kvh) * D;
-    ld.load(a.k + o, a.v + o, stride, a.L - 1 - j0,
-            lds0 + (i % kSlots) * kPair);
-  };
   // memory keys that all of the wave's rows see
   const int full = stream ? p0 / a.block * a.block : p0 + 1;
+  const int64_t kv0 = (static_cast<int64_t>(sq) * 2 * a.L * a.Hkv + kvh) * D;
+  const PairLoader<D> loader(a.k + kv0, a.v + kv0, a.Hkv * D, wave,
+                             lds_address(smem));
+  // the tile that is loaded next
+  int ahead = 0, ahead_p = 0;
+  auto fetch = [&](int u, int slot) {
+    loader.load(u, static_cast<int64_t>(ahead_p) * (a.Hkv * D),
+                a.L - 1 - (ahead >= n_mem ? ahead_p - a.L : ahead_p),
+                slot * kPair);
+  };
+  // past the end: the last tile again, into a slot that nobody reads
+  auto advance = [&]() {
+    ahead = min(ahead + 1, n - 1);
+    ahead_p = ahead >= n_mem ? a.L + (own0 + ahead - n_mem) * kRows
+                             : ahead * kRows;
+  };
+  if (n_mem == 0) ahead_p = a.L + own0 * kRows;
+  const Reader<D> rd;
+  constexpr int kE = 16 / NK;              // elements per step
+  bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
 #pragma unroll
-  for (int i = 0; i < kSlots - 1; ++i) fetch(i);
+  for (int i = 0; i < kSlots - 1; ++i) {
+#pragma unroll
+    for (int u = 0; u < PairLoader<D>::kCount; ++u) fetch(u, i);
+    advance();
+  }
+  // take delivery of the rows: no wait for them in the loop
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk)
+      asm volatile("" : "+v"(qf[b][kk]), "+v"(dof[b][kk]));
+  wait_vmcnt<(kSlots - 2) * PairLoader<D>::kCount>();
+  __syncthreads();
+#pragma unroll
+  for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem, kk);
+  int slot = 0, next_slot = 1, load_slot = kSlots - 1;
   for (int i = 0; i < n; ++i) {
-    // this wave's loads of tile i, then everybody's; the barrier also frees
-    // the slot of tile i - 1
-    wait_vmcnt<(kSlots - 2) * PairLoader<D>::kCount>();
+    // this wave's loads of tile i + 1, then everybody's; the barrier also
+    // frees the slot of tile i - 1
+    wait_vmcnt<(kSlots - 3) * PairLoader<D>::kCount>();
     __syncthreads();
-    fetch(i + kSlots - 1);
-    const char* kt = smem + (i % kSlots) * kPair;
+    const char* kt = smem + slot * kPair;
+    const char* vt = kt + T::bytes;
+    // A tile that this wave's rows do not see is computed all the same, P = 0:
+    // the waves are in step, and a branch around the accumulators costs copies
     const bool own = i >= n_mem;
     const int j0 = (own ? own0 + i - n_mem : i) * kRows;
-    // (a tile that this wave's rows do not see is computed all the same, P = 0:
-    // the waves are in step, and a branch around the accumulators costs copies)
-    tile(kt, j0, own, own || j0 + kRows > full);
+    const bool mask = own || j0 + kRows > full;
+    floatx16_t s[2], dp[2];
+    float p[2][16];
+    bf16x8_t ds[2][2];
+    auto hide = [&](int b) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int j = j0 + 16 * (e >> 3) + 8 * hf + (e & 7);
+        const int from = own ? lo[b] : 0, to = own || !stream ? hi[b] : lo[b];
+        s[b][e] = j >= from && j < to ? s[b][e] : kNegInf;
+      }
+    };
+    auto weigh = [&](int b, int kk) {       // P
+#pragma unroll
+      for (int e = kk * kE; e < kk * kE + kE; ++e) {
+        p[b][e] = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[b][e], a.scale_log2, -lse2[b]));
+        here(p[b][e]);
+      }
+    };
+    auto grad = [&](int b, int kk) {        // dS
+#pragma unroll
+      for (int e = kk * kE; e < kk * kE + kE; ++e)
+        ds[b][e >> 3][e & 7] =
+            static_cast<__bf16>(p[b][e] * (dp[b][e] - delta[b]));
+    };
+    step();
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      s[0] = mfma(f[kk], qf[0][kk], kk ? s[0] : floatx16_t{});
+      if (kk < PairLoader<D>::kCount) fetch(kk, load_slot);
+      step();
+    }
+    if (mask) hide(0);
+    step();
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      s[1] = mfma(f[kk], qf[1][kk], kk ? s[1] : floatx16_t{});
+      f[kk] = rd.rows(vt, kk);
+      weigh(0, kk);
+      step();
+    }
+    if (mask) hide(1);
+    step();
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      dp[0] = mfma(f[kk], dof[0][kk], kk ? dp[0] : floatx16_t{});
+      weigh(1, kk);
+      step();
+    }
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      dp[1] = mfma(f[kk], dof[1][kk], kk ? dp[1] : floatx16_t{});
+      f[kk] = rd.cols(kt, kk / NM, kk % NM);
+      grad(0, kk);
+      step();
+    }
+    settle(ds[0]);
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {          // NK = 2 NM
+      mfma_acc(acc[0][x % NM], f[x], ds[0][x / NM]);
+      grad(1, x);
+      step();
+    }
+    settle(ds[1]);
+    const char* nt = smem + next_slot * kPair;
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      mfma_acc(acc[1][x % NM], f[x], ds[1][x / NM]);
+      f[x] = rd.rows(nt, x);
+      step();
+    }
+    advance();
+    load_slot = slot;
+    slot = next_slot;
+    next_slot = next_slot == kSlots - 1 ? 0 : next_slot + 1;
   }
   wait_vmcnt<0>();      // surplus loads land before the LDS is given up
   drain(acc);
@@ -394,10 +461,8 @@ void dkv_kernel(BwdArgs a) {
   constexpr int NK = D / 16, NM = D / 32;
   using T = RowTile<D>;
   constexpr int kPair = 2 * T::bytes;
-  constexpr int kSlot = kPair + 2 * kRows * 4;     // rows' lse and D behind
+  constexpr int kSlot = kPair + 2 * kRows * 4;     // rows' -lse, -D behind
   __shared__ __attribute__((aligned(1024))) char smem[kSlots * kSlot];
-  // V of the workgroup's keys, in tiles of 32
-  __shared__ __attribute__((aligned(1024))) char vsm[kKeysPerWg / kRows * T::bytes];
   const int tiles = (a.L + kKeysPerWg - 1) / kKeysPerWg;
   const int n_mem = a.n_seq * a.Hkv * tiles * a.nsplit;
   int wg = blockIdx.x;
@@ -414,26 +479,22 @@ void dkv_kernel(BwdArgs a) {
   const int lane = lane_id(), col = lane & 31, hf = lane >> 5;
   const int kw0 = j0 + wave * kOwn;
 
-  bf16x8_t kf[2][NK];
-  // rows that see this lane's keys: memory rows key .. L-1 and prediction
-  // rows next .. L-1, or for a prediction key rows key .. next-1 (next: the
-  // block after the key's)
-  int key[2], next[2];
+  bf16x8_t kf[2][NK], vf[2][NK];
+  // a lane's keys are kw0 + 32 b + col; those of the memory are seen by memory
+  // rows key .. L-1 and prediction rows next .. L-1 (next: the block after the
+  // key's), those of the prediction by prediction rows key .. next-1
+  int next[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    key[b] = kw0 + 32 * b + col;
-    const int jc = min(key[b], a.L - 1);
+    const int jc = min(kw0 + 32 * b + col, a.L - 1);
     next[b] = min(a.L, (jc / a.block + 1) * a.block);
     const int64_t o =
         (((static_cast<int64_t>(sq) * 2 + stream) * a.L + jc) * a.Hkv + kvh) * D;
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       kf[b][kk] = load8(a.k + o + kk * 16 + hf * 8);
-      *reinterpret_cast<u16x8_t*>(vsm + (2 * wave + b) * T::bytes +
-                                  T::off(col, 2 * kk + hf)) =
-          *reinterpret_cast<const u16x8_t*>(a.v + o + kk * 16 + hf * 8);
+      vf[b][kk] = load8(a.v + o + kk * 16 + hf * 8);
     }
-    if (key[b] >= a.L) key[b] = next[b] = 0x40000000;   // seen by no row
   }
   floatx16_t dk[2][NM], dv[2][NM];
 #pragma unroll
@@ -441,77 +502,6 @@ void dkv_kernel(BwdArgs a) {
 #pragma unroll
     for (int m = 0; m < NM; ++m) dk[b][m] = dv[b][m] = floatx16_t{};
 
-  const Reader<D> rd;
-  // the wave's V as the second operand: lane's key, rows in plain order
-  int vrow[4];
-#pragma unroll
-  for (int x = 0; x < 4; ++x)
-    vrow[x] = T::off(col, (D == 128 ? 4 : 2) * x + hf) + 2 * wave * T::bytes;
-  auto vfrag = [&](int b, int kk) {
-    return load8(reinterpret_cast<const uint16_t*>(
-        vsm + b * T::bytes +
-        (D == 128 ? vrow[kk >> 1] + (kk & 1) * 32 : vrow[kk])));
-  };
-  // one tile of rows p0 .. p0+31
-  auto tile = [&](const char* qt, int p0, bool pred, bool mask) {
-    const char* dot = qt + T::bytes;
-    const float* ldt = reinterpret_cast<const float*>(qt + kPair) + 8 * hf;
-    floatx16_t s[2] = {}, dp[2] = {};
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      const bf16x8_t f = rd.rows(qt, kk);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) s[b] = mfma(f, kf[b][kk], s[b]);
-    }
-    if (mask) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int p = p0 + 16 * (e >> 3) + 8 * hf + (e & 7);
-          const int from = pred ? next[b] : key[b];
-          const int to = stream ? next[b] : a.L;
-          s[b][e] = p >= from && p < to ? s[b][e] : kNegInf;
-        }
-    }
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      const bf16x8_t f = rd.rows(dot, kk);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) dp[b] = mfma(f, vfrag(b, kk), dp[b]);
-    }
-    bf16x8_t pb[2][2], ds[2][2];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float l2 = ldt[16 * (e >> 3) + (e & 7)];
-      const float d = ldt[kRows + 16 * (e >> 3) + (e & 7)];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const float p =
-            __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], a.scale_log2, -l2));
-        pb[b][e >> 3][e & 7] = static_cast<__bf16>(p);
-        ds[b][e >> 3][e & 7] = static_cast<__bf16>(p * (dp[b][e] - d));
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int m = 0; m < NM; ++m) {
-        const bf16x8_t f = rd.cols(dot, h, m);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) mfma_acc(dv[b][m], f, pb[b][h]);
-      }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int m = 0; m < NM; ++m) {
-        const bf16x8_t f = rd.cols(qt, h, m);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) mfma_acc(dk[b][m], f, ds[b][h]);
-      }
-  };
   // items: row tiles t from the last down, in each the streams that see the
   // keys (memory, prediction) and their heads.  Every workgroup of a kv head
   // starts at the same rows, which they then find in the L2
@@ -544,57 +534,202 @@ void dkv_kernel(BwdArgs a) {
     }
     return x;
   };
-  const PairLoader<D> loader(wave);
   const uint32_t lds0 = lds_address(smem);
-  const int stride = a.Hq * D * 2;
+  const int64_t q0 = (static_cast<int64_t>(sq) * 2 * a.L * a.Hq + kvh * a.G) * D;
+  const PairLoader<D> loader(a.q + q0, a.dout + q0, a.Hq * D, wave, lds0);
+  constexpr int kLoads = PairLoader<D>::kCount + 1;
+  const float* ld0 = a.ld + (static_cast<int64_t>(sq) * a.Hq + kvh * a.G) * 2 *
+                                a.T * 2 * kRows;
+  // the item that is loaded next
   Item ahead = item_at(it0);
-  int n_ahead = it0;
-  auto fetch = [&](int slot) {
-    const int rs = stream || ahead.sg >= a.G ? 1 : 0;
-    const int head = kvh * a.G + (ahead.sg >= a.G ? ahead.sg - a.G : ahead.sg);
-    const int p0 = ahead.t * kRows;
-    const int64_t o =
-        (((static_cast<int64_t>(sq) * 2 + rs) * a.L + p0) * a.Hq + head) * D;
-    const uint32_t dst = lds0 + slot * kSlot;
-    loader.load(a.q + o, a.dout + o, stride, a.L - 1 - p0, dst);
-    // every wave the same 256 bytes, so that all wait for as many loads
-    const float* l = a.ld + (((static_cast<int64_t>(sq) * a.Hq + head) * 2 + rs) *
-                                 a.T + ahead.t) * 2 * kRows;
-    load_to_lds4(buffer_rsrc(l, 2 * kRows * 4), lane * 4,
-                 __builtin_amdgcn_readfirstlane(dst + kPair));
-    // past the end: the last item again, into a slot that nobody reads
-    if (++n_ahead < it1) ahead = next_item(ahead);
+  int n_ahead = it0, ahead_rs = 0, ahead_head = 0;
+  auto place = [&]() {
+    const bool up = ahead.sg >= a.G;
+    ahead_rs = stream || up ? 1 : 0;
+    ahead_head = up ? ahead.sg - a.G : ahead.sg;
   };
+  auto fetch = [&](int u, int slot) {
+    if (u < PairLoader<D>::kCount) {
+      loader.load(u,
+                  static_cast<int64_t>(ahead_rs * a.L + ahead.t * kRows) *
+                          (a.Hq * D) + ahead_head * D,
+                  a.L - 1 - ahead.t * kRows, slot * kSlot);
+    } else {
+      // every wave the same 256 bytes, so that all wait for as many loads
+      const float* l =
+          ld0 + static_cast<int64_t>((ahead_head * 2 + ahead_rs) * a.T + ahead.t) *
+                    (2 * kRows);
+      load_to_lds4(buffer_rsrc(l, 2 * kRows * 4), lane_here() * 4,
+                   lds0 + slot * kSlot + kPair);
+    }
+  };
+  // past the end: the last item again, into a slot that nobody reads
+  auto advance = [&]() {
+    if (++n_ahead < it1) ahead = next_item(ahead);
+    place();
+  };
+  const Reader<D> rd;
+  constexpr int kE = 16 / NK;              // elements per step
+  bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
   const int kwl = min(kw0 + kOwn, a.L) - 1;         // the wave's last key
   const int next_hi = (kwl / a.block + 1) * a.block;
+  Item cur = item_at(it0);
+  place();
   if (it0 < it1) {
 #pragma unroll
-    for (int i = 0; i < kSlots - 1; ++i) fetch(i);
+    for (int i = 0; i < kSlots - 1; ++i) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) fetch(u, i);
+      advance();
+    }
   }
-  Item cur = item_at(it0);
-  for (int it = it0, i = 0; it < it1; ++it, ++i) {
-    wait_vmcnt<(kSlots - 2) * (PairLoader<D>::kCount + 1)>();
+  // take delivery of the keys: no wait for them in the loop
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk)
+      asm volatile("" : "+v"(kf[b][kk]), "+v"(vf[b][kk]));
+  wait_vmcnt<(kSlots - 2) * kLoads>();
+  __syncthreads();
+#pragma unroll
+  for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem, kk);
+  int slot = 0, next_slot = 1, load_slot = kSlots - 1;
+  for (int it = it0; it < it1; ++it) {
+    // this wave's loads of the next item, then everybody's; the barrier also
+    // frees the slot of the previous one
+    wait_vmcnt<(kSlots - 3) * kLoads>();
     __syncthreads();
-    fetch((i + kSlots - 1) % kSlots);
-    const char* qt = smem + i % kSlots * kSlot;
+    const char* qt = smem + slot * kSlot;
+    const char* ot = qt + T::bytes;
+    const floatx4_t* ldt =
+        reinterpret_cast<const floatx4_t*>(qt + kPair) + 2 * hf;
     const int p0 = cur.t * kRows;
-    // a mask unless every row sees all keys of the wave
+    // a mask unless every row sees all keys of the wave.  (A tile of which it
+    // sees none is computed all the same, P = 0, as in dq_kernel)
     const bool pred = cur.sg >= a.G;        // prediction rows, memory keys
-    tile(qt, p0, pred,
-         stream || p0 < (pred ? next_hi : kwl) || p0 + kRows > a.L ||
-             kw0 + kOwn > a.L);
+    const bool mask = stream || p0 < (pred ? next_hi : kwl) ||
+                      p0 + kRows > a.L || kw0 + kOwn > a.L;
+    floatx16_t s[2], dp[2];
+    floatx4_t nl[4];
+    float p[2][16];
+    bf16x8_t pb[2][2], ds[2][2];
+    auto hide = [&](int b) {
+      const int l = lane_here();
+      const int k0 = kw0 + 32 * b + (l & 31), i0 = p0 + 8 * (l >> 5);
+      const int from = pred ? next[b] : k0;
+      const int to = k0 < a.L ? stream ? next[b] : a.L : 0;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int i = i0 + 16 * (e >> 3) + (e & 7);
+        s[b][e] = i >= from && i < to ? s[b][e] : kNegInf;
+      }
+    };
+    // -lse (x < 4) and -D (x >= 4) of rows 16 (x / 2 % 2) + 8 hf + 4 (x % 2) ..
+    auto row_values = [&](int x) {
+      return ldt[8 * (x >> 2) + 4 * (x >> 1 & 1) + (x & 1)];
+    };
+    auto weigh = [&](int b, int kk) {       // P
+#pragma unroll
+      for (int e = kk * kE; e < kk * kE + kE; ++e) {
+        p[b][e] = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[b][e], a.scale_log2, nl[e >> 2][e & 3]));
+        here(p[b][e]);
+        pb[b][e >> 3][e & 7] = static_cast<__bf16>(p[b][e]);
+      }
+    };
+    // dP starts from -D, read straight into its accumulator
+    auto minus_d = [&](int b, int x) {
+      const floatx4_t v = row_values(4 + x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[b][4 * x + e] = v[e];
+    };
+    auto grad = [&](int b, int kk) {        // dS
+#pragma unroll
+      for (int e = kk * kE; e < kk * kE + kE; ++e)
+        ds[b][e >> 3][e & 7] = static_cast<__bf16>(p[b][e] * dp[b][e]);
+    };
+    // Eight phases of NK = 2 NM MFMAs: S, dV, dP, dK for either group of keys.
+    // dV comes before dP so that P's operands are gone when dP needs registers
+    step();
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      s[0] = mfma(f[kk], kf[0][kk], kk ? s[0] : floatx16_t{});
+      if (kk >= NK - 4) nl[kk - (NK - 4)] = row_values(kk - (NK - 4));
+      if (kk < kLoads) fetch(kk, load_slot);
+      step();
+    }
+    if (mask) hide(0);
+    step();
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      s[1] = mfma(f[kk], kf[1][kk], kk ? s[1] : floatx16_t{});
+      f[kk] = rd.cols(ot, kk / NM, kk % NM);
+      weigh(0, kk);
+      step();
+    }
+    if (mask) hide(1);
+    settle(pb[0]);
+    step();
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      mfma_acc(dv[0][x % NM], f[x], pb[0][x / NM]);
+      weigh(1, x);
+      step();
+    }
+    settle(pb[1]);
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      mfma_acc(dv[1][x % NM], f[x], pb[1][x / NM]);
+      f[x] = rd.rows(ot, x);
+      if (x >= NK - 4) minus_d(0, x - (NK - 4));
+      step();
+    }
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      dp[0] = mfma(f[kk], vf[0][kk], dp[0]);
+      if (kk >= NK - 4) minus_d(1, kk - (NK - 4));
+      step();
+    }
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      dp[1] = mfma(f[kk], vf[1][kk], dp[1]);
+      f[kk] = rd.cols(qt, kk / NM, kk % NM);
+      grad(0, kk);
+      step();
+    }
+    settle(ds[0]);
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      mfma_acc(dk[0][x % NM], f[x], ds[0][x / NM]);
+      grad(1, x);
+      step();
+    }
+    settle(ds[1]);
+    const char* nt = smem + next_slot * kSlot;
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      mfma_acc(dk[1][x % NM], f[x], ds[1][x / NM]);
+      f[x] = rd.rows(nt, x);
+      step();
+    }
     cur = next_item(cur);
+    advance();
+    load_slot = slot;
+    slot = next_slot;
+    next_slot = next_slot == kSlots - 1 ? 0 : next_slot + 1;
   }
   wait_vmcnt<0>();      // surplus loads land before the LDS is given up
   drain(dv);
   drain(dk);
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    if (key[b] >= a.L) continue;
+    const int l = lane_here(), hf = l >> 5;
+    const int key = kw0 + 32 * b + (l & 31);
+    if (key >= a.L) continue;
     const int64_t kv = static_cast<int64_t>(a.Hkv) * D;
     if (nsplit == 1) {
       const int64_t o =
-          ((static_cast<int64_t>(sq) * 2 + stream) * a.L + key[b]) * kv + kvh * D;
+          ((static_cast<int64_t>(sq) * 2 + stream) * a.L + key) * kv + kvh * D;
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
@@ -611,7 +746,7 @@ void dkv_kernel(BwdArgs a) {
     } else {
       const int64_t n = a.n_seq * static_cast<int64_t>(a.L) * kv;
       float* o = a.part + split * n +
-                 (static_cast<int64_t>(sq) * a.L + key[b]) * kv + kvh * D;
+                 (static_cast<int64_t>(sq) * a.L + key) * kv + kvh * D;
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
