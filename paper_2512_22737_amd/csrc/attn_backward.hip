@@ -199,13 +199,20 @@ __device__ __forceinline__ void mfma_acc(floatx16_t& acc, bf16x8_t a,
                : "v"(a), "v"(b));
 }
 
-// Two wait states between VALU writes of operands and an MFMA's read.
-__device__ __forceinline__ void settle(bf16x8_t (&x)[2]) {
-  asm volatile("s_nop 1" : "+v"(x[0]), "+v"(x[1]));
+// Two wait states between the VALU's writes of an operand and an MFMA's read;
+// the operand is complete here.
+__device__ __forceinline__ void settle(bf16x8_t& x) {
+  asm volatile("s_nop 1" : "+v"(x));
 }
 
 // The value is computed here, not sunk past the next branch.
 __device__ __forceinline__ void here(float& x) { asm volatile("" : "+v"(x)); }
+
+// All waves are here.  Without the wait for this wave's own LDS reads that
+// __syncthreads() has: those under way are of the next tile, which stays.
+__device__ __forceinline__ void meet() {
+  asm volatile("s_barrier" ::: "memory");
+}
 
 // Lane index, computed where it stands (no register from outside the loop).
 __device__ __forceinline__ int lane_here() {
@@ -325,11 +332,12 @@ void dq_kernel(BwdArgs a) {
   if (n_mem == 0) ahead_p = a.L + own0 * kRows;
   const Reader<D> rd;
   constexpr int kE = 16 / NK;              // elements per step
+  constexpr int kLoads = PairLoader<D>::kCount;
   bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
 #pragma unroll
   for (int i = 0; i < kSlots - 1; ++i) {
 #pragma unroll
-    for (int u = 0; u < PairLoader<D>::kCount; ++u) fetch(u, i);
+    for (int u = 0; u < kLoads; ++u) fetch(u, i);
     advance();
   }
   // take delivery of the rows: no wait for them in the loop
@@ -338,7 +346,7 @@ void dq_kernel(BwdArgs a) {
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
       asm volatile("" : "+v"(qf[b][kk]), "+v"(dof[b][kk]));
-  wait_vmcnt<(kSlots - 2) * PairLoader<D>::kCount>();
+  wait_vmcnt<(kSlots - 2) * kLoads>();
   __syncthreads();
 #pragma unroll
   for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem, kk);
@@ -346,8 +354,8 @@ void dq_kernel(BwdArgs a) {
   for (int i = 0; i < n; ++i) {
     // this wave's loads of tile i + 1, then everybody's; the barrier also
     // frees the slot of tile i - 1
-    wait_vmcnt<(kSlots - 3) * PairLoader<D>::kCount>();
-    __syncthreads();
+    wait_vmcnt<(kSlots - 3) * kLoads>();
+    meet();
     const char* kt = smem + slot * kPair;
     const char* vt = kt + T::bytes;
     // A tile that this wave's rows do not see is computed all the same, P = 0:
@@ -380,11 +388,13 @@ void dq_kernel(BwdArgs a) {
         ds[b][e >> 3][e & 7] =
             static_cast<__bf16>(p[b][e] * (dp[b][e] - delta[b]));
     };
+    // Six phases of NK = 2 NM MFMAs: S, dP, dq for either group of rows.  The
+    // vector work on a product starts a step after its last MFMA
     step();
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       s[0] = mfma(f[kk], qf[0][kk], kk ? s[0] : floatx16_t{});
-      if (kk < PairLoader<D>::kCount) fetch(kk, load_slot);
+      if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
       step();
     }
     if (mask) hide(0);
@@ -393,7 +403,7 @@ void dq_kernel(BwdArgs a) {
     for (int kk = 0; kk < NK; ++kk) {
       s[1] = mfma(f[kk], qf[1][kk], kk ? s[1] : floatx16_t{});
       f[kk] = rd.rows(vt, kk);
-      weigh(0, kk);
+      if (kk >= 1) weigh(0, kk - 1);
       step();
     }
     if (mask) hide(1);
@@ -401,29 +411,33 @@ void dq_kernel(BwdArgs a) {
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       dp[0] = mfma(f[kk], dof[0][kk], kk ? dp[0] : floatx16_t{});
-      weigh(1, kk);
+      weigh(kk ? 1 : 0, kk ? kk - 1 : NK - 1);
       step();
     }
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       dp[1] = mfma(f[kk], dof[1][kk], kk ? dp[1] : floatx16_t{});
       f[kk] = rd.cols(kt, kk / NM, kk % NM);
-      grad(0, kk);
+      if (kk)
+        grad(0, kk - 1);
+      else
+        weigh(1, NK - 1);
       step();
     }
-    settle(ds[0]);
 #pragma unroll
-    for (int x = 0; x < NK; ++x) {          // NK = 2 NM
+    for (int x = 0; x < NK; ++x) {
+      if (x % NM == 0) settle(ds[0][x / NM]);
       mfma_acc(acc[0][x % NM], f[x], ds[0][x / NM]);
-      grad(1, x);
+      grad(x ? 1 : 0, x ? x - 1 : NK - 1);
       step();
     }
-    settle(ds[1]);
     const char* nt = smem + next_slot * kPair;
 #pragma unroll
     for (int x = 0; x < NK; ++x) {
+      if (x % NM == 0) settle(ds[1][x / NM]);
       mfma_acc(acc[1][x % NM], f[x], ds[1][x / NM]);
       f[x] = rd.rows(nt, x);
+      if (x == 0) grad(1, NK - 1);
       step();
     }
     advance();
@@ -518,21 +532,34 @@ void dkv_kernel(BwdArgs a) {
   const int it0 = static_cast<int>(static_cast<int64_t>(n_items) * split / nsplit);
   const int it1 =
       static_cast<int>(static_cast<int64_t>(n_items) * (split + 1) / nsplit);
-  // an item: its row tile and (stream, head of the group)
+  // an item: its row tile, its rows' stream and its head of the group.  Steps
+  // are branches, so that everything stays in scalar registers
   struct Item {
-    int t, sg;
+    int t, rs, g;
   };
   auto item_at = [&](int it) {
-    return it < n1 ? Item{t_hi - 1 - it / (2 * a.G), it % (2 * a.G)}
-                   : Item{t_mid - 1 - (it - n1) / a.G, (it - n1) % a.G};
+    Item x;
+    if (it < n1) {
+      x.t = t_hi - 1 - it / (2 * a.G);
+      x.g = it % (2 * a.G);
+      x.rs = x.g / a.G;
+    } else {
+      x.t = t_mid - 1 - (it - n1) / a.G;
+      x.g = it - n1;
+      x.rs = stream;
+    }
+    x.g %= a.G;
+    return x;
   };
-  auto next_item = [&](Item x) {
-    ++x.sg;
-    if (x.sg == (x.t >= t_mid ? 2 * a.G : a.G)) {
-      x.sg = 0;
+  auto next_item = [&](Item& x) {
+    if (++x.g < a.G) return;
+    x.g = 0;
+    if (x.rs == 0 && x.t >= t_mid) {
+      x.rs = 1;
+    } else {
+      x.rs = stream;
       --x.t;
     }
-    return x;
   };
   const uint32_t lds0 = lds_address(smem);
   const int64_t q0 = (static_cast<int64_t>(sq) * 2 * a.L * a.Hq + kvh * a.G) * D;
@@ -542,22 +569,17 @@ void dkv_kernel(BwdArgs a) {
                                 a.T * 2 * kRows;
   // the item that is loaded next
   Item ahead = item_at(it0);
-  int n_ahead = it0, ahead_rs = 0, ahead_head = 0;
-  auto place = [&]() {
-    const bool up = ahead.sg >= a.G;
-    ahead_rs = stream || up ? 1 : 0;
-    ahead_head = up ? ahead.sg - a.G : ahead.sg;
-  };
+  int n_ahead = it0;
   auto fetch = [&](int u, int slot) {
     if (u < PairLoader<D>::kCount) {
       loader.load(u,
-                  static_cast<int64_t>(ahead_rs * a.L + ahead.t * kRows) *
-                          (a.Hq * D) + ahead_head * D,
+                  static_cast<int64_t>(ahead.rs * a.L + ahead.t * kRows) *
+                          (a.Hq * D) + ahead.g * D,
                   a.L - 1 - ahead.t * kRows, slot * kSlot);
     } else {
       // every wave the same 256 bytes, so that all wait for as many loads
       const float* l =
-          ld0 + static_cast<int64_t>((ahead_head * 2 + ahead_rs) * a.T + ahead.t) *
+          ld0 + static_cast<int64_t>((ahead.g * 2 + ahead.rs) * a.T + ahead.t) *
                     (2 * kRows);
       load_to_lds4(buffer_rsrc(l, 2 * kRows * 4), lane_here() * 4,
                    lds0 + slot * kSlot + kPair);
@@ -565,8 +587,7 @@ void dkv_kernel(BwdArgs a) {
   };
   // past the end: the last item again, into a slot that nobody reads
   auto advance = [&]() {
-    if (++n_ahead < it1) ahead = next_item(ahead);
-    place();
+    if (++n_ahead < it1) next_item(ahead);
   };
   const Reader<D> rd;
   constexpr int kE = 16 / NK;              // elements per step
@@ -574,7 +595,6 @@ void dkv_kernel(BwdArgs a) {
   const int kwl = min(kw0 + kOwn, a.L) - 1;         // the wave's last key
   const int next_hi = (kwl / a.block + 1) * a.block;
   Item cur = item_at(it0);
-  place();
   if (it0 < it1) {
 #pragma unroll
     for (int i = 0; i < kSlots - 1; ++i) {
@@ -598,7 +618,7 @@ void dkv_kernel(BwdArgs a) {
     // this wave's loads of the next item, then everybody's; the barrier also
     // frees the slot of the previous one
     wait_vmcnt<(kSlots - 3) * kLoads>();
-    __syncthreads();
+    meet();
     const char* qt = smem + slot * kSlot;
     const char* ot = qt + T::bytes;
     const floatx4_t* ldt =
@@ -606,7 +626,7 @@ void dkv_kernel(BwdArgs a) {
     const int p0 = cur.t * kRows;
     // a mask unless every row sees all keys of the wave.  (A tile of which it
     // sees none is computed all the same, P = 0, as in dq_kernel)
-    const bool pred = cur.sg >= a.G;        // prediction rows, memory keys
+    const bool pred = cur.rs > stream;      // prediction rows, memory keys
     const bool mask = stream || p0 < (pred ? next_hi : kwl) ||
                       p0 + kRows > a.L || kw0 + kOwn > a.L;
     floatx16_t s[2], dp[2];
@@ -648,14 +668,15 @@ void dkv_kernel(BwdArgs a) {
       for (int e = kk * kE; e < kk * kE + kE; ++e)
         ds[b][e >> 3][e & 7] = static_cast<__bf16>(p[b][e] * dp[b][e]);
     };
-    // Eight phases of NK = 2 NM MFMAs: S, dV, dP, dK for either group of keys.
-    // dV comes before dP so that P's operands are gone when dP needs registers
+    // Eight phases of NK = 2 NM MFMAs: S, dV, dP, dK for either group of keys
+    // (dV before dP, so that P's operands are gone when dP needs registers).
+    // The vector work on a product starts a step after its last MFMA
     step();
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       s[0] = mfma(f[kk], kf[0][kk], kk ? s[0] : floatx16_t{});
-      if (kk >= NK - 4) nl[kk - (NK - 4)] = row_values(kk - (NK - 4));
-      if (kk < kLoads) fetch(kk, load_slot);
+      if (kk < 4) nl[kk] = row_values(kk);
+      if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
       step();
     }
     if (mask) hide(0);
@@ -664,55 +685,57 @@ void dkv_kernel(BwdArgs a) {
     for (int kk = 0; kk < NK; ++kk) {
       s[1] = mfma(f[kk], kf[1][kk], kk ? s[1] : floatx16_t{});
       f[kk] = rd.cols(ot, kk / NM, kk % NM);
-      weigh(0, kk);
+      if (kk) weigh(0, kk - 1);
       step();
     }
     if (mask) hide(1);
-    settle(pb[0]);
     step();
 #pragma unroll
     for (int x = 0; x < NK; ++x) {
+      if (x % NM == 0) settle(pb[0][x / NM]);
       mfma_acc(dv[0][x % NM], f[x], pb[0][x / NM]);
-      weigh(1, x);
+      weigh(x ? 1 : 0, x ? x - 1 : NK - 1);
       step();
     }
-    settle(pb[1]);
 #pragma unroll
     for (int x = 0; x < NK; ++x) {
+      if (x % NM == 0) settle(pb[1][x / NM]);
       mfma_acc(dv[1][x % NM], f[x], pb[1][x / NM]);
       f[x] = rd.rows(ot, x);
-      if (x >= NK - 4) minus_d(0, x - (NK - 4));
+      if (x == 0) weigh(1, NK - 1);
+      if (x < 4) minus_d(0, x);
       step();
     }
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       dp[0] = mfma(f[kk], vf[0][kk], dp[0]);
-      if (kk >= NK - 4) minus_d(1, kk - (NK - 4));
+      if (kk < 4) minus_d(1, kk);
       step();
     }
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       dp[1] = mfma(f[kk], vf[1][kk], dp[1]);
       f[kk] = rd.cols(qt, kk / NM, kk % NM);
-      grad(0, kk);
+      if (kk) grad(0, kk - 1);
       step();
     }
-    settle(ds[0]);
 #pragma unroll
     for (int x = 0; x < NK; ++x) {
+      if (x % NM == 0) settle(ds[0][x / NM]);
       mfma_acc(dk[0][x % NM], f[x], ds[0][x / NM]);
-      grad(1, x);
+      grad(x ? 1 : 0, x ? x - 1 : NK - 1);
       step();
     }
-    settle(ds[1]);
     const char* nt = smem + next_slot * kSlot;
 #pragma unroll
     for (int x = 0; x < NK; ++x) {
+      if (x % NM == 0) settle(ds[1][x / NM]);
       mfma_acc(dk[1][x % NM], f[x], ds[1][x / NM]);
       f[x] = rd.rows(nt, x);
+      if (x == 0) grad(1, NK - 1);
       step();
     }
-    cur = next_item(cur);
+    next_item(cur);
     advance();
     load_slot = slot;
     slot = next_slot;
