@@ -1,19 +1,28 @@
 // The masked-token loss of the training objective with the gradient of its
-// logits.  Row r with target t and weight w (logits l, Z = sum_v e^{l_v - m},
-// m the largest logit):
+// logits.  Row r with target t and weight w (logits l, m the largest,
+// Z = sum_v e^{l_v - m}):
 //   loss = w (ln Z - (l_t - m))      dl_v = w (e^{l_v - m} / Z - [v = t])
-// One workgroup per row: a pass with a running maximum and sum per thread,
-// then one that forms the gradient from logits that are still in a cache.
+// One workgroup per row.  Every thread keeps the first H 16-byte chunks that
+// it reads in registers: their maximum, then e^{l - m} in their place with
+// the sum, then the gradient, so that these logits are read once and their
+// exponentials taken once.  What does not fit (fp32 rows beyond 81920) is
+// reduced with a running maximum and read again for the gradient, while it is
+// in the L2.  Few long rows are split over workgroups: one kernel for the
+// slices' maxima and sums, one that joins them and forms the gradient.
 // Bound by HBM: logits read once, gradients written once.
 #include "common.h"
 #include "wedlm_train.h"
+
+#include <algorithm>
 
 using namespace wedlm;
 
 namespace {
 
-constexpr int kThreads = 512;
 constexpr float kLog2e = 1.4426950408889634f;
+// Workgroups of few long rows: threads, chunks a thread holds
+constexpr int kSmallThreads = 256, kSmallHeld = 16;
+constexpr int kSmallChunks = kSmallThreads * kSmallHeld;
 
 struct LossArgs {
   const void* logits;     // [R, stride] fp32 or bf16
@@ -21,8 +30,9 @@ struct LossArgs {
   const float* weight;    // [R] or null
   float* loss;            // [R]
   void* dlogits;          // [R, stride] or null
+  float2* part;           // [R, slices]: maximum, sum
   int64_t stride;
-  int R, V;
+  int R, V, slices, slice_len;
 };
 
 // Running maximum and sum of e^{x - m}.
@@ -40,66 +50,370 @@ __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b) {
   return {m, a.s * exp_below(a.m, m) + b.s * exp_below(b.m, m)};
 }
 
-__device__ __forceinline__ float load1(const float* p) { return *p; }
-__device__ __forceinline__ float load1(const uint16_t* p) {
-  return bf16_to_f32(*p);
-}
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store1(uint16_t* p, float v) {
-  *p = f32_to_bf16(v);
+// One element type: values of a 16-byte chunk and of a single element.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<float> {
+  static constexpr int n = 4;
+  typedef floatx4_t chunk;
+  __device__ static float get(const chunk& c, int e) { return c[e]; }
+  __device__ static void set(chunk& c, int e, float v) { c[e] = v; }
+  __device__ static float get(const float* p) { return *p; }
+  __device__ static void set(float* p, float v) { *p = v; }
+};
+template <>
+struct Elem<uint16_t> {
+  static constexpr int n = 8;
+  typedef u16x8_t chunk;
+  __device__ static float get(const chunk& c, int e) { return bf16_to_f32(c[e]); }
+  __device__ static void set(chunk& c, int e, float v) { c[e] = f32_to_bf16(v); }
+  __device__ static float get(const uint16_t* p) { return bf16_to_f32(*p); }
+  __device__ static void set(uint16_t* p, float v) { *p = f32_to_bf16(v); }
+};
+
+// A stretch of a row: elements up to the first 16-byte boundary, whole
+// chunks, and the rest; the single elements (fewer than 16) are numbered on.
+template <typename T>
+struct Span {
+  int head, chunks, singles;
+  __device__ __forceinline__ Span(const T* p, int n) {
+    constexpr int E = Elem<T>::n;
+    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(p) / sizeof(T)) &
+                    (E - 1);
+    head = min(off ? E - off : 0, n);
+    chunks = (n - head) / E;
+    singles = n - chunks * E;
+  }
+  __device__ __forceinline__ int single(int i) const {
+    return i < head ? i : i + chunks * Elem<T>::n;
+  }
+};
+
+// Reduction over the workgroup, the same value in every thread.
+template <int NT, typename Op>
+__device__ __forceinline__ float reduce(float v, float* lds, Op op) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = op(v, __shfl_xor(v, off));
+  if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
+  __syncthreads();
+  v = lds[0];
+#pragma unroll
+  for (int i = 1; i < NT / kWave; ++i) v = op(v, lds[i]);
+  return v;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void token_loss_kernel(LossArgs a) {
+__device__ __forceinline__ bool no_loss(const LossArgs& a, int r, int& t,
+                                        float& w) {
+  t = a.target[r];
+  w = a.weight ? a.weight[r] : 1.f;
+  return t < 0 || t >= a.V || w == 0.f;
+}
+
+__device__ __forceinline__ float row_loss(float w, float m, float s, float lt) {
+  return w * (m == kNegInf ? -kNegInf : logf(s) - (lt - m));
+}
+
+// Zeros over a stretch of a row of dlogits.
+template <typename T, int NT>
+__device__ __forceinline__ void clear(T* p, int n) {
+  const Span<T> sp(p, n);
+  typedef typename Elem<T>::chunk C;
+  C* body = reinterpret_cast<C*>(p + sp.head);
+  for (int c = threadIdx.x; c < sp.chunks; c += NT) body[c] = C{};
+  if (static_cast<int>(threadIdx.x) < sp.singles)
+    p[sp.single(threadIdx.x)] = static_cast<T>(0);
+}
+
+// Logits and gradients at the same offset from a 16-byte boundary: rows of
+// both have the same chunks.
+template <typename T, int NT, int H>
+__global__ __launch_bounds__(NT) void token_loss_kernel(LossArgs a) {
+  typedef Elem<T> E;
+  typedef typename E::chunk C;
   const int r = blockIdx.x;
   const T* row = static_cast<const T*>(a.logits) + r * a.stride;
   T* drow = a.dlogits ? static_cast<T*>(a.dlogits) + r * a.stride : nullptr;
-  const int t = a.target[r];
-  const float w = a.weight ? a.weight[r] : 1.f;
-  if (t < 0 || t >= a.V || w == 0.f) {
+  int t;
+  float w;
+  if (no_loss(a, r, t, w)) {
     if (threadIdx.x == 0) a.loss[r] = 0.f;
-    if (drow)
-      for (int v = threadIdx.x; v < a.V; v += kThreads) store1(drow + v, 0.f);
+    if (drow) clear<T, NT>(drow, a.V);
     return;
   }
-  MaxSum x{kNegInf, 0.f};
-  for (int v = threadIdx.x; v < a.V; v += kThreads) {
-    const float l = load1(row + v);
-    if (l == kNegInf) continue;
-    if (l > x.m) {
-      x.s = x.s * exp_below(x.m, l) + 1.f;
-      x.m = l;
-    } else {
-      x.s += exp_below(l, x.m);
+  __shared__ float lds[2][NT / kWave];
+  const Span<T> sp(row, a.V);
+  const C* body = reinterpret_cast<const C*>(row + sp.head);
+  const int tid = threadIdx.x;
+  // the target's logit is read before any gradient is written over it
+  const float lt = E::get(row + t);
+  C held[H];
+  float one = kNegInf, m = kNegInf;
+#pragma unroll
+  for (int i = 0; i < H; ++i)
+    if (tid + i * NT < sp.chunks) held[i] = body[tid + i * NT];
+  if (tid < sp.singles) m = one = E::get(row + sp.single(tid));
+#pragma unroll
+  for (int i = 0; i < H; ++i)
+    if (tid + i * NT < sp.chunks) {
+#pragma unroll
+      for (int e = 0; e < E::n; ++e) m = fmaxf(m, E::get(held[i], e));
+    }
+  MaxSum rest{kNegInf, 0.f};
+  for (int c = tid + H * NT; c < sp.chunks; c += NT) {
+    const C x = body[c];
+    float cm = E::get(x, 0);
+#pragma unroll
+    for (int e = 1; e < E::n; ++e) cm = fmaxf(cm, E::get(x, e));
+    if (cm > rest.m) {
+      rest.s *= exp_below(rest.m, cm);
+      rest.m = cm;
+    }
+    if (rest.m != kNegInf) {
+#pragma unroll
+      for (int e = 0; e < E::n; ++e) rest.s += exp_below(E::get(x, e), rest.m);
     }
   }
-  __shared__ MaxSum part[kThreads / kWave];
+  m = reduce<NT>(fmaxf(m, rest.m), lds[0],
+                 [](float x, float y) { return fmaxf(x, y); });
+  // a row of nothing but -inf: no probabilities, gradient 0
+  const float ref = m == kNegInf ? 0.f : m;
+  float s = rest.m == kNegInf ? 0.f : rest.s * exp_below(rest.m, ref);
+  if (tid < sp.singles) s += exp_below(one, ref);
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1)
-    x = merge(x, MaxSum{__shfl_xor(x.m, off), __shfl_xor(x.s, off)});
-  if (lane_id() == 0) part[threadIdx.x / kWave] = x;
-  // the target's logit is read before any gradient is written over it
-  const float lt = load1(row + t);
-  __syncthreads();
-  x = part[0];
+  for (int i = 0; i < H; ++i)
+    if (tid + i * NT < sp.chunks) {
+      float x = 0.f;
 #pragma unroll
-  for (int i = 1; i < kThreads / kWave; ++i) x = merge(x, part[i]);
-  if (threadIdx.x == 0)
-    a.loss[r] = w * (x.m == kNegInf ? -kNegInf : logf(x.s) - (lt - x.m));
+      for (int e = 0; e < E::n; ++e) x += exp_below(E::get(held[i], e), ref);
+      s += x;
+    }
+  s = reduce<NT>(s, lds[1], [](float x, float y) { return x + y; });
+  if (tid == 0) a.loss[r] = row_loss(w, m, s, lt);
   if (!drow) return;
-  const float k = x.m == kNegInf ? 0.f : w / x.s;
-  for (int v = threadIdx.x; v < a.V; v += kThreads) {
-    const float l = load1(row + v);
-    float d = l == kNegInf ? 0.f : exp_below(l, x.m) * k;
-    if (v == t && x.m != kNegInf) d -= w;
-    store1(drow + v, d);
+  const float k = m == kNegInf ? 0.f : w / s;
+  const float hit = m == kNegInf ? 0.f : w;
+  C* dbody = reinterpret_cast<C*>(drow + sp.head);
+  const int tb = t - sp.head;            // the target, from the first chunk
+  auto grad = [&](const C& x, int c) {
+    C d;
+#pragma unroll
+    for (int e = 0; e < E::n; ++e)
+      E::set(d, e, exp_below(E::get(x, e), ref) * k -
+                       (tb == c * E::n + e ? hit : 0.f));
+    dbody[c] = d;
+  };
+#pragma unroll
+  for (int i = 0; i < H; ++i)
+    if (tid + i * NT < sp.chunks) grad(held[i], tid + i * NT);
+  for (int c = tid + H * NT; c < sp.chunks; c += NT) grad(body[c], c);
+  if (tid < sp.singles) {
+    const int v = sp.single(tid);
+    E::set(drow + v, exp_below(one, ref) * k - (v == t ? hit : 0.f));
   }
+}
+
+// Maximum and sum of one slice.
+template <typename T>
+__global__ __launch_bounds__(kSmallThreads) void slice_kernel(LossArgs a) {
+  typedef Elem<T> E;
+  typedef typename E::chunk C;
+  const int r = blockIdx.y, sl = blockIdx.x;
+  int t;
+  float w;
+  if (no_loss(a, r, t, w)) return;
+  __shared__ float lds[2][kSmallThreads / kWave];
+  const int v0 = sl * a.slice_len;
+  const int n = min(a.slice_len, a.V - v0);
+  const T* p = static_cast<const T*>(a.logits) + r * a.stride + v0;
+  const Span<T> sp(p, n);
+  const C* body = reinterpret_cast<const C*>(p + sp.head);
+  const int tid = threadIdx.x;
+  C held[kSmallHeld];
+  float one = kNegInf, m = kNegInf, s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kSmallHeld; ++i)
+    if (tid + i * kSmallThreads < sp.chunks) held[i] = body[tid + i * kSmallThreads];
+  if (tid < sp.singles) m = one = E::get(p + sp.single(tid));
+#pragma unroll
+  for (int i = 0; i < kSmallHeld; ++i)
+    if (tid + i * kSmallThreads < sp.chunks) {
+#pragma unroll
+      for (int e = 0; e < E::n; ++e) m = fmaxf(m, E::get(held[i], e));
+    }
+  m = reduce<kSmallThreads>(m, lds[0],
+                            [](float x, float y) { return fmaxf(x, y); });
+  const float ref = m == kNegInf ? 0.f : m;
+  if (tid < sp.singles) s += exp_below(one, ref);
+#pragma unroll
+  for (int i = 0; i < kSmallHeld; ++i)
+    if (tid + i * kSmallThreads < sp.chunks) {
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < E::n; ++e) x += exp_below(E::get(held[i], e), ref);
+      s += x;
+    }
+  s = reduce<kSmallThreads>(s, lds[1], [](float x, float y) { return x + y; });
+  if (tid == 0)
+    a.part[static_cast<int64_t>(r) * a.slices + sl] = make_float2(m, s);
+}
+
+// Loss (first slice) and gradient of one slice, the slices joined in order.
+// The target's logit comes from the slice that holds it, which alone may
+// write over it: the loss is that slice's.
+template <typename T>
+__global__ __launch_bounds__(kSmallThreads) void slice_grad_kernel(LossArgs a) {
+  typedef Elem<T> E;
+  typedef typename E::chunk C;
+  const int r = blockIdx.y, sl = blockIdx.x;
+  const int v0 = sl * a.slice_len;
+  const int n = min(a.slice_len, a.V - v0);
+  const T* p = static_cast<const T*>(a.logits) + r * a.stride + v0;
+  T* dp = a.dlogits ? static_cast<T*>(a.dlogits) + r * a.stride + v0 : nullptr;
+  int t;
+  float w;
+  if (no_loss(a, r, t, w)) {
+    if (sl == 0 && threadIdx.x == 0) a.loss[r] = 0.f;
+    if (dp) clear<T, kSmallThreads>(dp, n);
+    return;
+  }
+  const int tid = threadIdx.x;
+  const bool mine = t >= v0 && t < v0 + n;
+  if (!dp && !mine) return;
+  const float lt = mine ? E::get(p + t - v0) : 0.f;
+  MaxSum x{kNegInf, 0.f};
+  for (int i = 0; i < a.slices; ++i) {
+    const float2 v = a.part[static_cast<int64_t>(r) * a.slices + i];
+    x = merge(x, MaxSum{v.x, v.y});
+  }
+  if (mine && tid == 0) a.loss[r] = row_loss(w, x.m, x.s, lt);
+  if (!dp) return;
+  // every thread has the target's logit before its gradient is written
+  __syncthreads();
+  const float ref = x.m == kNegInf ? 0.f : x.m;
+  const float k = x.m == kNegInf ? 0.f : w / x.s;
+  const float hit = x.m == kNegInf ? 0.f : w;
+  const Span<T> sp(p, n);
+  const C* body = reinterpret_cast<const C*>(p + sp.head);
+  C* dbody = reinterpret_cast<C*>(dp + sp.head);
+  const int tb = t - v0 - sp.head;
+#pragma unroll 4
+  for (int c = tid; c < sp.chunks; c += kSmallThreads) {
+    const C l = body[c];
+    C d;
+#pragma unroll
+    for (int e = 0; e < E::n; ++e)
+      E::set(d, e, exp_below(E::get(l, e), ref) * k -
+                       (tb == c * E::n + e ? hit : 0.f));
+    dbody[c] = d;
+  }
+  if (tid < sp.singles) {
+    const int v = sp.single(tid);
+    E::set(dp + v, exp_below(E::get(p + v), ref) * k -
+                       (v + v0 == t ? hit : 0.f));
+  }
+}
+
+// Logits and gradients at different offsets from 16-byte boundaries: element
+// by element, a running maximum and sum, then the gradient.
+template <typename T>
+__global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
+    LossArgs a) {
+  typedef Elem<T> E;
+  const int r = blockIdx.x;
+  const T* row = static_cast<const T*>(a.logits) + r * a.stride;
+  T* drow = static_cast<T*>(a.dlogits) + r * a.stride;
+  const int tid = threadIdx.x;
+  int t;
+  float w;
+  if (no_loss(a, r, t, w)) {
+    if (tid == 0) a.loss[r] = 0.f;
+    clear<T, kSmallThreads>(drow, a.V);
+    return;
+  }
+  __shared__ float lds[2][kSmallThreads / kWave];
+  const float lt = E::get(row + t);
+  MaxSum x{kNegInf, 0.f};
+  for (int v = tid; v < a.V; v += kSmallThreads) {
+    const float l = E::get(row + v);
+    if (l > x.m) {
+      x.s *= exp_below(x.m, l);
+      x.m = l;
+    }
+    if (x.m != kNegInf) x.s += exp_below(l, x.m);
+  }
+  const float m = reduce<kSmallThreads>(
+      x.m, lds[0], [](float y, float z) { return fmaxf(y, z); });
+  const float ref = m == kNegInf ? 0.f : m;
+  const float s = reduce<kSmallThreads>(
+      x.m == kNegInf ? 0.f : x.s * exp_below(x.m, ref), lds[1],
+      [](float y, float z) { return y + z; });
+  if (tid == 0) a.loss[r] = row_loss(w, m, s, lt);
+  const float k = m == kNegInf ? 0.f : w / s;
+  for (int v = tid; v < a.V; v += kSmallThreads)
+    E::set(drow + v, exp_below(E::get(row + v), ref) * k -
+                         (v == t && m != kNegInf ? w : 0.f));
+}
+
+// Elements of a row's slices, or V (one slice): rows beyond one small
+// workgroup's registers that are too few to give every CU one are cut so that
+// there are about 512 workgroups.
+int slice_len(int R, int V, int per_chunk) {
+  const int64_t chunks = V / per_chunk;
+  if (R >= 256 || chunks <= kSmallChunks) return V;
+  int64_t c = (chunks * R / 512 + kSmallThreads - 1) / kSmallThreads;
+  c = c < 1 ? 1 : c > kSmallHeld ? kSmallHeld : c;
+  return static_cast<int>(c) * kSmallThreads * per_chunk;
+}
+
+int row_slices(int R, int V, int per_chunk) {
+  const int len = slice_len(R, V, per_chunk);
+  return V / len + (V % len != 0);
+}
+
+template <typename T>
+int launch(const LossArgs& a0, hipStream_t st) {
+  LossArgs a = a0;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.logits);
+  const uintptr_t y = reinterpret_cast<uintptr_t>(a.dlogits);
+  if (y && (x ^ y) % 16 != 0) {
+    hipLaunchKernelGGL(token_loss_plain_kernel<T>, dim3(a.R),
+                       dim3(kSmallThreads), 0, st, a);
+    WEDLM_LAUNCH_CHECK();
+    return WEDLM_OK;
+  }
+  a.slices = row_slices(a.R, a.V, Elem<T>::n);
+  a.slice_len = slice_len(a.R, a.V, Elem<T>::n);
+  if (a.slices > 1) {
+    hipLaunchKernelGGL(slice_kernel<T>, dim3(a.slices, a.R),
+                       dim3(kSmallThreads), 0, st, a);
+    WEDLM_LAUNCH_CHECK();
+    hipLaunchKernelGGL(slice_grad_kernel<T>, dim3(a.slices, a.R),
+                       dim3(kSmallThreads), 0, st, a);
+    WEDLM_LAUNCH_CHECK();
+    return WEDLM_OK;
+  }
+  const int chunks = a.V / Elem<T>::n;
+  if (chunks <= kSmallThreads * 4)
+    hipLaunchKernelGGL((token_loss_kernel<T, kSmallThreads, 4>), dim3(a.R),
+                       dim3(kSmallThreads), 0, st, a);
+  else if (chunks <= kSmallChunks)
+    hipLaunchKernelGGL((token_loss_kernel<T, kSmallThreads, kSmallHeld>),
+                       dim3(a.R), dim3(kSmallThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((token_loss_kernel<T, 1024, 20>), dim3(a.R), dim3(1024),
+                       0, st, a);
+  WEDLM_LAUNCH_CHECK();
+  return WEDLM_OK;
 }
 
 }  // namespace
 
 extern "C" size_t wedlm_token_loss_workspace_size(int32_t R, int32_t V) {
-  return 0;
+  if (R < 1 || V < 1) return 0;
+  const int n = std::max(row_slices(R, V, Elem<float>::n),
+                         row_slices(R, V, Elem<uint16_t>::n));
+  return n > 1 ? static_cast<size_t>(R) * n * sizeof(float2) : 0;
 }
 
 extern "C" int wedlm_token_loss(const void* logits, int32_t logits_type,
@@ -113,12 +427,18 @@ extern "C" int wedlm_token_loss(const void* logits, int32_t logits_type,
   if (R < 1 || V < 1 || row_stride < V) return WEDLM_E_SHAPE;
   const size_t need = wedlm_token_loss_workspace_size(R, V);
   if (need && (!workspace || workspace_bytes < need)) return WEDLM_E_WORKSPACE;
-  LossArgs a{logits, target, weight, loss, dlogits, row_stride, R, V};
-  hipLaunchKernelGGL(logits_type == WEDLM_LOGITS_F32
-                         ? token_loss_kernel<float>
-                         : token_loss_kernel<uint16_t>,
-                     dim3(R), dim3(kThreads), 0,
-                     static_cast<hipStream_t>(stream), a);
-  WEDLM_LAUNCH_CHECK();
-  return WEDLM_OK;
+  LossArgs a{};
+  a.logits = logits;
+  a.target = target;
+  a.weight = weight;
+  a.loss = loss;
+  a.dlogits = dlogits;
+  a.part = static_cast<float2*>(workspace);
+  a.stride = row_stride;
+  a.R = R;
+  a.V = V;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return logits_type == WEDLM_LOGITS_F32
+             ? launch<float>(a, st)
+             : launch<uint16_t>(a, st);
 }
