@@ -201,7 +201,7 @@ __global__ __launch_bounds__(NT) void token_loss_kernel(LossArgs a) {
     for (int e = 0; e < E::n; ++e)
       E::set(d, e, exp_below(E::get(x, e), ref) * k -
                        (tb == c * E::n + e ? hit : 0.f));
-    dbody[c] = d;
+    __builtin_nontemporal_store(d, dbody + c);
   };
 #pragma unroll
   for (int i = 0; i < H; ++i)
