@@ -5,6 +5,8 @@
 //   dx = r (u - x r mean(u x r))  [+ the gradient that came past the norm]
 // Per-head q/k norm with RoPE: the gradient is first rotated back (by minus
 // the row's angles), then each head is such a norm over its D values.
+#include <cmath>
+
 #include "common.h"
 #include "wedlm_train.h"
 
@@ -13,7 +15,8 @@ using namespace wedlm;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kParts = 512;       // partial gain gradients of a call
+constexpr int kParts = 1024;      // partial gain gradients of a call, at most
+constexpr int kQkParts = 2048;
 
 // Sum over the wave.
 __device__ __forceinline__ float wave_sum(float v) {
@@ -165,116 +168,146 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_long_kernel(
 }
 
 // Columns of part [parts, n0 + n1] summed in a fixed order into out0 [n0] and
-// out1 [n1] (either may be null): 64 columns per workgroup, its four waves
-// take every fourth part.
-__global__ __launch_bounds__(kThreads) void sum_parts_kernel(
+// out1 [n1] (either may be null): 64 columns per workgroup, its 16 waves take
+// every 16th part, eight loads under way each (512 parts are four round trips
+// to memory; four waves with a load at a time took 25 us).
+constexpr int kSumThreads = 1024;
+
+__global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(
     const float* __restrict__ part, int parts, int n0, int n1,
     float* __restrict__ out0, float* __restrict__ out1) {
+  constexpr int W = kSumThreads / kWave;
   const int n = n0 + n1;
   const int c = blockIdx.x * kWave + lane_id();
   const int w = threadIdx.x / kWave;
-  __shared__ float s[kThreads / kWave][kWave];
+  __shared__ float s[W][kWave];
   float v = 0.f;
-  if (c < n)
-    for (int p = w; p < parts; p += kThreads / kWave)
-      v += part[static_cast<int64_t>(p) * n + c];
+  if (c < n) {
+    int p = w;
+    for (; p + 7 * W < parts; p += 8 * W) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[i] = part[static_cast<int64_t>(p + i * W) * n + c];
+      v += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    }
+#pragma unroll 4
+    for (; p < parts; p += W) v += part[static_cast<int64_t>(p) * n + c];
+  }
   s[w][lane_id()] = v;
   __syncthreads();
   float* out = c < n0 ? out0 : out1;
-  if (w == 0 && c < n && out)
-    out[c < n0 ? c : c - n0] = (s[0][lane_id()] + s[1][lane_id()]) +
-                               (s[2][lane_id()] + s[3][lane_id()]);
+  if (w == 0 && c < n && out) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) t += s[i][lane_id()];
+    out[c < n0 ? c : c - n0] = t;
+  }
 }
 
-// q/k norm with RoPE: one workgroup walks rows; an item is 8 rotation pairs
-// of one head, the D/16 items of a head sit on neighbouring lanes.  A thread
-// meets the same pairs j0 .. j0+7 of D in every item (the strides are
-// multiples of a head's items), so the gains' gradients stay in its
-// registers until the end.
+// q/k norm with RoPE: one workgroup walks groups of R rows; an item is 8
+// rotation pairs of one head of one row, the D/16 items of a head sit on
+// neighbouring lanes.  A thread meets the same pairs j0 .. j0+7 of D in every
+// item (the strides are multiples of a head's items), so the gains' gradients
+// stay in its registers until the end.  Four rows at once give every thread
+// an angle (64 bits: positions are far) and enough items to hide the loads;
+// one, where there are fewer rows than that fills the card with.
 constexpr int kMaxHalf = 64;
 
+struct QkArgs {
+  const uint16_t* qkv;
+  const uint16_t* gq;
+  const uint16_t* gk;
+  const int32_t* pos;
+  const uint16_t* dq;
+  const uint16_t* dk;
+  const uint16_t* dv;
+  uint16_t* dqkv;
+  float* part;            // [grid, 2, D] or null
+  int M, Hq, Hkv, D;
+  float eps;
+  double omega[kMaxHalf]; // theta^(-2j/D)
+};
+
+template <int R>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(
-    const uint16_t* __restrict__ qkv, const uint16_t* __restrict__ gq,
-    const uint16_t* __restrict__ gk, const int32_t* __restrict__ pos_ids,
-    const uint16_t* __restrict__ dq, const uint16_t* __restrict__ dk,
-    const uint16_t* __restrict__ dv, int M, int Hq, int Hkv, int D,
-    double theta, float eps, uint16_t* __restrict__ dqkv,
-    float* __restrict__ part) {
-  const int half = D / 2, per_head = half / 8;
-  const int n_items = (Hq + Hkv) * per_head, nv = Hkv * D / 8;
-  const int H = Hq + 2 * Hkv;
+    QkArgs a) {
+  const int half = a.D / 2, per_head = half / 8;
+  const int n_items = (a.Hq + a.Hkv) * per_head, nv = a.Hkv * a.D / 8;
+  const int H = a.Hq + 2 * a.Hkv;
   const int j0 = threadIdx.x % per_head * 8;
-  __shared__ float s_cos[kMaxHalf], s_sin[kMaxHalf];
+  __shared__ float s_cos[R][kMaxHalf], s_sin[R][kMaxHalf];
   __shared__ float s_dg[kThreads / kWave][2][2 * kMaxHalf];
   float dga[2][8] = {}, dgb[2][8] = {};
-  double omega = 0.0;
-  if (threadIdx.x < half)
-    omega = pow(theta, -2.0 * static_cast<double>(threadIdx.x) / D);
-  for (int t = blockIdx.x; t < M; t += gridDim.x) {
+  for (int t0 = blockIdx.x * R; t0 < a.M; t0 += gridDim.x * R) {
+    const int rows = min(R, a.M - t0);
     __syncthreads();
-    if (threadIdx.x < half) {
+    for (int i = threadIdx.x; i < R * half; i += kThreads) {
+      const int j = i % half, t = min(t0 + i / half, a.M - 1);
       double sn, cs;
-      sincos(static_cast<double>(pos_ids[t]) * omega, &sn, &cs);
-      s_cos[threadIdx.x] = static_cast<float>(cs);
-      s_sin[threadIdx.x] = static_cast<float>(sn);
+      sincos(static_cast<double>(a.pos[t]) * a.omega[j], &sn, &cs);
+      s_cos[i / half][j] = static_cast<float>(cs);
+      s_sin[i / half][j] = static_cast<float>(sn);
+    }
+    // the rows' v are one stretch of dv
+    for (int i = threadIdx.x; i < rows * nv; i += kThreads) {
+      const int t = i / nv;
+      *reinterpret_cast<u16x8_t*>(
+          a.dqkv + (static_cast<int64_t>(t0 + t) * H + a.Hq + a.Hkv) * a.D +
+          (i - t * nv) * 8) =
+          *reinterpret_cast<const u16x8_t*>(
+              a.dv + static_cast<int64_t>(t0) * a.Hkv * a.D + i * 8);
     }
     __syncthreads();
-    const int64_t row = static_cast<int64_t>(t) * H * D;
-    for (int base = 0; base < n_items + nv; base += kThreads) {
-      const int it = base + threadIdx.x;
-      if (it >= n_items) {
-        if (it < n_items + nv)
-          *reinterpret_cast<u16x8_t*>(dqkv + row + (Hq + Hkv) * D +
-                                      (it - n_items) * 8) =
-              *reinterpret_cast<const u16x8_t*>(
-                  dv + static_cast<int64_t>(t) * Hkv * D + (it - n_items) * 8);
-        continue;
-      }
-      const int head = it / per_head;
-      const bool isq = head < Hq;
-      const uint16_t* xp = qkv + row + head * D + j0;
-      const uint16_t* dp =
-          (isq ? dq + (static_cast<int64_t>(t) * Hq + head) * D
-               : dk + (static_cast<int64_t>(t) * Hkv + head - Hq) * D) + j0;
-      const uint16_t* gp = (isq ? gq : gk) + j0;
-      const u16x8_t xl = *reinterpret_cast<const u16x8_t*>(xp);
-      const u16x8_t xh = *reinterpret_cast<const u16x8_t*>(xp + half);
+    for (int i = threadIdx.x; i < rows * n_items; i += kThreads) {
+      const int tr = i / n_items, head = (i - tr * n_items) / per_head;
+      const int64_t t = t0 + tr;
+      const bool isq = head < a.Hq;
+      const int64_t o = (t * H + head) * a.D + j0;
+      const uint16_t* dp = (isq ? a.dq + (t * a.Hq + head) * a.D
+                                : a.dk + (t * a.Hkv + head - a.Hq) * a.D) + j0;
+      const uint16_t* gp = (isq ? a.gq : a.gk) + j0;
+      const u16x8_t xl = *reinterpret_cast<const u16x8_t*>(a.qkv + o);
+      const u16x8_t xh = *reinterpret_cast<const u16x8_t*>(a.qkv + o + half);
       const u16x8_t dl = *reinterpret_cast<const u16x8_t*>(dp);
       const u16x8_t dh = *reinterpret_cast<const u16x8_t*>(dp + half);
       const u16x8_t gl = *reinterpret_cast<const u16x8_t*>(gp);
       const u16x8_t gh = *reinterpret_cast<const u16x8_t*>(gp + half);
-      float a[8], b[8], za[8], zb[8], ss = 0.f, dot = 0.f;
+      float x[8], y[8], za[8], zb[8], ss = 0.f, dot = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        a[e] = bf16_to_f32(xl[e]);
-        b[e] = bf16_to_f32(xh[e]);
+        x[e] = bf16_to_f32(xl[e]);
+        y[e] = bf16_to_f32(xh[e]);
         const float lo = bf16_to_f32(dl[e]), hi = bf16_to_f32(dh[e]);
-        const float cs = s_cos[j0 + e], sn = s_sin[j0 + e];
+        const float cs = s_cos[tr][j0 + e], sn = s_sin[tr][j0 + e];
         za[e] = lo * cs + hi * sn;
         zb[e] = hi * cs - lo * sn;
-        ss += a[e] * a[e] + b[e] * b[e];
-        dot += za[e] * bf16_to_f32(gl[e]) * a[e] +
-               zb[e] * bf16_to_f32(gh[e]) * b[e];
+        ss += x[e] * x[e] + y[e] * y[e];
+        dot += za[e] * bf16_to_f32(gl[e]) * x[e] +
+               zb[e] * bf16_to_f32(gh[e]) * y[e];
       }
       for (int off = 1; off < per_head; off <<= 1) {
         ss += __shfl_xor(ss, off);
         dot += __shfl_xor(dot, off);
       }
-      const float r = 1.0f / sqrtf(ss / static_cast<float>(D) + eps);
-      const float k = dot * r / static_cast<float>(D) * r;
+      const float r = 1.0f / sqrtf(ss / static_cast<float>(a.D) + a.eps);
+      const float k = dot * r / static_cast<float>(a.D) * r;
       u16x8_t ol, oh;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dga[isq ? 0 : 1][e] += za[e] * (a[e] * r);
-        dgb[isq ? 0 : 1][e] += zb[e] * (b[e] * r);
-        ol[e] = f32_to_bf16(r * (za[e] * bf16_to_f32(gl[e]) - a[e] * k));
-        oh[e] = f32_to_bf16(r * (zb[e] * bf16_to_f32(gh[e]) - b[e] * k));
+        const float ga = za[e] * (x[e] * r), gb = zb[e] * (y[e] * r);
+        dga[0][e] += isq ? ga : 0.f;
+        dgb[0][e] += isq ? gb : 0.f;
+        dga[1][e] += isq ? 0.f : ga;
+        dgb[1][e] += isq ? 0.f : gb;
+        ol[e] = f32_to_bf16(r * (za[e] * bf16_to_f32(gl[e]) - x[e] * k));
+        oh[e] = f32_to_bf16(r * (zb[e] * bf16_to_f32(gh[e]) - y[e] * k));
       }
-      *reinterpret_cast<u16x8_t*>(dqkv + row + head * D + j0) = ol;
-      *reinterpret_cast<u16x8_t*>(dqkv + row + head * D + j0 + half) = oh;
+      *reinterpret_cast<u16x8_t*>(a.dqkv + o) = ol;
+      *reinterpret_cast<u16x8_t*>(a.dqkv + o + half) = oh;
     }
   }
-  if (!part) return;
+  if (!a.part) return;
   // lanes of equal j0, then the waves
 #pragma unroll
   for (int s = 0; s < 2; ++s)
@@ -291,19 +324,27 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(
       }
     }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
-    const int s = i / D, d = i % D;
-    part[static_cast<int64_t>(blockIdx.x) * 2 * D + i] =
+  for (int i = threadIdx.x; i < 2 * a.D; i += kThreads) {
+    const int s = i / a.D, d = i % a.D;
+    a.part[static_cast<int64_t>(blockIdx.x) * 2 * a.D + i] =
         (s_dg[0][s][d] + s_dg[1][s][d]) + (s_dg[2][s][d] + s_dg[3][s][d]);
   }
 }
 
 int norm_parts(int M) { return M < kParts ? M : kParts; }
 
+// rows that a workgroup of the q/k kernel takes at once, and workgroups
+constexpr int kQkRows = 4;
+int qk_rows(int M) { return M >= 2 * kQkRows * 256 ? kQkRows : 1; }
+int qk_parts(int M) {
+  const int groups = (M - 1) / qk_rows(M) + 1;
+  return groups < kQkParts ? groups : kQkParts;
+}
+
 int sum_parts(const float* part, int parts, int n0, int n1, float* out0,
               float* out1, hipStream_t st) {
   hipLaunchKernelGGL(sum_parts_kernel, dim3((n0 + n1 + kWave - 1) / kWave),
-                     dim3(kThreads), 0, st, part, parts, n0, n1, out0, out1);
+                     dim3(kSumThreads), 0, st, part, parts, n0, n1, out0, out1);
   WEDLM_LAUNCH_CHECK();
   return WEDLM_OK;
 }
@@ -333,10 +374,11 @@ extern "C" int wedlm_rmsnorm_backward(const float* x, const uint16_t* gain,
   hipStream_t st = static_cast<hipStream_t>(stream);
   float* part = dgain ? static_cast<float*>(workspace) : nullptr;
   const int parts = norm_parts(M), nc = Hd / 4;
-  auto k = nc <= kThreads       ? rmsnorm_backward_kernel<1>
-           : nc <= 2 * kThreads ? rmsnorm_backward_kernel<2>
-           : nc <= 4 * kThreads ? rmsnorm_backward_kernel<4>
-           : nc <= 8 * kThreads ? rmsnorm_backward_kernel<8>
+  auto k = nc <= kThreads        ? rmsnorm_backward_kernel<1>
+           : nc <= 2 * kThreads  ? rmsnorm_backward_kernel<2>
+           : nc <= 3 * kThreads  ? rmsnorm_backward_kernel<3>
+           : nc <= 4 * kThreads  ? rmsnorm_backward_kernel<4>
+           : nc <= 8 * kThreads  ? rmsnorm_backward_kernel<8>
            : nc <= 16 * kThreads ? rmsnorm_backward_kernel<16>
                                  : rmsnorm_backward_long_kernel;
   hipLaunchKernelGGL(k, dim3(parts), dim3(kThreads), 0, st, x, gain, dy, dres,
@@ -350,7 +392,7 @@ extern "C" size_t wedlm_qk_norm_rope_backward_workspace_size(int32_t M,
                                                              int32_t Hkv,
                                                              int32_t D) {
   if (!qk_ok(M, Hq, Hkv, D)) return 0;
-  return static_cast<size_t>(norm_parts(M)) * 2 * D * sizeof(float);
+  return static_cast<size_t>(qk_parts(M)) * 2 * D * sizeof(float);
 }
 
 extern "C" int wedlm_qk_norm_rope_backward(
@@ -370,10 +412,16 @@ extern "C" int wedlm_qk_norm_rope_backward(
     return WEDLM_E_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   float* part = gains ? static_cast<float*>(workspace) : nullptr;
-  const int parts = norm_parts(M);
-  hipLaunchKernelGGL(qk_norm_rope_backward_kernel, dim3(parts), dim3(kThreads),
-                     0, st, qkv, q_gain, k_gain, pos_ids, dq, dk, dv, M, Hq,
-                     Hkv, D, rope_theta, eps, dqkv, part);
+  QkArgs a{qkv, q_gain, k_gain, pos_ids, dq, dk, dv, dqkv, part, M, Hq, Hkv,
+           D, eps, {}};
+  for (int j = 0; j < D / 2; ++j) a.omega[j] = std::pow(rope_theta, -2.0 * j / D);
+  const int parts = qk_parts(M);
+  if (qk_rows(M) > 1)
+    hipLaunchKernelGGL(qk_norm_rope_backward_kernel<kQkRows>, dim3(parts),
+                       dim3(kThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL(qk_norm_rope_backward_kernel<1>, dim3(parts),
+                       dim3(kThreads), 0, st, a);
   WEDLM_LAUNCH_CHECK();
   return gains ? sum_parts(part, parts, D, D, dq_gain, dk_gain, st) : WEDLM_OK;
 }
