@@ -30,6 +30,8 @@
 // Each operand read from LDS feeds two MFMAs (the wave's two 32-row groups).
 // P and dS are rounded to bf16 for the second products, as the forward
 // rounds P; all sums are fp32.
+#include <algorithm>
+
 #include "common.h"
 #include "wedlm_train.h"
 
@@ -59,8 +61,10 @@ struct BwdArgs {
   uint16_t* dk;
   uint16_t* dv;
   float* ld;              // [n_seq, Hq, 2, T, 2, 32]: -lse (log2 units), -D
-  float* part;            // [2 (dk, dv)][nsplit][n_seq, L, Hkv, D], or null
-  int n_seq, L, block, Hq, Hkv, G, T, nsplit;
+  float* part;            // [2 W][2 (dk, dv)][256 keys][D] of cut tiles
+  int n_seq, L, block, Hq, Hkv, G, T;
+  int W;                  // workgroups of dkv_kernel
+  int group_cost;         // work of one (sequence, kv head) of it
   float scale, scale_log2;
 };
 
@@ -162,7 +166,8 @@ struct PairLoader {
   __device__ __forceinline__ void load(int u, int64_t o, int left,
                                        uint32_t dst) const {
     load_to_lds16<false>(buffer_rsrc(src + o, 31 * stride + 2 * D),
-                         min(row + u * T::per_group * stride, left * stride) +
+                         min(row + u * T::per_group * stride,
+                             min(left, kRows - 1) * stride) +
                              chunk,
                          lds + dst + u * T::group_bytes);
   }
@@ -466,8 +471,112 @@ void dq_kernel(BwdArgs a) {
   }
 }
 
-// dk and dv: workgroup = 256 keys of one stream and kv head; the memory
-// stream's tiles first (they have the long walks), the earliest keys first.
+// ---------------------------------------------------------------------------
+// The work of dk and dv: key tiles of 256 keys, each with a walk of row tiles
+// (its items).  The tiles of a (sequence, kv head) are listed in fours: memory
+// tiles i and n-1-i, whose walks add up to the same for every i, and the
+// prediction tiles i and n-1-i.  The list of all of them is cut into W
+// stretches of equal work, one per workgroup (one per CU); a cut near a
+// tile's end moves there, one inside a tile leaves two workgroups partial sums
+// of it, which a last kernel adds up in order.
+// ---------------------------------------------------------------------------
+constexpr int kTileCost = 4;     // a tile's fixed work, in items
+constexpr int kSnap = 6;         // items: no cut nearer to a tile's end
+
+// The key tile at position p of the list.
+struct KeyTile {
+  int stream, j0;
+  int t_hi, t_mid, t_lo;         // row tiles t_mid .. t_hi-1: both streams'
+  int items;                     // rows see it; t_lo .. t_mid-1: one's
+};
+
+__host__ __device__ inline int key_list(int L) {
+  return ((L + kKeysPerWg - 1) / kKeysPerWg + 1) / 2 * 4;
+}
+
+__host__ __device__ inline KeyTile key_tile(int L, int block, int G, int p) {
+  const int tiles = (L + kKeysPerWg - 1) / kKeysPerWg, T = (L + kRows - 1) / kRows;
+  const int i = p >> 2, other = tiles - 1 - i;
+  KeyTile x;
+  x.stream = p >> 1 & 1;
+  x.j0 = (p & 1 ? other : i) * kKeysPerWg;
+  const int kend = x.j0 + kKeysPerWg < L ? x.j0 + kKeysPerWg : L;
+  x.t_lo = x.j0 / kRows;
+  if (x.stream) {
+    const int end = ((kend - 1) / block + 1) * block;     // L, if not before
+    x.t_hi = x.t_mid = (end + kRows - 1) / kRows;
+  } else {
+    x.t_hi = T;
+    x.t_mid = (x.j0 / block + 1) * block / kRows;
+    if (x.t_mid > T) x.t_mid = T;
+  }
+  // the middle tile of an odd number is its own counterpart
+  x.items = (p & 1) && other == i
+                ? 0 : ((x.t_hi - x.t_mid) * 2 + (x.t_mid - x.t_lo)) * G;
+  return x;
+}
+
+// Where stretch w begins: list position p of group g, after `item` items of
+// its tile.
+struct Cut {
+  int g, p, item;
+  __device__ __forceinline__ bool before(const Cut& c) const {
+    return g != c.g ? g < c.g : p != c.p ? p < c.p : item < c.item;
+  }
+  // inside the same tile
+  __device__ __forceinline__ bool shares(const Cut& c) const {
+    return item > 0 && c.item > 0 && g == c.g && p == c.p;
+  }
+};
+
+__device__ inline Cut cut_at(const BwdArgs& a, int w) {
+  const int groups = a.n_seq * a.Hkv, list = key_list(a.L);
+  if (w >= a.W) return {groups, 0, 0};
+  const int64_t raw = static_cast<int64_t>(a.group_cost) * groups * w / a.W;
+  int g = static_cast<int>(raw / a.group_cost);
+  const int x = static_cast<int>(raw - static_cast<int64_t>(g) * a.group_cost);
+  int base = 0, p = 0, off = 0, cost = 0;
+  for (int p0 = 0; p0 < list; p0 += kWave) {
+    const int lp = p0 + lane_id();
+    int c = 0;
+    if (lp < list) {
+      c = key_tile(a.L, a.block, a.G, lp).items;
+      if (c) c += kTileCost;
+    }
+    int sum = c;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int y = __shfl_up(sum, o);
+      if (lane_id() >= o) sum += y;
+    }
+    const uint64_t past = ballot(base + sum > x);
+    if (past) {
+      const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      cost = __builtin_amdgcn_readlane(c, l);
+      off = x - base - (__builtin_amdgcn_readlane(sum, l) - cost);
+      p = p0 + l;
+      break;
+    }
+    base += __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  Cut r{g, p, off - kTileCost};
+  if (r.item < kSnap) {
+    r.item = 0;
+  } else if (cost - off < kSnap) {
+    r.item = 0;
+    if (++r.p == list) {
+      r.p = 0;
+      ++r.g;
+    }
+  }
+  r.g = __builtin_amdgcn_readfirstlane(r.g);
+  r.p = __builtin_amdgcn_readfirstlane(r.p);
+  r.item = __builtin_amdgcn_readfirstlane(r.item);
+  return r;
+}
+
+// dk and dv: workgroup w walks stretch w; workgroups of one XCD take
+// neighbouring stretches, of kv heads whose rows then stay in its L2.
 template <int D>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(1)))
@@ -477,31 +586,30 @@ void dkv_kernel(BwdArgs a) {
   constexpr int kPair = 2 * T::bytes;
   constexpr int kSlot = kPair + 2 * kRows * 4;     // rows' -lse, -D behind
   __shared__ __attribute__((aligned(1024))) char smem[kSlots * kSlot];
-  const int tiles = (a.L + kKeysPerWg - 1) / kKeysPerWg;
-  const int n_mem = a.n_seq * a.Hkv * tiles * a.nsplit;
-  int wg = blockIdx.x;
-  const int stream = wg >= n_mem ? 1 : 0;
-  if (stream) wg -= n_mem;
-  const int nsplit = stream ? 1 : a.nsplit;
-  const int kvh = wg % a.Hkv;
-  wg /= a.Hkv;
-  const int split = wg % nsplit;
-  wg /= nsplit;
-  const int j0 = wg % tiles * kKeysPerWg;
-  const int sq = wg / tiles;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int lane = lane_id(), col = lane & 31, hf = lane >> 5;
+  const int W = a.W, list = key_list(a.L);
+  const int w = W % 8 == 0 ? blockIdx.x % 8 * (W / 8) + blockIdx.x / 8
+                           : static_cast<int>(blockIdx.x);
+  const Cut end = cut_at(a, w + 1);
+  Cut at = cut_at(a, w);
+  const Reader<D> rd;
+  for (; at.before(end); at.item = 0, at.p = at.p + 1 == list ? 0 : at.p + 1,
+                         at.g += at.p == 0) {
+  const KeyTile kt = key_tile(a.L, a.block, a.G, at.p);
+  const int it0 = at.item;
+  const int it1 = at.g == end.g && at.p == end.p ? end.item : kt.items;
+  if (it0 >= it1) continue;
+  const int stream = kt.stream, j0 = kt.j0;
+  const int kvh = at.g / a.n_seq, sq = at.g - kvh * a.n_seq;
   const int kw0 = j0 + wave * kOwn;
+  // the last tile's reads of the ring are done
+  __syncthreads();
+  const int lane = lane_here(), col = lane & 31, hf = lane >> 5;
 
   bf16x8_t kf[2][NK], vf[2][NK];
-  // a lane's keys are kw0 + 32 b + col; those of the memory are seen by memory
-  // rows key .. L-1 and prediction rows next .. L-1 (next: the block after the
-  // key's), those of the prediction by prediction rows key .. next-1
-  int next[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int jc = min(kw0 + 32 * b + col, a.L - 1);
-    next[b] = min(a.L, (jc / a.block + 1) * a.block);
     const int64_t o =
         (((static_cast<int64_t>(sq) * 2 + stream) * a.L + jc) * a.Hkv + kvh) * D;
 #pragma unroll
@@ -519,19 +627,8 @@ void dkv_kernel(BwdArgs a) {
   // items: row tiles t from the last down, in each the streams that see the
   // keys (memory, prediction) and their heads.  Every workgroup of a kv head
   // starts at the same rows, which they then find in the L2
-  const int kend = min(a.L, j0 + kKeysPerWg);
-  int t_hi = a.T, t_mid, t_lo = j0 / kRows;
-  if (stream) {
-    t_hi = (min(a.L, ((kend - 1) / a.block + 1) * a.block) + kRows - 1) / kRows;
-    t_mid = t_hi;
-  } else {
-    t_mid = min(t_hi, (j0 / a.block + 1) * a.block / kRows);
-  }
+  const int t_hi = kt.t_hi, t_mid = kt.t_mid;
   const int n1 = (t_hi - t_mid) * 2 * a.G;
-  const int n_items = n1 + (t_mid - t_lo) * a.G;
-  const int it0 = static_cast<int>(static_cast<int64_t>(n_items) * split / nsplit);
-  const int it1 =
-      static_cast<int>(static_cast<int64_t>(n_items) * (split + 1) / nsplit);
   // an item: its row tile, its rows' stream and its head of the group.  Steps
   // are branches, so that everything stays in scalar registers
   struct Item {
@@ -589,19 +686,16 @@ void dkv_kernel(BwdArgs a) {
   auto advance = [&]() {
     if (++n_ahead < it1) next_item(ahead);
   };
-  const Reader<D> rd;
   constexpr int kE = 16 / NK;              // elements per step
   bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
   const int kwl = min(kw0 + kOwn, a.L) - 1;         // the wave's last key
   const int next_hi = (kwl / a.block + 1) * a.block;
   Item cur = item_at(it0);
-  if (it0 < it1) {
 #pragma unroll
-    for (int i = 0; i < kSlots - 1; ++i) {
+  for (int i = 0; i < kSlots - 1; ++i) {
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) fetch(u, i);
-      advance();
-    }
+    for (int u = 0; u < kLoads; ++u) fetch(u, i);
+    advance();
   }
   // take delivery of the keys: no wait for them in the loop
 #pragma unroll
@@ -634,10 +728,14 @@ void dkv_kernel(BwdArgs a) {
     float p[2][16];
     bf16x8_t pb[2][2], ds[2][2];
     auto hide = [&](int b) {
+      // a lane's key k0 of the memory is seen by memory rows k0 .. L-1 and
+      // prediction rows next .. L-1 (next: the block after the key's), one of
+      // the prediction by prediction rows k0 .. next-1
       const int l = lane_here();
       const int k0 = kw0 + 32 * b + (l & 31), i0 = p0 + 8 * (l >> 5);
-      const int from = pred ? next[b] : k0;
-      const int to = k0 < a.L ? stream ? next[b] : a.L : 0;
+      const int next = min(a.L, (min(k0, a.L - 1) / a.block + 1) * a.block);
+      const int from = pred ? next : k0;
+      const int to = k0 < a.L ? stream ? next : a.L : 0;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int i = i0 + 16 * (e >> 3) + (e & 7);
@@ -749,10 +847,10 @@ void dkv_kernel(BwdArgs a) {
     const int l = lane_here(), hf = l >> 5;
     const int key = kw0 + 32 * b + (l & 31);
     if (key >= a.L) continue;
-    const int64_t kv = static_cast<int64_t>(a.Hkv) * D;
-    if (nsplit == 1) {
+    if (it0 == 0 && it1 == kt.items) {
       const int64_t o =
-          ((static_cast<int64_t>(sq) * 2 + stream) * a.L + key) * kv + kvh * D;
+          (((static_cast<int64_t>(sq) * 2 + stream) * a.L + key) * a.Hkv + kvh) *
+          D;
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
@@ -767,9 +865,8 @@ void dkv_kernel(BwdArgs a) {
           *reinterpret_cast<u16x4_t*>(a.dv + o + 32 * m + 8 * g + 4 * hf) = y;
         }
     } else {
-      const int64_t n = a.n_seq * static_cast<int64_t>(a.L) * kv;
-      float* o = a.part + split * n +
-                 (static_cast<int64_t>(sq) * a.L + key) * kv + kvh * D;
+      float* o = a.part + (static_cast<int64_t>(2 * w + (it0 == 0)) * 2 *
+                               kKeysPerWg + key - j0) * D;
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
@@ -781,39 +878,56 @@ void dkv_kernel(BwdArgs a) {
             y[e] = dv[b][m][4 * g + e];
           }
           *reinterpret_cast<floatx4_t*>(o + 32 * m + 8 * g + 4 * hf) = x;
-          *reinterpret_cast<floatx4_t*>(o + a.nsplit * n + 32 * m + 8 * g +
+          *reinterpret_cast<floatx4_t*>(o + kKeysPerWg * D + 32 * m + 8 * g +
                                         4 * hf) = y;
         }
     }
   }
+  }
 }
 
-// dk and dv of the memory keys from the fp32 partials of the splits, added in
-// split order; four values a thread.
-__global__ __launch_bounds__(256) void join_kernel(
-    const float* __restrict__ part, int nsplit, int64_t n, int64_t per_seq,
-    uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
-  if (i >= n) return;
-  const float* src = part + (blockIdx.y ? nsplit * n : 0) + i;
-  floatx4_t s = *reinterpret_cast<const floatx4_t*>(src);
-  for (int k = 1; k < nsplit; ++k) {
-    const floatx4_t x = *reinterpret_cast<const floatx4_t*>(src + k * n);
+// dk and dv of the cut tiles: workgroup row w adds up the partial sums of the
+// tile whose first cut is w (the piece before it is stretch w-1's last, the
+// others are their stretches' first).
+template <int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(BwdArgs a) {
+  const int w = blockIdx.x + 1;
+  const Cut c = cut_at(a, w);
+  if (c.item == 0 || cut_at(a, w - 1).shares(c)) return;
+  int n = 1;
+  while (w + n < a.W && cut_at(a, w + n).shares(c)) ++n;
+  const KeyTile kt = key_tile(a.L, a.block, a.G, c.p);
+  const int keys = min(kKeysPerWg, a.L - kt.j0);
+  const int kvh = c.g / a.n_seq, sq = c.g - kvh * a.n_seq;
+  constexpr int64_t kPiece = 2 * kKeysPerWg * D;
+  const float* first = a.part + (2 * w - 1) * kPiece;
+  const float* others = a.part + 2 * w * kPiece;
+  for (int i = blockIdx.y * kThreads + threadIdx.x; i < 2 * keys * (D / 4);
+       i += gridDim.y * kThreads) {
+    const int which = i >= keys * (D / 4) ? 1 : 0;
+    const int e0 = (i - which * keys * (D / 4)) * 4;
+    const int64_t at = static_cast<int64_t>(which) * kKeysPerWg * D + e0;
+    floatx4_t s = *reinterpret_cast<const floatx4_t*>(first + at);
+    for (int k = 0; k < n; ++k) {
+      const floatx4_t x =
+          *reinterpret_cast<const floatx4_t*>(others + 2 * k * kPiece + at);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += x[e];
+      for (int e = 0; e < 4; ++e) s[e] += x[e];
+    }
+    u16x4_t o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = f32_to_bf16(s[e]);
+    *reinterpret_cast<u16x4_t*>(
+        (which ? a.dv : a.dk) +
+        (((static_cast<int64_t>(sq) * 2 + kt.stream) * a.L + kt.j0 + e0 / D) *
+             a.Hkv + kvh) * D + e0 % D) = o;
   }
-  u16x4_t o;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = f32_to_bf16(s[e]);
-  // memory rows are the first half of each sequence's
-  *reinterpret_cast<u16x4_t*>((blockIdx.y ? dv : dk) + i +
-                              i / per_seq * per_seq) = o;
 }
 
 struct BwdPlan {
-  int T, nsplit;
+  int T, W, group_cost;
   size_t part, total;
-  unsigned dq_grid, dkv_grid;
+  unsigned dq_grid;
 };
 
 size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
@@ -827,24 +941,21 @@ bool bwd_plan(int n_seq, int L, int block, int Hq, int Hkv, int D,
   p->T = (L + kRows - 1) / kRows;
   const int64_t chunks = (L + kOwn - 1) / kOwn;
   const int64_t dq = 2 * n_seq * ((chunks * G + kWaves - 1) / kWaves) * Hkv;
-  const int64_t tiles = static_cast<int64_t>(n_seq) * Hkv *
-                        ((L + kKeysPerWg - 1) / kKeysPerWg);
-  // Memory key tiles walk up to L rows of each head, half of that on
-  // average: two workgroups per CU even that out.  With fewer tiles than
-  // that the walks are split, down to four row tiles each.
-  const int64_t longest = 2ll * G * p->T;
-  int64_t ns = (512 + tiles - 1) / tiles;
-  if (ns > longest / 4) ns = longest / 4;
-  if (ns < 1) ns = 1;
-  p->nsplit = static_cast<int>(ns);
-  const int64_t dkv = tiles * (ns + 1);
-  if (dq > 0x7fffffffll || dkv > 0x7fffffffll) return false;
+  int64_t cost = 0;
+  for (int i = 0; i < key_list(L); ++i) {
+    const int items = key_tile(L, block, G, i).items;
+    if (items) cost += items + kTileCost;
+  }
+  if (dq > 0x7fffffffll || cost > 0x7fffffffll) return false;
+  // one workgroup per CU, but none with less than 16 items' work
+  const int64_t all = cost * n_seq * Hkv;
+  p->W = static_cast<int>(std::min<int64_t>(256, std::max<int64_t>(1, all / 16)));
+  p->group_cost = static_cast<int>(cost);
   p->dq_grid = static_cast<unsigned>(dq);
-  p->dkv_grid = static_cast<unsigned>(dkv);
   p->part = up256(static_cast<size_t>(n_seq) * Hq * 2 * p->T * 2 * kRows * 4);
   p->total = p->part;
-  if (ns > 1)
-    p->total += up256(2 * ns * static_cast<size_t>(n_seq) * L * Hkv * D * 4);
+  if (p->W > 1)
+    p->total += static_cast<size_t>(p->W) * 2 * 2 * kKeysPerWg * D * 4;
   return true;
 }
 
@@ -882,7 +993,7 @@ extern "C" int wedlm_dual_stream_attn_backward(
   a.dk = dk;
   a.dv = dv;
   a.ld = reinterpret_cast<float*>(ws);
-  a.part = p.nsplit > 1 ? reinterpret_cast<float*>(ws + p.part) : nullptr;
+  a.part = reinterpret_cast<float*>(ws + p.part);
   a.n_seq = n_seq;
   a.L = L;
   a.block = block;
@@ -890,21 +1001,19 @@ extern "C" int wedlm_dual_stream_attn_backward(
   a.Hkv = Hkv;
   a.G = Hq / Hkv;
   a.T = p.T;
-  a.nsplit = p.nsplit;
+  a.W = p.W;
+  a.group_cost = p.group_cost;
   a.scale = softmax_scale;
   a.scale_log2 = softmax_scale * kLog2e;
   hipLaunchKernelGGL(D == 128 ? dq_kernel<128> : dq_kernel<64>,
                      dim3(p.dq_grid), dim3(kThreads), 0, st, a);
   WEDLM_LAUNCH_CHECK();
   hipLaunchKernelGGL(D == 128 ? dkv_kernel<128> : dkv_kernel<64>,
-                     dim3(p.dkv_grid), dim3(kThreads), 0, st, a);
+                     dim3(p.W), dim3(kThreads), 0, st, a);
   WEDLM_LAUNCH_CHECK();
-  if (p.nsplit > 1) {
-    const int64_t per_seq = static_cast<int64_t>(L) * Hkv * D;
-    const int64_t n = n_seq * per_seq;
-    hipLaunchKernelGGL(join_kernel,
-                       dim3(static_cast<unsigned>((n / 4 + 255) / 256), 2),
-                       dim3(256), 0, st, a.part, p.nsplit, n, per_seq, dk, dv);
+  if (p.W > 1) {
+    hipLaunchKernelGGL(D == 128 ? join_kernel<128> : join_kernel<64>,
+                       dim3(p.W - 1, 16), dim3(kThreads), 0, st, a);
     WEDLM_LAUNCH_CHECK();
   }
   return WEDLM_OK;

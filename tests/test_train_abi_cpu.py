@@ -29,8 +29,8 @@ def refusals(call, args, cases):
 def test_attention_backward_workspace():
     ws = _lib().wedlm_dual_stream_attn_backward_workspace_size
     assert ws(1, 128, 32, 4, 2, 64) > 0
-    # one split: lse and D of 4 x 2 x 4096 rows of 32 heads
-    assert ws(4, 4096, 32, 32, 8, 128) == 4 * 8192 * 32 * 8
+    # lse and D of 4 x 2 x 4096 rows of 32 heads, and partial sums
+    assert ws(4, 4096, 32, 32, 8, 128) > 4 * 8192 * 32 * 8
     for bad in ((0, 128, 32, 4, 2, 64), (1, 100, 32, 4, 2, 64),
                 (1, 128, 96, 4, 2, 64), (1, 128, 32, 4, 2, 96),
                 (1, 128, 32, 5, 2, 64), (1, 128, 0, 4, 2, 64),
