@@ -219,6 +219,24 @@ __device__ __forceinline__ void meet() {
   asm volatile("s_barrier" ::: "memory");
 }
 
+// x where bit e of see is set, -inf elsewhere.
+__device__ __forceinline__ float seen(uint32_t see, int e, float x) {
+  const uint32_t m = __builtin_amdgcn_sbfe(see, e, 1);       // 0 or ~0
+  return __uint_as_float((__float_as_uint(x) & m) |
+                         (__float_as_uint(kNegInf) & ~m));
+}
+
+// Bits e of the elements of a lane (tile rows 16 (e / 8) + 8 hf + e % 8) whose
+// rows lie in from .. to-1, both relative to row 8 hf of the tile.
+__device__ __forceinline__ uint32_t rows_between(int from, int to) {
+  // rows 0 .. 7 and 16 .. 23 of 32 bits
+  const uint32_t below_to = to <= 0 ? 0u : to >= 32 ? ~0u : (1u << to) - 1u;
+  const uint32_t below_from =
+      from <= 0 ? 0u : from >= 32 ? ~0u : (1u << from) - 1u;
+  const uint32_t m = below_to & ~below_from;
+  return (m & 0xffu) | (m >> 8 & 0xff00u);
+}
+
 // Lane index, computed where it stands (no register from outside the loop).
 __device__ __forceinline__ int lane_here() {
   int l;
@@ -372,12 +390,11 @@ void dq_kernel(BwdArgs a) {
     float p[2][16];
     bf16x8_t ds[2][2];
     auto hide = [&](int b) {
+      const int k0 = j0 + 8 * (lane_here() >> 5);
+      const int from = own ? lo[b] : 0, to = own || !stream ? hi[b] : lo[b];
+      const uint32_t see = rows_between(from - k0, to - k0);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int j = j0 + 16 * (e >> 3) + 8 * hf + (e & 7);
-        const int from = own ? lo[b] : 0, to = own || !stream ? hi[b] : lo[b];
-        s[b][e] = j >= from && j < to ? s[b][e] : kNegInf;
-      }
+      for (int e = 0; e < 16; ++e) s[b][e] = seen(see, e, s[b][e]);
     };
     auto weigh = [&](int b, int kk) {       // P
 #pragma unroll
@@ -486,8 +503,8 @@ constexpr int kSnap = 6;         // items: no cut nearer to a tile's end
 // The key tile at position p of the list.
 struct KeyTile {
   int stream, j0;
-  int t_hi, t_mid, t_lo;         // row tiles t_mid .. t_hi-1: both streams'
-  int items;                     // rows see it; t_lo .. t_mid-1: one's
+  int t_hi, t_mid;               // memory keys: both streams see them from row
+  int items;                     // tile t_mid on, memory rows alone before
 };
 
 __host__ __device__ inline int key_list(int L) {
@@ -500,19 +517,17 @@ __host__ __device__ inline KeyTile key_tile(int L, int block, int G, int p) {
   KeyTile x;
   x.stream = p >> 1 & 1;
   x.j0 = (p & 1 ? other : i) * kKeysPerWg;
-  const int kend = x.j0 + kKeysPerWg < L ? x.j0 + kKeysPerWg : L;
-  x.t_lo = x.j0 / kRows;
-  if (x.stream) {
-    const int end = ((kend - 1) / block + 1) * block;     // L, if not before
-    x.t_hi = x.t_mid = (end + kRows - 1) / kRows;
-  } else {
-    x.t_hi = T;
-    x.t_mid = (x.j0 / block + 1) * block / kRows;
-    if (x.t_mid > T) x.t_mid = T;
-  }
+  x.t_hi = T;
+  x.t_mid = x.stream ? T : (x.j0 / block + 1) * block / kRows;
+  if (x.t_mid > T) x.t_mid = T;
+  // row tiles of a wave's 64 prediction keys: up to the end of the last one's
+  // block
+  const int own = kOwn % block == 0 ? kOwn / kRows
+                                    : (kOwn - 1 + block + kRows - 1) / kRows;
   // the middle tile of an odd number is its own counterpart
-  x.items = (p & 1) && other == i
-                ? 0 : ((x.t_hi - x.t_mid) * 2 + (x.t_mid - x.t_lo)) * G;
+  x.items = (p & 1) && other == i ? 0
+            : x.stream            ? own * G
+                       : ((T - x.t_mid) * 2 + (x.t_mid - x.j0 / kRows)) * G;
   return x;
 }
 
@@ -585,7 +600,10 @@ void dkv_kernel(BwdArgs a) {
   using T = RowTile<D>;
   constexpr int kPair = 2 * T::bytes;
   constexpr int kSlot = kPair + 2 * kRows * 4;     // rows' -lse, -D behind
-  __shared__ __attribute__((aligned(1024))) char smem[kSlots * kSlot];
+  // the ring, or two slots for each wave and one that nobody reads
+  constexpr int kAll = 2 * kWaves + 1;
+  static_assert(kAll >= kSlots, "the ring");
+  __shared__ __attribute__((aligned(1024))) char smem[kAll * kSlot];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int W = a.W, list = key_list(a.L);
   const int w = W % 8 == 0 ? blockIdx.x % 8 * (W / 8) + blockIdx.x / 8
@@ -624,26 +642,32 @@ void dkv_kernel(BwdArgs a) {
 #pragma unroll
     for (int m = 0; m < NM; ++m) dk[b][m] = dv[b][m] = floatx16_t{};
 
-  // items: row tiles t from the last down, in each the streams that see the
-  // keys (memory, prediction) and their heads.  Every workgroup of a kv head
-  // starts at the same rows, which they then find in the L2
+  // Items of memory keys: row tiles t from the last down, in each the streams
+  // that see the keys (memory, prediction) and their heads; the waves share
+  // the tiles.  Every workgroup of a kv head starts at the same rows, which
+  // they then find in the L2.  Items of prediction keys: each wave's own few
+  // row tiles from its first key on, in each the heads; every wave loads for
+  // itself, a tile ahead, into two slots of its own.
+  // Steps are branches, so that everything stays in scalar registers
   const int t_hi = kt.t_hi, t_mid = kt.t_mid;
   const int n1 = (t_hi - t_mid) * 2 * a.G;
-  // an item: its row tile, its rows' stream and its head of the group.  Steps
-  // are branches, so that everything stays in scalar registers
   struct Item {
-    int t, rs, g;
+    int t, rs, g;             // row tile, its rows' stream, head of the group
   };
   auto item_at = [&](int it) {
     Item x;
-    if (it < n1) {
+    if (stream) {
+      x.t = kw0 / kRows + it / a.G;
+      x.g = it;
+      x.rs = 1;
+    } else if (it < n1) {
       x.t = t_hi - 1 - it / (2 * a.G);
       x.g = it % (2 * a.G);
       x.rs = x.g / a.G;
     } else {
       x.t = t_mid - 1 - (it - n1) / a.G;
       x.g = it - n1;
-      x.rs = stream;
+      x.rs = 0;
     }
     x.g %= a.G;
     return x;
@@ -651,10 +675,12 @@ void dkv_kernel(BwdArgs a) {
   auto next_item = [&](Item& x) {
     if (++x.g < a.G) return;
     x.g = 0;
-    if (x.rs == 0 && x.t >= t_mid) {
+    if (stream) {
+      ++x.t;
+    } else if (x.rs == 0 && x.t >= t_mid) {
       x.rs = 1;
     } else {
-      x.rs = stream;
+      x.rs = 0;
       --x.t;
     }
   };
@@ -667,20 +693,38 @@ void dkv_kernel(BwdArgs a) {
   // the item that is loaded next
   Item ahead = item_at(it0);
   int n_ahead = it0;
+  auto row_values_at = [&]() {
+    return ld0 + static_cast<int64_t>((ahead.g * 2 + ahead.rs) * a.T +
+                                      min(ahead.t, a.T - 1)) * (2 * kRows);
+  };
+  auto rows_at = [&]() {       // elements from q0 (row tiles past the last: it)
+    return static_cast<int64_t>(ahead.rs * a.L + min(ahead.t, a.T - 1) * kRows) *
+               (a.Hq * D) + ahead.g * D;
+  };
   auto fetch = [&](int u, int slot) {
-    if (u < PairLoader<D>::kCount) {
-      loader.load(u,
-                  static_cast<int64_t>(ahead.rs * a.L + ahead.t * kRows) *
-                          (a.Hq * D) + ahead.g * D,
-                  a.L - 1 - ahead.t * kRows, slot * kSlot);
-    } else {
+    const int left = a.L - 1 - min(ahead.t, a.T - 1) * kRows;
+    if (u < PairLoader<D>::kCount)
+      loader.load(u, rows_at(), left, slot * kSlot);
+    else
       // every wave the same 256 bytes, so that all wait for as many loads
-      const float* l =
-          ld0 + static_cast<int64_t>((ahead.g * 2 + ahead.rs) * a.T + ahead.t) *
-                    (2 * kRows);
-      load_to_lds4(buffer_rsrc(l, 2 * kRows * 4), lane_here() * 4,
+      load_to_lds4(buffer_rsrc(row_values_at(), 2 * kRows * 4), lane_here() * 4,
                    lds0 + slot * kSlot + kPair);
-    }
+  };
+  // the whole of a tile by this wave
+  auto fetch_own = [&](int slot) {
+    const int left = a.L - 1 - min(ahead.t, a.T - 1) * kRows;
+    const int64_t o = rows_at();
+    const int l = lane_here(), i = l / T::chunks;
+    const int chunk = ((l % T::chunks) ^ T::swz(i)) * 16, stride = a.Hq * D * 2;
+#pragma unroll
+    for (int g = 0; g < 2 * T::groups; ++g)
+      load_to_lds16<false>(
+          buffer_rsrc((g < T::groups ? a.q : a.dout) + q0 + o,
+                      31 * stride + 2 * D),
+          min(g % T::groups * T::per_group + i, left) * stride + chunk,
+          lds0 + slot * kSlot + g * T::group_bytes);
+    load_to_lds4(buffer_rsrc(row_values_at(), 2 * kRows * 4), l * 4,
+                 lds0 + slot * kSlot + kPair);
   };
   // past the end: the last item again, into a slot that nobody reads
   auto advance = [&]() {
@@ -691,11 +735,23 @@ void dkv_kernel(BwdArgs a) {
   const int kwl = min(kw0 + kOwn, a.L) - 1;         // the wave's last key
   const int next_hi = (kwl / a.block + 1) * a.block;
   Item cur = item_at(it0);
-#pragma unroll
-  for (int i = 0; i < kSlots - 1; ++i) {
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) fetch(u, i);
+  int slot, next_slot, load_slot;
+  if (stream) {
+    slot = 2 * wave;
+    next_slot = slot + 1;
+    load_slot = 2 * kWaves;        // the shared loads go where nobody reads
+    fetch_own(slot);
     advance();
+  } else {
+    slot = 0;
+    next_slot = 1;
+    load_slot = kSlots - 1;
+#pragma unroll
+    for (int i = 0; i < kSlots - 1; ++i) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) fetch(u, i);
+      advance();
+    }
   }
   // take delivery of the keys: no wait for them in the loop
 #pragma unroll
@@ -703,16 +759,26 @@ void dkv_kernel(BwdArgs a) {
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
       asm volatile("" : "+v"(kf[b][kk]), "+v"(vf[b][kk]));
-  wait_vmcnt<(kSlots - 2) * kLoads>();
-  __syncthreads();
+  if (!stream) {
+    wait_vmcnt<(kSlots - 2) * kLoads>();
+    __syncthreads();
 #pragma unroll
-  for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem, kk);
-  int slot = 0, next_slot = 1, load_slot = kSlots - 1;
+    for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem, kk);
+  }
   for (int it = it0; it < it1; ++it) {
-    // this wave's loads of the next item, then everybody's; the barrier also
-    // frees the slot of the previous one
-    wait_vmcnt<(kSlots - 3) * kLoads>();
-    meet();
+    if (stream) {
+      // this wave's tile; the other slot is free
+      wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+      fetch_own(next_slot);
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem + slot * kSlot, kk);
+    } else {
+      // this wave's loads of the next item, then everybody's; the barrier also
+      // frees the slot of the previous one
+      wait_vmcnt<(kSlots - 3) * kLoads>();
+      meet();
+    }
     const char* qt = smem + slot * kSlot;
     const char* ot = qt + T::bytes;
     const floatx4_t* ldt =
@@ -736,11 +802,9 @@ void dkv_kernel(BwdArgs a) {
       const int next = min(a.L, (min(k0, a.L - 1) / a.block + 1) * a.block);
       const int from = pred ? next : k0;
       const int to = k0 < a.L ? stream ? next : a.L : 0;
+      const uint32_t see = rows_between(from - i0, to - i0);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int i = i0 + 16 * (e >> 3) + (e & 7);
-        s[b][e] = i >= from && i < to ? s[b][e] : kNegInf;
-      }
+      for (int e = 0; e < 16; ++e) s[b][e] = seen(see, e, s[b][e]);
     };
     // -lse (x < 4) and -D (x >= 4) of rows 16 (x / 2 % 2) + 8 hf + 4 (x % 2) ..
     auto row_values = [&](int x) {
@@ -835,9 +899,14 @@ void dkv_kernel(BwdArgs a) {
     }
     next_item(cur);
     advance();
-    load_slot = slot;
-    slot = next_slot;
-    next_slot = next_slot == kSlots - 1 ? 0 : next_slot + 1;
+    if (stream) {
+      slot = next_slot;
+      next_slot ^= 1;
+    } else {
+      load_slot = slot;
+      slot = next_slot;
+      next_slot = next_slot == kSlots - 1 ? 0 : next_slot + 1;
+    }
   }
   wait_vmcnt<0>();      // surplus loads land before the LDS is given up
   drain(dv);
