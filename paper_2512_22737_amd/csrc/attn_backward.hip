@@ -63,6 +63,7 @@ struct BwdArgs {
   float* ld;              // [n_seq, Hq, 2, T, 2, 32]: -lse (log2 units), -D
   float* part;            // [2 W][2 (dk, dv)][256 keys][D] of cut tiles
   int n_seq, L, block, Hq, Hkv, G, T;
+  int4* cuts;             // [W + 1]: see Cut
   int W;                  // workgroups of dkv_kernel
   int group_cost;         // work of one (sequence, kv head) of it
   float scale, scale_log2;
@@ -260,6 +261,120 @@ __device__ __forceinline__ void drain(floatx16_t (&acc)[2][N]) {
     for (int m = 0; m < N; ++m) asm volatile("" : "+a"(acc[b][m]));
 }
 
+// ---------------------------------------------------------------------------
+// The work of dk and dv: key tiles of 256 keys, each with a walk of row tiles
+// (its items).  The tiles of a (sequence, kv head) are listed in fours: memory
+// tiles i and n-1-i, whose walks add up to the same for every i, and the
+// prediction tiles i and n-1-i.  The list of all of them is cut into W
+// stretches of equal work, one per workgroup (one per CU); a cut near a
+// tile's end moves there, one inside a tile leaves two workgroups partial sums
+// of it, which a last kernel adds up in order.
+// ---------------------------------------------------------------------------
+constexpr int kTileCost = 4;     // a tile's fixed work, in items
+constexpr int kSnap = 6;         // items: no cut nearer to a tile's end
+
+// The key tile at position p of the list.
+struct KeyTile {
+  int stream, j0;
+  int t_hi, t_mid;               // memory keys: both streams see them from row
+  int items;                     // tile t_mid on, memory rows alone before
+};
+
+__host__ __device__ inline int key_list(int L) {
+  return ((L + kKeysPerWg - 1) / kKeysPerWg + 1) / 2 * 4;
+}
+
+__host__ __device__ inline KeyTile key_tile(int L, int block, int G, int p) {
+  const int tiles = (L + kKeysPerWg - 1) / kKeysPerWg, T = (L + kRows - 1) / kRows;
+  const int i = p >> 2, other = tiles - 1 - i;
+  KeyTile x;
+  x.stream = p >> 1 & 1;
+  x.j0 = (p & 1 ? other : i) * kKeysPerWg;
+  x.t_hi = T;
+  x.t_mid = x.stream ? T : (x.j0 / block + 1) * block / kRows;
+  if (x.t_mid > T) x.t_mid = T;
+  // row tiles of a wave's 64 prediction keys: up to the end of the last one's
+  // block
+  const int own = kOwn % block == 0 ? kOwn / kRows
+                                    : (kOwn - 1 + block + kRows - 1) / kRows;
+  // the middle tile of an odd number is its own counterpart
+  x.items = (p & 1) && other == i ? 0
+            : x.stream            ? own * G
+                       : ((T - x.t_mid) * 2 + (x.t_mid - x.j0 / kRows)) * G;
+  return x;
+}
+
+// Where stretch w begins: list position p of group g, after `item` items of
+// its tile.
+struct Cut {
+  int g, p, item;
+  __device__ __forceinline__ bool before(const Cut& c) const {
+    return g != c.g ? g < c.g : p != c.p ? p < c.p : item < c.item;
+  }
+  // inside the same tile
+  __device__ __forceinline__ bool shares(const Cut& c) const {
+    return item > 0 && c.item > 0 && g == c.g && p == c.p;
+  }
+};
+
+__device__ inline Cut cut_at(const BwdArgs& a, int w) {
+  const int groups = a.n_seq * a.Hkv, list = key_list(a.L);
+  if (w >= a.W) return {groups, 0, 0};
+  const int64_t raw = static_cast<int64_t>(a.group_cost) * groups * w / a.W;
+  int g = static_cast<int>(raw / a.group_cost);
+  const int x = static_cast<int>(raw - static_cast<int64_t>(g) * a.group_cost);
+  int base = 0, p = 0, off = 0, cost = 0;
+  for (int p0 = 0; p0 < list; p0 += kWave) {
+    const int lp = p0 + lane_id();
+    int c = 0;
+    if (lp < list) {
+      c = key_tile(a.L, a.block, a.G, lp).items;
+      if (c) c += kTileCost;
+    }
+    int sum = c;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int y = __shfl_up(sum, o);
+      if (lane_id() >= o) sum += y;
+    }
+    const uint64_t past = ballot(base + sum > x);
+    if (past) {
+      const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      cost = __builtin_amdgcn_readlane(c, l);
+      off = x - base - (__builtin_amdgcn_readlane(sum, l) - cost);
+      p = p0 + l;
+      break;
+    }
+    base += __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  Cut r{g, p, off - kTileCost};
+  if (r.item < kSnap) {
+    r.item = 0;
+  } else if (cost - off < kSnap) {
+    r.item = 0;
+    if (++r.p == list) {
+      r.p = 0;
+      ++r.g;
+    }
+  }
+  return r;
+}
+
+// The cuts are found once, by dq_kernel's workgroups, for the kernels after it.
+__device__ inline void write_cuts(const BwdArgs& a) {
+  for (int w = blockIdx.x; w <= a.W; w += gridDim.x) {
+    const Cut c = cut_at(a, w);
+    if (lane_id() == 0) a.cuts[w] = make_int4(c.g, c.p, c.item, 0);
+  }
+}
+
+__device__ __forceinline__ Cut read_cut(const BwdArgs& a, int w) {
+  const int4 c = a.cuts[w];
+  return {__builtin_amdgcn_readfirstlane(c.x),
+          __builtin_amdgcn_readfirstlane(c.y),
+          __builtin_amdgcn_readfirstlane(c.z)};
+}
+
 // dq: workgroup = four units (64-position chunk, head) of one stream and kv
 // head, one per wave; the longest first.
 template <int D>
@@ -363,6 +478,7 @@ void dq_kernel(BwdArgs a) {
     for (int u = 0; u < kLoads; ++u) fetch(u, i);
     advance();
   }
+  if (wave == 0) write_cuts(a);
   // take delivery of the rows: no wait for them in the loop
 #pragma unroll
   for (int b = 0; b < 2; ++b)
@@ -488,108 +604,6 @@ void dq_kernel(BwdArgs a) {
   }
 }
 
-// ---------------------------------------------------------------------------
-// The work of dk and dv: key tiles of 256 keys, each with a walk of row tiles
-// (its items).  The tiles of a (sequence, kv head) are listed in fours: memory
-// tiles i and n-1-i, whose walks add up to the same for every i, and the
-// prediction tiles i and n-1-i.  The list of all of them is cut into W
-// stretches of equal work, one per workgroup (one per CU); a cut near a
-// tile's end moves there, one inside a tile leaves two workgroups partial sums
-// of it, which a last kernel adds up in order.
-// ---------------------------------------------------------------------------
-constexpr int kTileCost = 4;     // a tile's fixed work, in items
-constexpr int kSnap = 6;         // items: no cut nearer to a tile's end
-
-// The key tile at position p of the list.
-struct KeyTile {
-  int stream, j0;
-  int t_hi, t_mid;               // memory keys: both streams see them from row
-  int items;                     // tile t_mid on, memory rows alone before
-};
-
-__host__ __device__ inline int key_list(int L) {
-  return ((L + kKeysPerWg - 1) / kKeysPerWg + 1) / 2 * 4;
-}
-
-__host__ __device__ inline KeyTile key_tile(int L, int block, int G, int p) {
-  const int tiles = (L + kKeysPerWg - 1) / kKeysPerWg, T = (L + kRows - 1) / kRows;
-  const int i = p >> 2, other = tiles - 1 - i;
-  KeyTile x;
-  x.stream = p >> 1 & 1;
-  x.j0 = (p & 1 ? other : i) * kKeysPerWg;
-  x.t_hi = T;
-  x.t_mid = x.stream ? T : (x.j0 / block + 1) * block / kRows;
-  if (x.t_mid > T) x.t_mid = T;
-  // row tiles of a wave's 64 prediction keys: up to the end of the last one's
-  // block
-  const int own = kOwn % block == 0 ? kOwn / kRows
-                                    : (kOwn - 1 + block + kRows - 1) / kRows;
-  // the middle tile of an odd number is its own counterpart
-  x.items = (p & 1) && other == i ? 0
-            : x.stream            ? own * G
-                       : ((T - x.t_mid) * 2 + (x.t_mid - x.j0 / kRows)) * G;
-  return x;
-}
-
-// Where stretch w begins: list position p of group g, after `item` items of
-// its tile.
-struct Cut {
-  int g, p, item;
-  __device__ __forceinline__ bool before(const Cut& c) const {
-    return g != c.g ? g < c.g : p != c.p ? p < c.p : item < c.item;
-  }
-  // inside the same tile
-  __device__ __forceinline__ bool shares(const Cut& c) const {
-    return item > 0 && c.item > 0 && g == c.g && p == c.p;
-  }
-};
-
-__device__ inline Cut cut_at(const BwdArgs& a, int w) {
-  const int groups = a.n_seq * a.Hkv, list = key_list(a.L);
-  if (w >= a.W) return {groups, 0, 0};
-  const int64_t raw = static_cast<int64_t>(a.group_cost) * groups * w / a.W;
-  int g = static_cast<int>(raw / a.group_cost);
-  const int x = static_cast<int>(raw - static_cast<int64_t>(g) * a.group_cost);
-  int base = 0, p = 0, off = 0, cost = 0;
-  for (int p0 = 0; p0 < list; p0 += kWave) {
-    const int lp = p0 + lane_id();
-    int c = 0;
-    if (lp < list) {
-      c = key_tile(a.L, a.block, a.G, lp).items;
-      if (c) c += kTileCost;
-    }
-    int sum = c;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int y = __shfl_up(sum, o);
-      if (lane_id() >= o) sum += y;
-    }
-    const uint64_t past = ballot(base + sum > x);
-    if (past) {
-      const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
-      cost = __builtin_amdgcn_readlane(c, l);
-      off = x - base - (__builtin_amdgcn_readlane(sum, l) - cost);
-      p = p0 + l;
-      break;
-    }
-    base += __builtin_amdgcn_readlane(sum, kWave - 1);
-  }
-  Cut r{g, p, off - kTileCost};
-  if (r.item < kSnap) {
-    r.item = 0;
-  } else if (cost - off < kSnap) {
-    r.item = 0;
-    if (++r.p == list) {
-      r.p = 0;
-      ++r.g;
-    }
-  }
-  r.g = __builtin_amdgcn_readfirstlane(r.g);
-  r.p = __builtin_amdgcn_readfirstlane(r.p);
-  r.item = __builtin_amdgcn_readfirstlane(r.item);
-  return r;
-}
-
 // dk and dv: workgroup w walks stretch w; workgroups of one XCD take
 // neighbouring stretches, of kv heads whose rows then stay in its L2.
 template <int D>
@@ -608,8 +622,8 @@ void dkv_kernel(BwdArgs a) {
   const int W = a.W, list = key_list(a.L);
   const int w = W % 8 == 0 ? blockIdx.x % 8 * (W / 8) + blockIdx.x / 8
                            : static_cast<int>(blockIdx.x);
-  const Cut end = cut_at(a, w + 1);
-  Cut at = cut_at(a, w);
+  const Cut end = read_cut(a, w + 1);
+  Cut at = read_cut(a, w);
   const Reader<D> rd;
   for (; at.before(end); at.item = 0, at.p = at.p + 1 == list ? 0 : at.p + 1,
                          at.g += at.p == 0) {
@@ -961,10 +975,10 @@ void dkv_kernel(BwdArgs a) {
 template <int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(BwdArgs a) {
   const int w = blockIdx.x + 1;
-  const Cut c = cut_at(a, w);
-  if (c.item == 0 || cut_at(a, w - 1).shares(c)) return;
+  const Cut c = read_cut(a, w);
+  if (c.item == 0 || read_cut(a, w - 1).shares(c)) return;
   int n = 1;
-  while (w + n < a.W && cut_at(a, w + n).shares(c)) ++n;
+  while (w + n < a.W && read_cut(a, w + n).shares(c)) ++n;
   const KeyTile kt = key_tile(a.L, a.block, a.G, c.p);
   const int keys = min(kKeysPerWg, a.L - kt.j0);
   const int kvh = c.g / a.n_seq, sq = c.g - kvh * a.n_seq;
@@ -977,11 +991,17 @@ __global__ __launch_bounds__(kThreads) void join_kernel(BwdArgs a) {
     const int e0 = (i - which * keys * (D / 4)) * 4;
     const int64_t at = static_cast<int64_t>(which) * kKeysPerWg * D + e0;
     floatx4_t s = *reinterpret_cast<const floatx4_t*>(first + at);
-    for (int k = 0; k < n; ++k) {
-      const floatx4_t x =
-          *reinterpret_cast<const floatx4_t*>(others + 2 * k * kPiece + at);
+    // in order, four loads under way
+    for (int k0 = 0; k0 < n; k0 += 4) {
+      floatx4_t x[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += x[e];
+      for (int k = 0; k < 4; ++k)
+        x[k] = *reinterpret_cast<const floatx4_t*>(
+            others + 2 * min(k0 + k, n - 1) * kPiece + at);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += k0 + k < n ? x[k][e] : 0.f;
     }
     u16x4_t o;
 #pragma unroll
@@ -995,7 +1015,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(BwdArgs a) {
 
 struct BwdPlan {
   int T, W, group_cost;
-  size_t part, total;
+  size_t cuts, part, total;
   unsigned dq_grid;
 };
 
@@ -1021,7 +1041,8 @@ bool bwd_plan(int n_seq, int L, int block, int Hq, int Hkv, int D,
   p->W = static_cast<int>(std::min<int64_t>(256, std::max<int64_t>(1, all / 16)));
   p->group_cost = static_cast<int>(cost);
   p->dq_grid = static_cast<unsigned>(dq);
-  p->part = up256(static_cast<size_t>(n_seq) * Hq * 2 * p->T * 2 * kRows * 4);
+  p->cuts = up256(static_cast<size_t>(n_seq) * Hq * 2 * p->T * 2 * kRows * 4);
+  p->part = p->cuts + up256((p->W + 1) * sizeof(int4));
   p->total = p->part;
   if (p->W > 1)
     p->total += static_cast<size_t>(p->W) * 2 * 2 * kKeysPerWg * D * 4;
@@ -1062,6 +1083,7 @@ extern "C" int wedlm_dual_stream_attn_backward(
   a.dk = dk;
   a.dv = dv;
   a.ld = reinterpret_cast<float*>(ws);
+  a.cuts = reinterpret_cast<int4*>(ws + p.cuts);
   a.part = reinterpret_cast<float*>(ws + p.part);
   a.n_seq = n_seq;
   a.L = L;
@@ -1082,7 +1104,8 @@ extern "C" int wedlm_dual_stream_attn_backward(
   WEDLM_LAUNCH_CHECK();
   if (p.W > 1) {
     hipLaunchKernelGGL(D == 128 ? join_kernel<128> : join_kernel<64>,
-                       dim3(p.W - 1, 16), dim3(kThreads), 0, st, a);
+                       dim3(p.W - 1, 2 * kKeysPerWg * (D / 4) / kThreads),
+                       dim3(kThreads), 0, st, a);
     WEDLM_LAUNCH_CHECK();
   }
   return WEDLM_OK;
