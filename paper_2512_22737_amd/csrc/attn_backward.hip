@@ -403,6 +403,44 @@ void dq_kernel(BwdArgs a) {
   const int head = kvh * a.G + unit % a.G;
   const int64_t row0 = (static_cast<int64_t>(sq) * 2 + stream) * a.L;
 
+  // tiles: memory keys from 0, then for prediction rows their own blocks'
+  const int first = grp * kWaves / a.G * kOwn;
+  const int end = min(a.L, (min(grp * kWaves + kWaves - 1, last_unit) / a.G +
+                            1) * kOwn);
+  const int n_mem =
+      ((stream ? (end - 1) / a.block * a.block : end) + kRows - 1) / kRows;
+  const int own0 = first / a.block * a.block / kRows;
+  const int n = n_mem + (stream ? (end + kRows - 1) / kRows - own0 : 0);
+  // memory keys that all of the wave's rows see
+  const int full = stream ? p0 / a.block * a.block : p0 + 1;
+  const int64_t kv0 = (static_cast<int64_t>(sq) * 2 * a.L * a.Hkv + kvh) * D;
+  const PairLoader<D> loader(a.k + kv0, a.v + kv0, a.Hkv * D, wave,
+                             lds_address(smem));
+  // the tile that is loaded next
+  int ahead = 0, ahead_p = 0;
+  auto fetch = [&](int u, int slot) {
+    loader.load(u, static_cast<int64_t>(ahead_p) * (a.Hkv * D),
+                a.L - 1 - (ahead >= n_mem ? ahead_p - a.L : ahead_p),
+                slot * kPair);
+  };
+  // past the end: the last tile again, into a slot that nobody reads
+  auto advance = [&]() {
+    ahead = min(ahead + 1, n - 1);
+    ahead_p = ahead >= n_mem ? a.L + (own0 + ahead - n_mem) * kRows
+                             : ahead * kRows;
+  };
+  if (n_mem == 0) ahead_p = a.L + own0 * kRows;
+  const Reader<D> rd;
+  constexpr int kE = 16 / NK;              // elements per step
+  constexpr int kLoads = PairLoader<D>::kCount;
+  bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
+#pragma unroll
+  for (int i = 0; i < kSlots - 1; ++i) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) fetch(u, i);
+    advance();
+  }
+
   bf16x8_t qf[2][NK], dof[2][NK];
   float lse2[2], delta[2];
   int lo[2], hi[2];         // memory: keys below lo; own stream: see own()
@@ -441,43 +479,6 @@ void dq_kernel(BwdArgs a) {
 #pragma unroll
     for (int m = 0; m < NM; ++m) acc[b][m] = floatx16_t{};
 
-  // tiles: memory keys from 0, then for prediction rows their own blocks'
-  const int first = grp * kWaves / a.G * kOwn;
-  const int end = min(a.L, (min(grp * kWaves + kWaves - 1, last_unit) / a.G +
-                            1) * kOwn);
-  const int n_mem =
-      ((stream ? (end - 1) / a.block * a.block : end) + kRows - 1) / kRows;
-  const int own0 = first / a.block * a.block / kRows;
-  const int n = n_mem + (stream ? (end + kRows - 1) / kRows - own0 : 0);
-  // memory keys that all of the wave's rows see
-  const int full = stream ? p0 / a.block * a.block : p0 + 1;
-  const int64_t kv0 = (static_cast<int64_t>(sq) * 2 * a.L * a.Hkv + kvh) * D;
-  const PairLoader<D> loader(a.k + kv0, a.v + kv0, a.Hkv * D, wave,
-                             lds_address(smem));
-  // the tile that is loaded next
-  int ahead = 0, ahead_p = 0;
-  auto fetch = [&](int u, int slot) {
-    loader.load(u, static_cast<int64_t>(ahead_p) * (a.Hkv * D),
-                a.L - 1 - (ahead >= n_mem ? ahead_p - a.L : ahead_p),
-                slot * kPair);
-  };
-  // past the end: the last tile again, into a slot that nobody reads
-  auto advance = [&]() {
-    ahead = min(ahead + 1, n - 1);
-    ahead_p = ahead >= n_mem ? a.L + (own0 + ahead - n_mem) * kRows
-                             : ahead * kRows;
-  };
-  if (n_mem == 0) ahead_p = a.L + own0 * kRows;
-  const Reader<D> rd;
-  constexpr int kE = 16 / NK;              // elements per step
-  constexpr int kLoads = PairLoader<D>::kCount;
-  bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
-#pragma unroll
-  for (int i = 0; i < kSlots - 1; ++i) {
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) fetch(u, i);
-    advance();
-  }
   if (wave == 0) write_cuts(a);
   // take delivery of the rows: no wait for them in the loop
 #pragma unroll
