@@ -271,7 +271,7 @@ __device__ __forceinline__ void drain(floatx16_t (&acc)[2][N]) {
 // of it, which a last kernel adds up in order.
 // ---------------------------------------------------------------------------
 constexpr int kTileCost = 4;     // a tile's fixed work, in items
-constexpr int kSnap = 6;         // items: no cut nearer to a tile's end
+constexpr int kSnap = 3;         // items: no cut nearer to a tile's end
 
 // The key tile at position p of the list.
 struct KeyTile {
@@ -1039,7 +1039,7 @@ bool bwd_plan(int n_seq, int L, int block, int Hq, int Hkv, int D,
   if (dq > 0x7fffffffll || cost > 0x7fffffffll) return false;
   // one workgroup per CU, but none with less than 16 items' work
   const int64_t all = cost * n_seq * Hkv;
-  p->W = static_cast<int>(std::min<int64_t>(256, std::max<int64_t>(1, all / 16)));
+  p->W = static_cast<int>(std::min<int64_t>(256, std::max<int64_t>(1, all / 6)));
   p->group_cost = static_cast<int>(cost);
   p->dq_grid = static_cast<unsigned>(dq);
   p->cuts = up256(static_cast<size_t>(n_seq) * Hq * 2 * p->T * 2 * kRows * 4);
