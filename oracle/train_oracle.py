@@ -164,10 +164,11 @@ def token_loss(logits, target, weight):
     """logits [R, V], target [R], weight [R] -> (loss, dlogits), (their
     bounds).  Rows without loss: target outside the row, or weight 0.
 
-    fp32: an exponent x - m and its product with log2 e are off by 2 F32 of
-    their size, v_exp_f32 by a step, a sum of V terms by V F32 of itself at
-    most (thread sums and trees: V / 64 + 16 is above any split), the
-    logarithm by two steps of its size and the sum's relative error."""
+    fp32: an exponent x - m, log2 e and their product are off by 3 F32 of
+    its size, v_exp_f32 by a step (2 F32); thread sums and trees by V / 64 +
+    16 F32 of the sum of the others at most; logarithms by two steps.  Loss
+    and the target's gradient are made from the sum of the others, so that
+    their errors are relative to it where the target is the largest."""
     R, V = logits.shape
     loss, d = np.zeros(R), np.zeros((R, V))
     bl, bd = np.zeros(R), np.zeros((R, V))
@@ -181,16 +182,27 @@ def token_loss(logits, target, weight):
             continue
         z = logits[r] - m
         e = np.exp(z)
-        s = e.sum()
         a = np.abs(np.where(e > 0, z, 0.0))
-        sum_err = F32 * (V / 64 + 16) + (e * (3 * F32 * a + 2 * F32)).sum() / s
-        loss[r] = w * (np.log(s) - z[t])
-        bl[r] = 1.01 * abs(w) * (sum_err + 3 * F32 * (np.log(s) + 2) + (
-            4 * F32 * abs(z[t]) if z[t] > -np.inf else 0.0))
+        term = 3 * F32 * a + 2 * F32                  # relative, of each e
+        rest = e.copy()
+        rest[t] = 0.0
+        R1, s = rest.sum(), e.sum()
+        # absolute errors of the others' sum and of s; v_exp_f32 flushes
+        # below 2^-126
+        flush = V * 2.0 ** -126
+        e_rest = R1 * F32 * (V / 64 + 16) + (rest * term).sum() + flush
+        e_s = e_rest + e[t] * term[t] + 2 * F32 * s
+        if z[t] == 0:
+            loss[r] = w * np.log1p(R1)
+            bl[r] = abs(w) * (e_rest + 6 * F32 * np.log1p(R1))
+        else:
+            loss[r] = w * (np.log(s) - z[t])
+            bl[r] = abs(w) * (e_s / s + 6 * F32 * np.log(s) + (
+                4 * F32 * abs(z[t]) if z[t] > -np.inf else 0.0))
         p = e / s
         d[r] = w * p
-        d[r, t] -= w
-        # v_exp_f32 flushes below 2^-126
-        bd[r] = abs(w) * (p * (sum_err + 3 * F32 * a + 6 * F32) + 2.0 ** -125)
-        bd[r, t] += 2 * F32 * abs(w)
-    return (loss, d), (bl, 1.01 * bd)
+        d[r, t] = -w * R1 / s
+        bd[r] = abs(w) * (p * (e_s / s + term + 6 * F32) + 2.0 ** -125)
+        bd[r, t] = abs(w) * (R1 / s * (e_s / s + 6 * F32) + e_rest / s +
+                             2.0 ** -125)
+    return (loss, d), (1.01 * bl, 1.01 * bd)

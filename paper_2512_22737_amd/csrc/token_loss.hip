@@ -1,11 +1,14 @@
 // The masked-token loss of the training objective with the gradient of its
-// logits.  Row r with target t and weight w (logits l, m the largest,
-// Z = sum_v e^{l_v - m}):
-//   loss = w (ln Z - (l_t - m))      dl_v = w (e^{l_v - m} / Z - [v = t])
+// logits.  Row r with target t and weight w (logits l, m the largest; R the sum
+// over all others, Z = R + e^{l_t - m}):
+//   loss = w (ln Z + (m - l_t)), ln Z = ln(1 + R) if l_t = m
+//   dl_v = w e^{l_v - m} / Z for v != t,  dl_t = -w R / Z
+// Nothing cancels, so that a token predicted with p_t near 1 keeps the digits
+// of 1 - p_t; the target is kept out of the sum from the start.
 // One workgroup per row.  Every thread keeps the first H 16-byte chunks that
 // it reads in registers: their maximum, then e^{l - m} in their place with
 // the sum, then the gradient, so that these logits are read once and their
-// exponentials taken once.  What does not fit (fp32 rows beyond 81920) is
+// exponentials taken once.  What does not fit (fp32 rows beyond 77824) is
 // reduced with a running maximum and read again for the gradient, while it is
 // in the L2.  Few long rows are split over workgroups: one kernel for the
 // slices' maxima and sums, one that joins them and forms the gradient.
@@ -30,7 +33,7 @@ struct LossArgs {
   const float* weight;    // [R] or null
   float* loss;            // [R]
   void* dlogits;          // [R, stride] or null
-  float2* part;           // [R, slices]: maximum, sum
+  float2* part;           // [R, slices + 1]: maximum, sum; the target's logit
   int64_t stride;
   int R, V, slices, slice_len;
 };
@@ -110,8 +113,31 @@ __device__ __forceinline__ bool no_loss(const LossArgs& a, int r, int& t,
   return t < 0 || t >= a.V || w == 0.f;
 }
 
-__device__ __forceinline__ float row_loss(float w, float m, float s, float lt) {
-  return w * (m == kNegInf ? -kNegInf : logf(s) - (lt - m));
+// What a row's loss and gradient take from its maximum m, the sum of the
+// others r and the target's logit lt.
+struct RowStats {
+  float loss;
+  float ref, k, hit;      // dl_v = e^{l_v - ref} k, dl_t = hit
+  __device__ __forceinline__ RowStats(float w, float m, float r, float lt) {
+    if (m == kNegInf) {   // nothing but -inf: no probabilities, gradient 0
+      loss = w * -kNegInf;
+      ref = k = hit = 0.f;
+      return;
+    }
+    const float z = r + exp_below(lt, m);
+    loss = w * (lt == m ? log1pf(r) : logf(z) + (m - lt));
+    ref = m;
+    k = w / z;
+    hit = -w * (r / z);
+  }
+};
+
+// The chunk without the target (element e of it, if in 0 .. n-1).
+template <typename T>
+__device__ __forceinline__ void drop(typename Elem<T>::chunk& x, int e) {
+#pragma unroll
+  for (int i = 0; i < Elem<T>::n; ++i)
+    if (i == e) Elem<T>::set(x, i, kNegInf);
 }
 
 // Zeros over a stretch of a row of dlogits.
@@ -147,39 +173,54 @@ __global__ __launch_bounds__(NT) void token_loss_kernel(LossArgs a) {
   const int tid = threadIdx.x;
   // the target's logit is read before any gradient is written over it
   const float lt = E::get(row + t);
+  const int tb = t - sp.head;            // the target, from the first chunk
+  const int tc = tb >= 0 ? tb / E::n : -1;
   C held[H];
-  float one = kNegInf, m = kNegInf;
+  float one = kNegInf, m = lt;
 #pragma unroll
   for (int i = 0; i < H; ++i)
     if (tid + i * NT < sp.chunks) held[i] = body[tid + i * NT];
-  if (tid < sp.singles) m = one = E::get(row + sp.single(tid));
+  const bool single = tid < sp.singles && sp.single(tid) != t;
+  if (single) one = E::get(row + sp.single(tid));
+  m = fmaxf(m, one);
 #pragma unroll
   for (int i = 0; i < H; ++i)
     if (tid + i * NT < sp.chunks) {
+      if (tid + i * NT == tc) drop<T>(held[i], tb - tc * E::n);
 #pragma unroll
       for (int e = 0; e < E::n; ++e) m = fmaxf(m, E::get(held[i], e));
     }
+  // the rest, four chunks under way at a time (past the end: the last again)
+  constexpr int U = 4;
   MaxSum rest{kNegInf, 0.f};
-  for (int c = tid + H * NT; c < sp.chunks; c += NT) {
-    const C x = body[c];
-    float cm = E::get(x, 0);
+  for (int c0 = tid + H * NT; c0 < sp.chunks; c0 += U * NT) {
+    C x[U];
 #pragma unroll
-    for (int e = 1; e < E::n; ++e) cm = fmaxf(cm, E::get(x, e));
-    if (cm > rest.m) {
-      rest.s *= exp_below(rest.m, cm);
-      rest.m = cm;
-    }
-    if (rest.m != kNegInf) {
+    for (int u = 0; u < U; ++u) x[u] = body[min(c0 + u * NT, sp.chunks - 1)];
 #pragma unroll
-      for (int e = 0; e < E::n; ++e) rest.s += exp_below(E::get(x, e), rest.m);
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * NT;
+      if (c >= sp.chunks) break;
+      if (c == tc) drop<T>(x[u], tb - tc * E::n);
+      float cm = E::get(x[u], 0);
+#pragma unroll
+      for (int e = 1; e < E::n; ++e) cm = fmaxf(cm, E::get(x[u], e));
+      if (cm > rest.m) {
+        rest.s *= exp_below(rest.m, cm);
+        rest.m = cm;
+      }
+      if (rest.m != kNegInf) {
+#pragma unroll
+        for (int e = 0; e < E::n; ++e)
+          rest.s += exp_below(E::get(x[u], e), rest.m);
+      }
     }
   }
   m = reduce<NT>(fmaxf(m, rest.m), lds[0],
                  [](float x, float y) { return fmaxf(x, y); });
-  // a row of nothing but -inf: no probabilities, gradient 0
   const float ref = m == kNegInf ? 0.f : m;
   float s = rest.m == kNegInf ? 0.f : rest.s * exp_below(rest.m, ref);
-  if (tid < sp.singles) s += exp_below(one, ref);
+  if (single) s += exp_below(one, ref);
 #pragma unroll
   for (int i = 0; i < H; ++i)
     if (tid + i * NT < sp.chunks) {
@@ -189,31 +230,35 @@ __global__ __launch_bounds__(NT) void token_loss_kernel(LossArgs a) {
       s += x;
     }
   s = reduce<NT>(s, lds[1], [](float x, float y) { return x + y; });
-  if (tid == 0) a.loss[r] = row_loss(w, m, s, lt);
+  const RowStats q(w, m, s, lt);
+  if (tid == 0) a.loss[r] = q.loss;
   if (!drow) return;
-  const float k = m == kNegInf ? 0.f : w / s;
-  const float hit = m == kNegInf ? 0.f : w;
   C* dbody = reinterpret_cast<C*>(drow + sp.head);
-  const int tb = t - sp.head;            // the target, from the first chunk
   auto grad = [&](const C& x, int c) {
     C d;
 #pragma unroll
     for (int e = 0; e < E::n; ++e)
-      E::set(d, e, exp_below(E::get(x, e), ref) * k -
-                       (tb == c * E::n + e ? hit : 0.f));
+      E::set(d, e, tb == c * E::n + e ? q.hit
+                                      : exp_below(E::get(x, e), q.ref) * q.k);
     __builtin_nontemporal_store(d, dbody + c);
   };
 #pragma unroll
   for (int i = 0; i < H; ++i)
     if (tid + i * NT < sp.chunks) grad(held[i], tid + i * NT);
-  for (int c = tid + H * NT; c < sp.chunks; c += NT) grad(body[c], c);
-  if (tid < sp.singles) {
-    const int v = sp.single(tid);
-    E::set(drow + v, exp_below(one, ref) * k - (v == t ? hit : 0.f));
+  for (int c0 = tid + H * NT; c0 < sp.chunks; c0 += U * NT) {
+    C x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = body[min(c0 + u * NT, sp.chunks - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c0 + u * NT < sp.chunks) grad(x[u], c0 + u * NT);
   }
+  if (tid < sp.singles)
+    E::set(drow + sp.single(tid),
+           single ? exp_below(one, q.ref) * q.k : q.hit);
 }
 
-// Maximum and sum of one slice.
+// Maximum and sum of one slice, without the target.
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void slice_kernel(LossArgs a) {
   typedef Elem<T> E;
@@ -230,21 +275,25 @@ __global__ __launch_bounds__(kSmallThreads) void slice_kernel(LossArgs a) {
   const C* body = reinterpret_cast<const C*>(p + sp.head);
   const int tid = threadIdx.x;
   C held[kSmallHeld];
+  const int tb = t - v0 - sp.head;
+  const int tc = tb >= 0 ? tb / E::n : -1;
   float one = kNegInf, m = kNegInf, s = 0.f;
 #pragma unroll
   for (int i = 0; i < kSmallHeld; ++i)
     if (tid + i * kSmallThreads < sp.chunks) held[i] = body[tid + i * kSmallThreads];
-  if (tid < sp.singles) m = one = E::get(p + sp.single(tid));
+  const bool single = tid < sp.singles && v0 + sp.single(tid) != t;
+  if (single) m = one = E::get(p + sp.single(tid));
 #pragma unroll
   for (int i = 0; i < kSmallHeld; ++i)
     if (tid + i * kSmallThreads < sp.chunks) {
+      if (tid + i * kSmallThreads == tc) drop<T>(held[i], tb - tc * E::n);
 #pragma unroll
       for (int e = 0; e < E::n; ++e) m = fmaxf(m, E::get(held[i], e));
     }
   m = reduce<kSmallThreads>(m, lds[0],
                             [](float x, float y) { return fmaxf(x, y); });
   const float ref = m == kNegInf ? 0.f : m;
-  if (tid < sp.singles) s += exp_below(one, ref);
+  if (single) s += exp_below(one, ref);
 #pragma unroll
   for (int i = 0; i < kSmallHeld; ++i)
     if (tid + i * kSmallThreads < sp.chunks) {
@@ -254,13 +303,17 @@ __global__ __launch_bounds__(kSmallThreads) void slice_kernel(LossArgs a) {
       s += x;
     }
   s = reduce<kSmallThreads>(s, lds[1], [](float x, float y) { return x + y; });
-  if (tid == 0)
-    a.part[static_cast<int64_t>(r) * a.slices + sl] = make_float2(m, s);
+  if (tid == 0) {
+    float2* part = a.part + static_cast<int64_t>(r) * (a.slices + 1);
+    part[sl] = make_float2(m, s);
+    if (t >= v0 && t < v0 + n)
+      part[a.slices] = make_float2(E::get(p + t - v0), 0.f);
+  }
 }
 
-// Loss (first slice) and gradient of one slice, the slices joined in order.
-// The target's logit comes from the slice that holds it, which alone may
-// write over it: the loss is that slice's.
+// Gradient of one slice, the slices joined in order; the loss too where the
+// slice holds the target.  Every slice needs the target's logit, which
+// slice_kernel has left behind the slices' sums: here it may be overwritten.
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void slice_grad_kernel(LossArgs a) {
   typedef Elem<T> E;
@@ -280,19 +333,14 @@ __global__ __launch_bounds__(kSmallThreads) void slice_grad_kernel(LossArgs a) {
   const int tid = threadIdx.x;
   const bool mine = t >= v0 && t < v0 + n;
   if (!dp && !mine) return;
-  const float lt = mine ? E::get(p + t - v0) : 0.f;
+  const float2* part = a.part + static_cast<int64_t>(r) * (a.slices + 1);
   MaxSum x{kNegInf, 0.f};
-  for (int i = 0; i < a.slices; ++i) {
-    const float2 v = a.part[static_cast<int64_t>(r) * a.slices + i];
-    x = merge(x, MaxSum{v.x, v.y});
-  }
-  if (mine && tid == 0) a.loss[r] = row_loss(w, x.m, x.s, lt);
+  for (int i = 0; i < a.slices; ++i) x = merge(x, MaxSum{part[i].x, part[i].y});
+  const float lt = part[a.slices].x;
+  const float m = fmaxf(x.m, lt);
+  const RowStats q(w, m, x.m == kNegInf ? 0.f : x.s * exp_below(x.m, m), lt);
+  if (mine && tid == 0) a.loss[r] = q.loss;
   if (!dp) return;
-  // every thread has the target's logit before its gradient is written
-  __syncthreads();
-  const float ref = x.m == kNegInf ? 0.f : x.m;
-  const float k = x.m == kNegInf ? 0.f : w / x.s;
-  const float hit = x.m == kNegInf ? 0.f : w;
   const Span<T> sp(p, n);
   const C* body = reinterpret_cast<const C*>(p + sp.head);
   C* dbody = reinterpret_cast<C*>(dp + sp.head);
@@ -303,14 +351,14 @@ __global__ __launch_bounds__(kSmallThreads) void slice_grad_kernel(LossArgs a) {
     C d;
 #pragma unroll
     for (int e = 0; e < E::n; ++e)
-      E::set(d, e, exp_below(E::get(l, e), ref) * k -
-                       (tb == c * E::n + e ? hit : 0.f));
+      E::set(d, e, tb == c * E::n + e ? q.hit
+                                      : exp_below(E::get(l, e), q.ref) * q.k);
     dbody[c] = d;
   }
   if (tid < sp.singles) {
     const int v = sp.single(tid);
-    E::set(dp + v, exp_below(E::get(p + v), ref) * k -
-                       (v + v0 == t ? hit : 0.f));
+    E::set(dp + v, v + v0 == t ? q.hit
+                               : exp_below(E::get(p + v), q.ref) * q.k);
   }
 }
 
@@ -335,7 +383,7 @@ __global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
   const float lt = E::get(row + t);
   MaxSum x{kNegInf, 0.f};
   for (int v = tid; v < a.V; v += kSmallThreads) {
-    const float l = E::get(row + v);
+    const float l = v == t ? kNegInf : E::get(row + v);
     if (l > x.m) {
       x.s *= exp_below(x.m, l);
       x.m = l;
@@ -343,16 +391,15 @@ __global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
     if (x.m != kNegInf) x.s += exp_below(l, x.m);
   }
   const float m = reduce<kSmallThreads>(
-      x.m, lds[0], [](float y, float z) { return fmaxf(y, z); });
-  const float ref = m == kNegInf ? 0.f : m;
+      fmaxf(x.m, lt), lds[0], [](float y, float z) { return fmaxf(y, z); });
   const float s = reduce<kSmallThreads>(
-      x.m == kNegInf ? 0.f : x.s * exp_below(x.m, ref), lds[1],
+      x.m == kNegInf ? 0.f : x.s * exp_below(x.m, m), lds[1],
       [](float y, float z) { return y + z; });
-  if (tid == 0) a.loss[r] = row_loss(w, m, s, lt);
-  const float k = m == kNegInf ? 0.f : w / s;
+  const RowStats q(w, m, s, lt);
+  if (tid == 0) a.loss[r] = q.loss;
   for (int v = tid; v < a.V; v += kSmallThreads)
-    E::set(drow + v, exp_below(E::get(row + v), ref) * k -
-                         (v == t && m != kNegInf ? w : 0.f));
+    E::set(drow + v,
+           v == t ? q.hit : exp_below(E::get(row + v), q.ref) * q.k);
 }
 
 // Elements of a row's slices, or V (one slice): rows beyond one small
@@ -401,7 +448,7 @@ int launch(const LossArgs& a0, hipStream_t st) {
     hipLaunchKernelGGL((token_loss_kernel<T, kSmallThreads, kSmallHeld>),
                        dim3(a.R), dim3(kSmallThreads), 0, st, a);
   else
-    hipLaunchKernelGGL((token_loss_kernel<T, 1024, 20>), dim3(a.R), dim3(1024),
+    hipLaunchKernelGGL((token_loss_kernel<T, 1024, 19>), dim3(a.R), dim3(1024),
                        0, st, a);
   WEDLM_LAUNCH_CHECK();
   return WEDLM_OK;
@@ -413,7 +460,7 @@ extern "C" size_t wedlm_token_loss_workspace_size(int32_t R, int32_t V) {
   if (R < 1 || V < 1) return 0;
   const int n = std::max(row_slices(R, V, Elem<float>::n),
                          row_slices(R, V, Elem<uint16_t>::n));
-  return n > 1 ? static_cast<size_t>(R) * n * sizeof(float2) : 0;
+  return n > 1 ? static_cast<size_t>(R) * (n + 1) * sizeof(float2) : 0;
 }
 
 extern "C" int wedlm_token_loss(const void* logits, int32_t logits_type,

@@ -117,3 +117,27 @@ def test_default_weight_and_unaligned_arrays():
             wedlm.wedlm_token_loss(xv, t, loss, None, dv)
             _check(x, t, None, V, loss, dv, dtype)
             assert (ds[:b] == 5).all() and (ds[b + R * V:] == 5).all()
+
+
+# (the rows' sum of the others from about e^-7 down to 0 beside the target's 1;
+# V in one workgroup's registers, beyond them, and in slices)
+@pytest.mark.parametrize("R,V", [(12, 200), (12, 30000), (300, 100000)])
+def test_well_predicted_tokens_keep_their_digits(R, V):
+    """Loss and gradients of targets that stand 8 to 120 above the others:
+    relative to themselves, not to 1."""
+    from paper_2512_22737_amd import wedlm
+    rng = np.random.default_rng(V)
+    x = 0.1 * rng.standard_normal((R, V))
+    t = rng.integers(0, V, R).astype(np.int32)
+    x[np.arange(R), t] = np.linspace(np.log(V) + 8, 120, R)
+    x = torch.from_numpy(x).cuda().float()
+    t = torch.from_numpy(t).cuda()
+    for a in (0, 1):                   # logits and gradients alike, and not
+        loss = torch.empty(R, device="cuda")
+        d = torch.empty(R * V + 4, device="cuda")[a:a + R * V].view(R, V)
+        wedlm.wedlm_token_loss(x, t, loss, None, d)
+        _check(x, t, None, V, loss, d, torch.float32)
+        # not rounded away until e^-x is below 2^-126 (x = 87.3; the others
+        # are within 1 of 0)
+        near = x.gather(1, t[:, None].long())[:, 0] < 86
+        assert near.sum() > R // 2 and (loss[near] > 0).all()
