@@ -491,7 +491,8 @@ void dq_kernel(BwdArgs a) {
 #pragma unroll
   for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem, kk);
   int slot = 0, next_slot = 1, load_slot = kSlots - 1;
-  for (int i = 0; i < n; ++i) {
+  int i = 0;               // (n > 0: a loop that runs at least once)
+  do {
     // this wave's loads of tile i + 1, then everybody's; the barrier also
     // frees the slot of tile i - 1
     wait_vmcnt<(kSlots - 3) * kLoads>();
@@ -583,7 +584,7 @@ void dq_kernel(BwdArgs a) {
     load_slot = slot;
     slot = next_slot;
     next_slot = next_slot == kSlots - 1 ? 0 : next_slot + 1;
-  }
+  } while (++i < n);
   wait_vmcnt<0>();      // surplus loads land before the LDS is given up
   drain(acc);
   if (!live) return;
@@ -780,7 +781,8 @@ void dkv_kernel(BwdArgs a) {
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem, kk);
   }
-  for (int it = it0; it < it1; ++it) {
+  int it = it0;            // (it0 < it1)
+  do {
     if (stream) {
       // this wave's tile; the other slot is free
       wait_vmcnt<0>();
@@ -922,7 +924,7 @@ void dkv_kernel(BwdArgs a) {
       slot = next_slot;
       next_slot = next_slot == kSlots - 1 ? 0 : next_slot + 1;
     }
-  }
+  } while (++it < it1);
   wait_vmcnt<0>();      // surplus loads land before the LDS is given up
   drain(dv);
   drain(dk);
