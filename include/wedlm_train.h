@@ -78,10 +78,12 @@ size_t wedlm_dual_stream_attn_backward_workspace_size(int32_t n_seq, int32_t L,
  * Products take bf16 operands (the probabilities and the scores' gradients
  * are rounded to it) with fp32 sums, in an order that the sizes fix: the
  * result does not depend on the run.
- * Limits: those of the forward.
- * workspace: wedlm_dual_stream_attn_backward_workspace_size() bytes, 256-byte
- * aligned (each row's normaliser and output product; fp32 partial sums where
- * few key tiles are split); its contents on entry do not matter.  Two calls
+ * Limits: those of the forward, Hq * D < 2^25 and
+ * ceil(L / 32) * Hq/Hkv < 2^29.  bf16 arrays and the workspace on 16-byte
+ * boundaries (WEDLM_E_ARG).
+ * workspace: wedlm_dual_stream_attn_backward_workspace_size() bytes (each
+ * row's normaliser and product of out and dout; fp32 sums of keys whose work
+ * is split over workgroups); its contents on entry do not matter.  Two calls
  * that overlap in time must not share a workspace.
  */
 int wedlm_dual_stream_attn_backward(
@@ -109,10 +111,9 @@ size_t wedlm_rmsnorm_backward_workspace_size(int32_t M, int32_t Hd);
  *   dx [M, Hd] fp32 (may be dres itself: the gradient is then added in
  *   place), dgain [Hd] fp32 or NULL (a frozen gain); both overwritten.
  *   Otherwise they must not overlap the inputs or each other.
- * Hd a multiple of 4; x, dres and dx on 16-byte boundaries, gain and dy on
- * 8-byte ones.
- * workspace: wedlm_rmsnorm_backward_workspace_size() bytes, 16-byte aligned
- * (partial sums of dgain; none needed without it); its contents on entry do
+ * Hd a multiple of 4; x, dres, dx and the workspace on 16-byte boundaries,
+ * gain and dy on 8-byte ones (WEDLM_E_ARG).
+ * workspace: wedlm_rmsnorm_backward_workspace_size() bytes (partial sums of dgain; none needed without it); its contents on entry do
  * not matter.  The sums' order is fixed by the sizes.  Two calls that overlap
  * in time must not share a workspace.
  */
@@ -139,7 +140,7 @@ size_t wedlm_qk_norm_rope_backward_workspace_size(int32_t M, int32_t Hq,
  * Out:
  *   dqkv [M, (Hq + 2 Hkv) D] bf16; dq_gain, dk_gain [D] fp32, each NULL if
  *   not wanted; all overwritten, no overlap with the inputs or each other.
- * D 64 or 128; bf16 arrays on 16-byte boundaries.
+ * D 64 or 128; bf16 arrays on 16-byte boundaries (WEDLM_E_ARG).
  * workspace: wedlm_qk_norm_rope_backward_workspace_size() bytes (partial sums
  * of the gains' gradients; none needed without them); its contents on entry
  * do not matter.  The sums' order is fixed by the sizes.  Two calls that

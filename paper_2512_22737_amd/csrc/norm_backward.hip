@@ -5,7 +5,9 @@
 //   dx = r (u - x r mean(u x r))  [+ the gradient that came past the norm]
 // Per-head q/k norm with RoPE: the gradient is first rotated back (by minus
 // the row's angles), then each head is such a norm over its D values.
+#include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "common.h"
 #include "wedlm_train.h"
@@ -15,8 +17,7 @@ using namespace wedlm;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kParts = 1024;      // partial gain gradients of a call, at most
-constexpr int kQkParts = 2048;
+constexpr int kQkParts = 2048;    // workgroups of the q/k kernel, at most
 
 // Sum over the wave.
 __device__ __forceinline__ float wave_sum(float v) {
@@ -331,11 +332,23 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(
   }
 }
 
-int norm_parts(int M) { return M < kParts ? M : kParts; }
+bool aligned(std::initializer_list<const void*> ps, int bytes) {
+  for (const void* p : ps)
+    if (reinterpret_cast<uintptr_t>(p) % bytes != 0) return false;
+  return true;
+}
 
-// rows that a workgroup of the q/k kernel takes at once, and workgroups
+// Workgroups of the RMSNorm kernel, each with its part of the gain's gradient:
+// four per CU for rows of up to 4096 (32768 x 4096 346 us; 512 workgroups 416,
+// 2048 370), two for longer ones, whose registers hold no more (4096 x 8192
+// 111 us; 1024 workgroups 119).
+int norm_parts(int M, int Hd) { return std::min(M, Hd > 4096 ? 512 : 1024); }
+
+// Rows that a workgroup of the q/k kernel takes at once: four where that
+// leaves a workgroup per CU (1024 rows of 32/8 heads of 128 24 us with one,
+// 19 with four; 512 rows 14.4, 17.0; 32768 rows 304, 236).
 constexpr int kQkRows = 4;
-int qk_rows(int M) { return M >= 2 * kQkRows * 256 ? kQkRows : 1; }
+int qk_rows(int M) { return M >= kQkRows * 256 ? kQkRows : 1; }
 int qk_parts(int M) {
   const int groups = (M - 1) / qk_rows(M) + 1;
   return groups < kQkParts ? groups : kQkParts;
@@ -358,7 +371,7 @@ bool qk_ok(int M, int Hq, int Hkv, int D) {
 
 extern "C" size_t wedlm_rmsnorm_backward_workspace_size(int32_t M, int32_t Hd) {
   if (M < 1 || Hd < 4 || Hd % 4 != 0) return 0;
-  return static_cast<size_t>(norm_parts(M)) * Hd * sizeof(float);
+  return static_cast<size_t>(norm_parts(M, Hd)) * Hd * sizeof(float);
 }
 
 extern "C" int wedlm_rmsnorm_backward(const float* x, const uint16_t* gain,
@@ -367,13 +380,15 @@ extern "C" int wedlm_rmsnorm_backward(const float* x, const uint16_t* gain,
                                       float* dx, float* dgain, void* workspace,
                                       size_t workspace_bytes, void* stream) {
   if (!x || !gain || !dy || !dx || !(eps > 0.f)) return WEDLM_E_ARG;
+  if (!aligned({x, dres, dx, workspace}, 16) || !aligned({gain, dy}, 8))
+    return WEDLM_E_ARG;
   if (M < 1 || Hd < 4 || Hd % 4 != 0) return WEDLM_E_SHAPE;
   if (dgain && (!workspace ||
                 workspace_bytes < wedlm_rmsnorm_backward_workspace_size(M, Hd)))
     return WEDLM_E_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   float* part = dgain ? static_cast<float*>(workspace) : nullptr;
-  const int parts = norm_parts(M), nc = Hd / 4;
+  const int parts = norm_parts(M, Hd), nc = Hd / 4;
   auto k = nc <= kThreads        ? rmsnorm_backward_kernel<1>
            : nc <= 2 * kThreads  ? rmsnorm_backward_kernel<2>
            : nc <= 3 * kThreads  ? rmsnorm_backward_kernel<3>
@@ -404,6 +419,7 @@ extern "C" int wedlm_qk_norm_rope_backward(
   if (!qkv || !q_gain || !k_gain || !pos_ids || !dq || !dk || !dv || !dqkv)
     return WEDLM_E_ARG;
   if (!(rope_theta > 1.0) || !(eps > 0.f)) return WEDLM_E_ARG;
+  if (!aligned({qkv, q_gain, k_gain, dq, dk, dv, dqkv}, 16)) return WEDLM_E_ARG;
   if (!qk_ok(M, Hq, Hkv, D)) return WEDLM_E_SHAPE;
   const bool gains = dq_gain || dk_gain;
   if (gains && (!workspace ||

@@ -334,8 +334,13 @@ __global__ __launch_bounds__(kSmallThreads) void slice_grad_kernel(LossArgs a) {
   const bool mine = t >= v0 && t < v0 + n;
   if (!dp && !mine) return;
   const float2* part = a.part + static_cast<int64_t>(r) * (a.slices + 1);
+  // merge() is commutative to the bit: every lane ends with the same value
   MaxSum x{kNegInf, 0.f};
-  for (int i = 0; i < a.slices; ++i) x = merge(x, MaxSum{part[i].x, part[i].y});
+  for (int i = lane_id(); i < a.slices; i += kWave)
+    x = merge(x, MaxSum{part[i].x, part[i].y});
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1)
+    x = merge(x, MaxSum{__shfl_xor(x.m, off), __shfl_xor(x.s, off)});
   const float lt = part[a.slices].x;
   const float m = fmaxf(x.m, lt);
   const RowStats q(w, m, x.m == kNegInf ? 0.f : x.s * exp_below(x.m, m), lt);
@@ -402,14 +407,16 @@ __global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
            v == t ? q.hit : exp_below(E::get(row + v), q.ref) * q.k);
 }
 
-// Elements of a row's slices, or V (one slice): rows beyond one small
-// workgroup's registers that are too few to give every CU one are cut so that
-// there are about 512 workgroups.
+// Elements of a row's slices, or V (one slice).  Rows of more than 16384 chunks
+// (262144 bytes) are cut when they are fewer than 128, so that there are about
+// 512 workgroups, of 1024 chunks each at least.  In us, whole rows and slices:
+// 8 x 151936 fp32 22.9, 9.7, bf16 27.4, 9.9; 64 x 151936 25.4, 22.6 and 27.8,
+// 18.0; 200 x 151936 51.6, 59 and 34.8, 36.6; 64 x 32000 fp32 8.8, 10.4.
 int slice_len(int R, int V, int per_chunk) {
   const int64_t chunks = V / per_chunk;
-  if (R >= 256 || chunks <= kSmallChunks) return V;
+  if (R >= 128 || chunks <= 4 * kSmallChunks) return V;
   int64_t c = (chunks * R / 512 + kSmallThreads - 1) / kSmallThreads;
-  c = c < 1 ? 1 : c > kSmallHeld ? kSmallHeld : c;
+  c = c < 4 ? 4 : c > kSmallHeld ? kSmallHeld : c;
   return static_cast<int>(c) * kSmallThreads * per_chunk;
 }
 
@@ -440,11 +447,15 @@ int launch(const LossArgs& a0, hipStream_t st) {
     WEDLM_LAUNCH_CHECK();
     return WEDLM_OK;
   }
+  // 256 threads as long as they hold the row: 1000 x 8000 fp32 10.3 us against
+  // 20.8 with 1024; four chunks each where those do (4000 x 1000 9.6, 15.3).
+  // Few rows of more than that have CUs to spare: 64 x 32000 bf16 13.5 with
+  // 256, 9.6 with 1024
   const int chunks = a.V / Elem<T>::n;
   if (chunks <= kSmallThreads * 4)
     hipLaunchKernelGGL((token_loss_kernel<T, kSmallThreads, 4>), dim3(a.R),
                        dim3(kSmallThreads), 0, st, a);
-  else if (chunks <= kSmallChunks)
+  else if (chunks <= kSmallChunks && a.R >= 128)
     hipLaunchKernelGGL((token_loss_kernel<T, kSmallThreads, kSmallHeld>),
                        dim3(a.R), dim3(kSmallThreads), 0, st, a);
   else

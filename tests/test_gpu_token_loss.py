@@ -121,7 +121,8 @@ def test_default_weight_and_unaligned_arrays():
 
 # (the rows' sum of the others from about e^-7 down to 0 beside the target's 1;
 # V in one workgroup's registers, beyond them, and in slices)
-@pytest.mark.parametrize("R,V", [(12, 200), (12, 30000), (300, 100000)])
+@pytest.mark.parametrize("R,V", [(12, 200), (12, 30000), (12, 100000),
+                                 (300, 100000)])
 def test_well_predicted_tokens_keep_their_digits(R, V):
     """Loss and gradients of targets that stand 8 to 120 above the others:
     relative to themselves, not to 1."""

@@ -49,6 +49,15 @@ def test_attention_backward_refusals():
              [(12, 0.0, -1), (12, float("nan"), -1), (12, float("inf"), -1),
               (7, 120, -2), (8, 33, -2), (9, 3, -2), (11, 32, -2),
               (16, None, -3), (17, need - 1, -3)])
+    odd = ctypes.c_void_p(0x1008)
+    refusals(lib.wedlm_dual_stream_attn_backward, args,
+             [(i, odd, -1) for i in (0, 1, 2, 3, 5, 13, 14, 15, 16)])
+
+
+def test_attention_backward_refuses_what_its_offsets_cannot_hold():
+    ws = _lib().wedlm_dual_stream_attn_backward_workspace_size
+    assert ws(1, 16, 16, 1 << 18, 1 << 18, 128) == 0
+    assert ws(1, 1 << 20, 64, 1 << 16, 1, 64) == 0
 
 
 def test_rmsnorm_backward_refusals():
@@ -61,7 +70,9 @@ def test_rmsnorm_backward_refusals():
     refusals(lib.wedlm_rmsnorm_backward, args,
              [(i, None, -1) for i in (0, 1, 2, 7)] +
              [(6, 0.0, -1), (6, float("nan"), -1), (4, 0, -2), (5, 2, -2),
-              (5, 66, -2), (9, None, -3), (10, need - 1, -3)])
+              (5, 66, -2), (9, None, -3), (10, need - 1, -3)] +
+             [(i, ctypes.c_void_p(0x1008), -1) for i in (0, 3, 7, 9)] +
+             [(i, ctypes.c_void_p(0x1004), -1) for i in (1, 2)])
 
 
 def test_qk_norm_rope_backward_refusals():
@@ -74,7 +85,8 @@ def test_qk_norm_rope_backward_refusals():
     refusals(lib.wedlm_qk_norm_rope_backward, args,
              [(i, None, -1) for i in (0, 1, 2, 3, 4, 5, 6, 13)] +
              [(11, 1.0, -1), (12, 0.0, -1), (7, 0, -2), (8, 0, -2),
-              (9, -1, -2), (10, 32, -2), (16, None, -3), (17, need - 1, -3)])
+              (9, -1, -2), (10, 32, -2), (16, None, -3), (17, need - 1, -3)] +
+             [(i, ctypes.c_void_p(0x1008), -1) for i in (0, 1, 2, 4, 5, 6, 13)])
 
 
 def test_token_loss_refusals():
