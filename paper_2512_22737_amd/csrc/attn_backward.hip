@@ -46,6 +46,7 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKeysPerWg = kWaves * kOwn;
 constexpr int kSlots = 6;             // ring of tile pairs, five ahead
+constexpr int kRing = kSlots;
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -253,11 +254,11 @@ __device__ __forceinline__ int lane_here() {
 __device__ __forceinline__ void step() { __builtin_amdgcn_sched_barrier(0); }
 
 // The accumulators of the last mfma_acc() are written (18 wait states).
-template <int N>
-__device__ __forceinline__ void drain(floatx16_t (&acc)[2][N]) {
+template <int B, int N>
+__device__ __forceinline__ void drain(floatx16_t (&acc)[B][N]) {
   asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc[0][0]));
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int b = 0; b < B; ++b)
 #pragma unroll
     for (int m = 0; m < N; ++m) asm volatile("" : "+a"(acc[b][m]));
 }
@@ -376,13 +377,15 @@ __device__ __forceinline__ Cut read_cut(const BwdArgs& a, int w) {
           __builtin_amdgcn_readfirstlane(c.z)};
 }
 
-// dq: workgroup = four units (64-position chunk, head) of one stream and kv
-// head, one per wave; the longest first.
-template <int D>
+// dq: workgroup = four units (chunk of 32 QB positions, head) of one stream
+// and kv head, one per wave; the longest first.
+template <int D, int QB>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(1)))
+__attribute__((amdgpu_waves_per_eu(QB == 2 ? 1 : 2)))
 void dq_kernel(BwdArgs a) {
   constexpr int NK = D / 16, NM = D / 32;
+  constexpr int kOwn = 32 * QB;        // rows of a wave
+  constexpr int kSlots = QB == 2 ? kRing : 4;
   using T = RowTile<D>;
   constexpr int kPair = 2 * T::bytes;
   __shared__ __attribute__((aligned(1024))) char smem[kSlots * kPair];
@@ -442,11 +445,11 @@ void dq_kernel(BwdArgs a) {
     advance();
   }
 
-  bf16x8_t qf[2][NK], dof[2][NK];
-  float lse2[2], delta[2];
-  int lo[2], hi[2];         // memory: keys below lo; own stream: see own()
+  bf16x8_t qf[QB][NK], dof[QB][NK];
+  float lse2[QB], delta[QB];
+  int lo[QB], hi[QB];         // memory: keys below lo; own stream: see own()
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < QB; ++b) {
     const int p = p0 + 32 * b + col;
     const int pc = min(p, a.L - 1);
     const int64_t o = ((row0 + pc) * a.Hq + head) * D;
@@ -474,16 +477,16 @@ void dq_kernel(BwdArgs a) {
     lo[b] = stream ? pc / a.block * a.block : 0;
     hi[b] = pc + 1;
   }
-  floatx16_t acc[2][NM];
+  floatx16_t acc[QB][NM];
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int b = 0; b < QB; ++b)
 #pragma unroll
     for (int m = 0; m < NM; ++m) acc[b][m] = floatx16_t{};
 
   if (wave == 0) write_cuts(a);
   // take delivery of the rows: no wait for them in the loop
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int b = 0; b < QB; ++b)
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
       asm volatile("" : "+v"(qf[b][kk]), "+v"(dof[b][kk]));
@@ -505,9 +508,9 @@ void dq_kernel(BwdArgs a) {
     const bool own = i >= n_mem;
     const int j0 = (own ? own0 + i - n_mem : i) * kRows;
     const bool mask = own || j0 + kRows > full;
-    floatx16_t s[2], dp[2];
-    float p[2][16];
-    bf16x8_t ds[2][2];
+    floatx16_t s[QB], dp[QB];
+    float p[QB][16];
+    bf16x8_t ds[QB][2];
     auto hide = [&](int b) {
       const int k0 = j0 + 8 * (lane_here() >> 5);
       const int from = own ? lo[b] : 0, to = own || !stream ? hi[b] : lo[b];
@@ -529,57 +532,89 @@ void dq_kernel(BwdArgs a) {
         ds[b][e >> 3][e & 7] =
             static_cast<__bf16>(p[b][e] * (dp[b][e] - delta[b]));
     };
-    // Six phases of NK = 2 NM MFMAs: S, dP, dq for either group of rows.  The
-    // vector work on a product starts a step after its last MFMA
-    step();
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      s[0] = mfma(f[kk], qf[0][kk], kk ? s[0] : floatx16_t{});
-      if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
+    if constexpr (QB == 1) {
+      // One group: three phases, S, dP, dq.  (Two workgroups share a CU: the
+      // vector work of one runs under the other's products)
       step();
-    }
-    if (mask) hide(0);
-    step();
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      s[1] = mfma(f[kk], qf[1][kk], kk ? s[1] : floatx16_t{});
-      f[kk] = rd.rows(vt, kk);
-      if (kk >= 1) weigh(0, kk - 1);
+      for (int kk = 0; kk < NK; ++kk) {
+        s[0] = mfma(f[kk], qf[0][kk], kk ? s[0] : floatx16_t{});
+        f[kk] = rd.rows(vt, kk);
+        if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
+        step();
+      }
+      if (mask) hide(0);
       step();
-    }
-    if (mask) hide(1);
-    step();
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      dp[0] = mfma(f[kk], dof[0][kk], kk ? dp[0] : floatx16_t{});
-      weigh(kk ? 1 : 0, kk ? kk - 1 : NK - 1);
-      step();
-    }
+      for (int kk = 0; kk < NK; ++kk) {
+        dp[0] = mfma(f[kk], dof[0][kk], kk ? dp[0] : floatx16_t{});
+        f[kk] = rd.cols(kt, kk / NM, kk % NM);
+        weigh(0, kk);
+        step();
+      }
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      dp[1] = mfma(f[kk], dof[1][kk], kk ? dp[1] : floatx16_t{});
-      f[kk] = rd.cols(kt, kk / NM, kk % NM);
-      if (kk)
-        grad(0, kk - 1);
-      else
-        weigh(1, NK - 1);
-      step();
-    }
+      for (int kk = 0; kk < NK; ++kk) grad(0, kk);
+      const char* nt = smem + next_slot * kPair;
 #pragma unroll
-    for (int x = 0; x < NK; ++x) {
-      if (x % NM == 0) settle(ds[0][x / NM]);
-      mfma_acc(acc[0][x % NM], f[x], ds[0][x / NM]);
-      grad(x ? 1 : 0, x ? x - 1 : NK - 1);
+      for (int x = 0; x < NK; ++x) {
+        if (x % NM == 0) settle(ds[0][x / NM]);
+        mfma_acc(acc[0][x % NM], f[x], ds[0][x / NM]);
+        f[x] = rd.rows(nt, x);
+        step();
+      }
+    } else {
+      // Six phases of NK = 2 NM MFMAs: S, dP, dq for either group of rows.  The
+      // vector work on a product starts a step after its last MFMA
       step();
-    }
-    const char* nt = smem + next_slot * kPair;
 #pragma unroll
-    for (int x = 0; x < NK; ++x) {
-      if (x % NM == 0) settle(ds[1][x / NM]);
-      mfma_acc(acc[1][x % NM], f[x], ds[1][x / NM]);
-      f[x] = rd.rows(nt, x);
-      if (x == 0) grad(1, NK - 1);
+      for (int kk = 0; kk < NK; ++kk) {
+        s[0] = mfma(f[kk], qf[0][kk], kk ? s[0] : floatx16_t{});
+        if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
+        step();
+      }
+      if (mask) hide(0);
       step();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        s[1] = mfma(f[kk], qf[1][kk], kk ? s[1] : floatx16_t{});
+        f[kk] = rd.rows(vt, kk);
+        if (kk >= 1) weigh(0, kk - 1);
+        step();
+      }
+      if (mask) hide(1);
+      step();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        dp[0] = mfma(f[kk], dof[0][kk], kk ? dp[0] : floatx16_t{});
+        weigh(kk ? 1 : 0, kk ? kk - 1 : NK - 1);
+        step();
+      }
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        dp[1] = mfma(f[kk], dof[1][kk], kk ? dp[1] : floatx16_t{});
+        f[kk] = rd.cols(kt, kk / NM, kk % NM);
+        if (kk)
+          grad(0, kk - 1);
+        else
+          weigh(1, NK - 1);
+        step();
+      }
+#pragma unroll
+      for (int x = 0; x < NK; ++x) {
+        if (x % NM == 0) settle(ds[0][x / NM]);
+        mfma_acc(acc[0][x % NM], f[x], ds[0][x / NM]);
+        grad(x ? 1 : 0, x ? x - 1 : NK - 1);
+        step();
+      }
+      const char* nt = smem + next_slot * kPair;
+#pragma unroll
+      for (int x = 0; x < NK; ++x) {
+        if (x % NM == 0) settle(ds[1][x / NM]);
+        mfma_acc(acc[1][x % NM], f[x], ds[1][x / NM]);
+        f[x] = rd.rows(nt, x);
+        if (x == 0) grad(1, NK - 1);
+        step();
+      }
     }
     advance();
     load_slot = slot;
@@ -590,7 +625,7 @@ void dq_kernel(BwdArgs a) {
   drain(acc);
   if (!live) return;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < QB; ++b) {
     const int p = p0 + 32 * b + col;
     if (p >= a.L) continue;
     uint16_t* o = a.dq + ((row0 + p) * a.Hq + head) * D;
@@ -1021,6 +1056,7 @@ struct BwdPlan {
   int T, W, group_cost;
   size_t cuts, part, total;
   unsigned dq_grid;
+  int qb;                 // 32-row groups of a dq wave
 };
 
 size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
@@ -1036,8 +1072,12 @@ bool bwd_plan(int n_seq, int L, int block, int Hq, int Hkv, int D,
   if (static_cast<int64_t>(Hq) * D * 2 * kRows > 0x7fffffffll ||
       2ll * p->T * G > 0x3fffffffll)
     return false;
-  const int64_t chunks = (L + kOwn - 1) / kOwn;
-  const int64_t dq = 2 * n_seq * ((chunks * G + kWaves - 1) / kWaves) * Hkv;
+  auto dq_groups = [&](int own) {
+    const int64_t chunks = (L + own - 1) / own;
+    return 2ll * n_seq * ((chunks * G + kWaves - 1) / kWaves) * Hkv;
+  };
+  p->qb = dq_groups(64) < 512 ? 1 : 2;
+  const int64_t dq = dq_groups(32 * p->qb);
   int64_t cost = 0;
   for (int i = 0; i < key_list(L); ++i) {
     const int items = key_tile(L, block, G, i).items;
@@ -1111,8 +1151,9 @@ extern "C" int wedlm_dual_stream_attn_backward(
   a.group_cost = p.group_cost;
   a.scale = softmax_scale;
   a.scale_log2 = softmax_scale * kLog2e;
-  hipLaunchKernelGGL(D == 128 ? dq_kernel<128> : dq_kernel<64>,
-                     dim3(p.dq_grid), dim3(kThreads), 0, st, a);
+  auto dq_k = D == 128 ? (p.qb == 2 ? dq_kernel<128, 2> : dq_kernel<128, 1>)
+                       : (p.qb == 2 ? dq_kernel<64, 2> : dq_kernel<64, 1>);
+  hipLaunchKernelGGL(dq_k, dim3(p.dq_grid), dim3(kThreads), 0, st, a);
   WEDLM_LAUNCH_CHECK();
   hipLaunchKernelGGL(D == 128 ? dkv_kernel<128> : dkv_kernel<64>,
                      dim3(p.W), dim3(kThreads), 0, st, a);
