@@ -41,12 +41,11 @@ using namespace wedlm;
 namespace {
 
 constexpr int kRows = 32;             // streamed rows of an LDS tile
-constexpr int kOwn = 64;              // rows or keys that a wave owns
+constexpr int kOwn = 64;              // keys that a wave owns
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKeysPerWg = kWaves * kOwn;
-constexpr int kSlots = 6;             // ring of tile pairs, five ahead
-constexpr int kRing = kSlots;
+constexpr int kSlots = 6;             // dk, dv: ring of tile pairs
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -254,13 +253,11 @@ __device__ __forceinline__ int lane_here() {
 __device__ __forceinline__ void step() { __builtin_amdgcn_sched_barrier(0); }
 
 // The accumulators of the last mfma_acc() are written (18 wait states).
-template <int B, int N>
-__device__ __forceinline__ void drain(floatx16_t (&acc)[B][N]) {
-  asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc[0][0]));
+template <int N>
+__device__ __forceinline__ void drain(floatx16_t (&acc)[N]) {
+  asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc[0]));
 #pragma unroll
-  for (int b = 0; b < B; ++b)
-#pragma unroll
-    for (int m = 0; m < N; ++m) asm volatile("" : "+a"(acc[b][m]));
+  for (int m = 1; m < N; ++m) asm volatile("" : "+a"(acc[m]));
 }
 
 // ---------------------------------------------------------------------------
@@ -377,20 +374,24 @@ __device__ __forceinline__ Cut read_cut(const BwdArgs& a, int w) {
           __builtin_amdgcn_readfirstlane(c.z)};
 }
 
-// dq: workgroup = four units (chunk of 32 QB positions, head) of one stream
-// and kv head, one per wave; the longest first.
-template <int D, int QB>
+// dq: workgroup = four units (chunk of 32 positions, head) of one stream and
+// kv head, one per wave; the longest first.  Registers and a ring of four
+// tiles let two workgroups share a CU (D = 64: three), so that the vector work
+// of one runs under the products of the other.  With 64 rows a wave, half the
+// LDS reads per product but one workgroup per CU: 4 x 4096 tokens (32/8 heads
+// of 128) 1.53 ms against 1.47, 1 x 2048 (16/8) 92 us against 68.
+constexpr int kDqSlots = 4;
+
+template <int D>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(QB == 2 ? 1 : 2)))
+__attribute__((amdgpu_waves_per_eu(1, 2)))
 void dq_kernel(BwdArgs a) {
   constexpr int NK = D / 16, NM = D / 32;
-  constexpr int kOwn = 32 * QB;        // rows of a wave
-  constexpr int kSlots = QB == 2 ? kRing : 4;
   using T = RowTile<D>;
   constexpr int kPair = 2 * T::bytes;
-  __shared__ __attribute__((aligned(1024))) char smem[kSlots * kPair];
-  const int chunks = (a.L + kOwn - 1) / kOwn;
-  const int groups = (chunks * a.G + kWaves - 1) / kWaves;
+  constexpr int kLoads = PairLoader<D>::kCount;
+  __shared__ __attribute__((aligned(1024))) char smem[kDqSlots * kPair];
+  const int groups = (a.T * a.G + kWaves - 1) / kWaves;
   int wg = blockIdx.x;
   const int kvh = wg % a.Hkv;
   wg /= a.Hkv;
@@ -400,17 +401,18 @@ void dq_kernel(BwdArgs a) {
   const int sq = wg / groups;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = lane_id(), col = lane & 31, hf = lane >> 5;
-  const int last_unit = chunks * a.G - 1;
+  const int last_unit = a.T * a.G - 1;
+  // (past the last unit: it again, its results dropped)
   const int unit = min(grp * kWaves + wave, last_unit);
   const bool live = grp * kWaves + wave <= last_unit;
-  const int p0 = unit / a.G * kOwn;
+  const int p0 = unit / a.G * kRows;
   const int head = kvh * a.G + unit % a.G;
   const int64_t row0 = (static_cast<int64_t>(sq) * 2 + stream) * a.L;
 
   // tiles: memory keys from 0, then for prediction rows their own blocks'
-  const int first = grp * kWaves / a.G * kOwn;
+  const int first = grp * kWaves / a.G * kRows;
   const int end = min(a.L, (min(grp * kWaves + kWaves - 1, last_unit) / a.G +
-                            1) * kOwn);
+                            1) * kRows);
   const int n_mem =
       ((stream ? (end - 1) / a.block * a.block : end) + kRows - 1) / kRows;
   const int own0 = first / a.block * a.block / kRows;
@@ -420,8 +422,8 @@ void dq_kernel(BwdArgs a) {
   const int64_t kv0 = (static_cast<int64_t>(sq) * 2 * a.L * a.Hkv + kvh) * D;
   const PairLoader<D> loader(a.k + kv0, a.v + kv0, a.Hkv * D, wave,
                              lds_address(smem));
-  // the tile that is loaded next
-  int ahead = 0, ahead_p = 0;
+  // the tile that is loaded next, and its first key's row
+  int ahead = 0, ahead_p = n_mem == 0 ? a.L + own0 * kRows : 0;
   auto fetch = [&](int u, int slot) {
     loader.load(u, static_cast<int64_t>(ahead_p) * (a.Hkv * D),
                 a.L - 1 - (ahead >= n_mem ? ahead_p - a.L : ahead_p),
@@ -433,73 +435,60 @@ void dq_kernel(BwdArgs a) {
     ahead_p = ahead >= n_mem ? a.L + (own0 + ahead - n_mem) * kRows
                              : ahead * kRows;
   };
-  if (n_mem == 0) ahead_p = a.L + own0 * kRows;
-  const Reader<D> rd;
-  constexpr int kE = 16 / NK;              // elements per step
-  constexpr int kLoads = PairLoader<D>::kCount;
-  bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
 #pragma unroll
-  for (int i = 0; i < kSlots - 1; ++i) {
+  for (int i = 0; i < kDqSlots - 1; ++i) {
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) fetch(u, i);
     advance();
   }
 
-  bf16x8_t qf[QB][NK], dof[QB][NK];
-  float lse2[QB], delta[QB];
-  int lo[QB], hi[QB];         // memory: keys below lo; own stream: see own()
+  // the lane's row: q, dout, lse and D; it sees memory keys below lo
+  // (prediction) or hi (memory), and the own stream's lo .. hi-1
+  bf16x8_t qf[NK], dof[NK];
+  const int p = p0 + col, pc = min(p, a.L - 1);
+  const int lo = stream ? pc / a.block * a.block : 0, hi = pc + 1;
+  const int64_t o = ((row0 + pc) * a.Hq + head) * D;
+  float delta = 0.f;
 #pragma unroll
-  for (int b = 0; b < QB; ++b) {
-    const int p = p0 + 32 * b + col;
-    const int pc = min(p, a.L - 1);
-    const int64_t o = ((row0 + pc) * a.Hq + head) * D;
-    float d = 0.f;
+  for (int kk = 0; kk < NK; ++kk) {
+    const int at = kk * 16 + hf * 8;
+    qf[kk] = load8(a.q + o + at);
+    dof[kk] = load8(a.dout + o + at);
+    const bf16x8_t of = load8(a.out + o + at);
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-      const int at = kk * 16 + hf * 8;
-      qf[b][kk] = load8(a.q + o + at);
-      dof[b][kk] = load8(a.dout + o + at);
-      const bf16x8_t of = load8(a.out + o + at);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        d += static_cast<float>(dof[b][kk][e]) * static_cast<float>(of[e]);
-    }
-    d += __shfl_xor(d, 32);
-    const float l2 = a.lse[(row0 + pc) * a.Hq + head] * kLog2e;
-    lse2[b] = l2;
-    delta[b] = d;
-    if (live && hf == 0 && p < a.T * kRows) {
-      float* ld = a.ld + ((((static_cast<int64_t>(sq) * a.Hq + head) * 2 +
-                            stream) * a.T + p / kRows) * 2) * kRows + col;
-      ld[0] = p < a.L ? -l2 : 0.f;
-      ld[kRows] = p < a.L ? -d : 0.f;
-    }
-    lo[b] = stream ? pc / a.block * a.block : 0;
-    hi[b] = pc + 1;
+    for (int e = 0; e < 8; ++e)
+      delta += static_cast<float>(dof[kk][e]) * static_cast<float>(of[e]);
   }
-  floatx16_t acc[QB][NM];
+  delta += __shfl_xor(delta, 32);
+  const float lse2 = a.lse[(row0 + pc) * a.Hq + head] * kLog2e;
+  if (live && hf == 0) {
+    float* ld = a.ld + ((((static_cast<int64_t>(sq) * a.Hq + head) * 2 + stream) *
+                         a.T + p / kRows) * 2) * kRows + col;
+    ld[0] = p < a.L ? -lse2 : 0.f;
+    ld[kRows] = p < a.L ? -delta : 0.f;
+  }
+  floatx16_t acc[NM];
 #pragma unroll
-  for (int b = 0; b < QB; ++b)
-#pragma unroll
-    for (int m = 0; m < NM; ++m) acc[b][m] = floatx16_t{};
+  for (int m = 0; m < NM; ++m) acc[m] = floatx16_t{};
 
   if (wave == 0) write_cuts(a);
   // take delivery of the rows: no wait for them in the loop
 #pragma unroll
-  for (int b = 0; b < QB; ++b)
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk)
-      asm volatile("" : "+v"(qf[b][kk]), "+v"(dof[b][kk]));
-  wait_vmcnt<(kSlots - 2) * kLoads>();
+  for (int kk = 0; kk < NK; ++kk)
+    asm volatile("" : "+v"(qf[kk]), "+v"(dof[kk]));
+  wait_vmcnt<(kDqSlots - 2) * kLoads>();
   __syncthreads();
+  const Reader<D> rd;
+  constexpr int kE = 16 / NK;              // elements per step
+  bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
 #pragma unroll
   for (int kk = 0; kk < NK; ++kk) f[kk] = rd.rows(smem, kk);
-  int slot = 0, next_slot = 1, load_slot = kSlots - 1;
+  int slot = 0, next_slot = 1, load_slot = kDqSlots - 1;
   int i = 0;               // (n > 0: a loop that runs at least once)
   do {
     // this wave's loads of tile i + 1, then everybody's; the barrier also
     // frees the slot of tile i - 1
-    wait_vmcnt<(kSlots - 3) * kLoads>();
+    wait_vmcnt<(kDqSlots - 3) * kLoads>();
     meet();
     const char* kt = smem + slot * kPair;
     const char* vt = kt + T::bytes;
@@ -507,139 +496,67 @@ void dq_kernel(BwdArgs a) {
     // the waves are in step, and a branch around the accumulators costs copies
     const bool own = i >= n_mem;
     const int j0 = (own ? own0 + i - n_mem : i) * kRows;
-    const bool mask = own || j0 + kRows > full;
-    floatx16_t s[QB], dp[QB];
-    float p[QB][16];
-    bf16x8_t ds[QB][2];
-    auto hide = [&](int b) {
+    floatx16_t s, dp;
+    float w[16];
+    bf16x8_t ds[2];
+    // Three phases of NK = 2 NM MFMAs: S, dP, dq
+    step();
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      s = mfma(f[kk], qf[kk], kk ? s : floatx16_t{});
+      f[kk] = rd.rows(vt, kk);
+      if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
+      step();
+    }
+    if (own || j0 + kRows > full) {
       const int k0 = j0 + 8 * (lane_here() >> 5);
-      const int from = own ? lo[b] : 0, to = own || !stream ? hi[b] : lo[b];
+      const int from = own ? lo : 0, to = own || !stream ? hi : lo;
       const uint32_t see = rows_between(from - k0, to - k0);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[b][e] = seen(see, e, s[b][e]);
-    };
-    auto weigh = [&](int b, int kk) {       // P
+      for (int e = 0; e < 16; ++e) s[e] = seen(see, e, s[e]);
+    }
+    step();
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      dp = mfma(f[kk], dof[kk], kk ? dp : floatx16_t{});
+      f[kk] = rd.cols(kt, kk / NM, kk % NM);
 #pragma unroll
       for (int e = kk * kE; e < kk * kE + kE; ++e) {
-        p[b][e] = __builtin_amdgcn_exp2f(
-            __builtin_fmaf(s[b][e], a.scale_log2, -lse2[b]));
-        here(p[b][e]);
+        w[e] = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[e], a.scale_log2, -lse2));
+        here(w[e]);
       }
-    };
-    auto grad = [&](int b, int kk) {        // dS
-#pragma unroll
-      for (int e = kk * kE; e < kk * kE + kE; ++e)
-        ds[b][e >> 3][e & 7] =
-            static_cast<__bf16>(p[b][e] * (dp[b][e] - delta[b]));
-    };
-    if constexpr (QB == 1) {
-      // One group: three phases, S, dP, dq.  (Two workgroups share a CU: the
-      // vector work of one runs under the other's products)
       step();
+    }
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        s[0] = mfma(f[kk], qf[0][kk], kk ? s[0] : floatx16_t{});
-        f[kk] = rd.rows(vt, kk);
-        if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
-        step();
-      }
-      if (mask) hide(0);
+    for (int e = 0; e < 16; ++e)
+      ds[e >> 3][e & 7] = static_cast<__bf16>(w[e] * (dp[e] - delta));
+    const char* nt = smem + next_slot * kPair;
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      if (x % NM == 0) settle(ds[x / NM]);
+      mfma_acc(acc[x % NM], f[x], ds[x / NM]);
+      f[x] = rd.rows(nt, x);
       step();
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        dp[0] = mfma(f[kk], dof[0][kk], kk ? dp[0] : floatx16_t{});
-        f[kk] = rd.cols(kt, kk / NM, kk % NM);
-        weigh(0, kk);
-        step();
-      }
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) grad(0, kk);
-      const char* nt = smem + next_slot * kPair;
-#pragma unroll
-      for (int x = 0; x < NK; ++x) {
-        if (x % NM == 0) settle(ds[0][x / NM]);
-        mfma_acc(acc[0][x % NM], f[x], ds[0][x / NM]);
-        f[x] = rd.rows(nt, x);
-        step();
-      }
-    } else {
-      // Six phases of NK = 2 NM MFMAs: S, dP, dq for either group of rows.  The
-      // vector work on a product starts a step after its last MFMA
-      step();
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        s[0] = mfma(f[kk], qf[0][kk], kk ? s[0] : floatx16_t{});
-        if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
-        step();
-      }
-      if (mask) hide(0);
-      step();
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        s[1] = mfma(f[kk], qf[1][kk], kk ? s[1] : floatx16_t{});
-        f[kk] = rd.rows(vt, kk);
-        if (kk >= 1) weigh(0, kk - 1);
-        step();
-      }
-      if (mask) hide(1);
-      step();
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        dp[0] = mfma(f[kk], dof[0][kk], kk ? dp[0] : floatx16_t{});
-        weigh(kk ? 1 : 0, kk ? kk - 1 : NK - 1);
-        step();
-      }
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        dp[1] = mfma(f[kk], dof[1][kk], kk ? dp[1] : floatx16_t{});
-        f[kk] = rd.cols(kt, kk / NM, kk % NM);
-        if (kk)
-          grad(0, kk - 1);
-        else
-          weigh(1, NK - 1);
-        step();
-      }
-#pragma unroll
-      for (int x = 0; x < NK; ++x) {
-        if (x % NM == 0) settle(ds[0][x / NM]);
-        mfma_acc(acc[0][x % NM], f[x], ds[0][x / NM]);
-        grad(x ? 1 : 0, x ? x - 1 : NK - 1);
-        step();
-      }
-      const char* nt = smem + next_slot * kPair;
-#pragma unroll
-      for (int x = 0; x < NK; ++x) {
-        if (x % NM == 0) settle(ds[1][x / NM]);
-        mfma_acc(acc[1][x % NM], f[x], ds[1][x / NM]);
-        f[x] = rd.rows(nt, x);
-        if (x == 0) grad(1, NK - 1);
-        step();
-      }
     }
     advance();
     load_slot = slot;
     slot = next_slot;
-    next_slot = next_slot == kSlots - 1 ? 0 : next_slot + 1;
+    next_slot = next_slot == kDqSlots - 1 ? 0 : next_slot + 1;
   } while (++i < n);
   wait_vmcnt<0>();      // surplus loads land before the LDS is given up
   drain(acc);
-  if (!live) return;
+  if (!live || p >= a.L) return;
+  uint16_t* dst = a.dq + o;
 #pragma unroll
-  for (int b = 0; b < QB; ++b) {
-    const int p = p0 + 32 * b + col;
-    if (p >= a.L) continue;
-    uint16_t* o = a.dq + ((row0 + p) * a.Hq + head) * D;
+  for (int m = 0; m < NM; ++m)
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+    for (int g = 0; g < 4; ++g) {
+      u16x4_t x;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        u16x4_t x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          x[e] = f32_to_bf16(acc[b][m][4 * g + e] * a.scale);
-        *reinterpret_cast<u16x4_t*>(o + 32 * m + 8 * g + 4 * hf) = x;
-      }
-  }
+      for (int e = 0; e < 4; ++e) x[e] = f32_to_bf16(acc[m][4 * g + e] * a.scale);
+      *reinterpret_cast<u16x4_t*>(dst + 32 * m + 8 * g + 4 * hf) = x;
+    }
 }
 
 // dk and dv: workgroup w walks stretch w; workgroups of one XCD take
@@ -962,8 +879,10 @@ void dkv_kernel(BwdArgs a) {
     }
   } while (++it < it1);
   wait_vmcnt<0>();      // surplus loads land before the LDS is given up
-  drain(dv);
-  drain(dk);
+  drain(dv[0]);
+  drain(dv[1]);
+  drain(dk[0]);
+  drain(dk[1]);
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int l = lane_here(), hf = l >> 5;
@@ -1056,7 +975,6 @@ struct BwdPlan {
   int T, W, group_cost;
   size_t cuts, part, total;
   unsigned dq_grid;
-  int qb;                 // 32-row groups of a dq wave
 };
 
 size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
@@ -1072,12 +990,8 @@ bool bwd_plan(int n_seq, int L, int block, int Hq, int Hkv, int D,
   if (static_cast<int64_t>(Hq) * D * 2 * kRows > 0x7fffffffll ||
       2ll * p->T * G > 0x3fffffffll)
     return false;
-  auto dq_groups = [&](int own) {
-    const int64_t chunks = (L + own - 1) / own;
-    return 2ll * n_seq * ((chunks * G + kWaves - 1) / kWaves) * Hkv;
-  };
-  p->qb = dq_groups(64) < 512 ? 1 : 2;
-  const int64_t dq = dq_groups(32 * p->qb);
+  const int64_t dq = 2ll * n_seq * Hkv *
+                     ((static_cast<int64_t>(p->T) * G + kWaves - 1) / kWaves);
   int64_t cost = 0;
   for (int i = 0; i < key_list(L); ++i) {
     const int items = key_tile(L, block, G, i).items;
@@ -1151,9 +1065,8 @@ extern "C" int wedlm_dual_stream_attn_backward(
   a.group_cost = p.group_cost;
   a.scale = softmax_scale;
   a.scale_log2 = softmax_scale * kLog2e;
-  auto dq_k = D == 128 ? (p.qb == 2 ? dq_kernel<128, 2> : dq_kernel<128, 1>)
-                       : (p.qb == 2 ? dq_kernel<64, 2> : dq_kernel<64, 1>);
-  hipLaunchKernelGGL(dq_k, dim3(p.dq_grid), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL(D == 128 ? dq_kernel<128> : dq_kernel<64>,
+                     dim3(p.dq_grid), dim3(kThreads), 0, st, a);
   WEDLM_LAUNCH_CHECK();
   hipLaunchKernelGGL(D == 128 ? dkv_kernel<128> : dkv_kernel<64>,
                      dim3(p.W), dim3(kThreads), 0, st, a);
