@@ -10,26 +10,41 @@
 // where the sums over i run over the G = Hq/Hkv query heads of the kv head
 // too.  Memory row p sees memory keys 0..p; prediction row p (block
 // start f = p / block * block) sees memory keys 0..f-1 and prediction keys
-// f..p.  In both directions the visible ones are an interval: every mask is
-// two comparisons.
+// f..p.  In both directions the visible ones are an interval.
 //
 // Two kernels, each accumulating in registers what it owns, so that nothing
 // is added atomically and the result does not depend on the run:
-//   dq:    a wave owns 64 rows of one head and walks the keys.  It also
+//   dq:    a wave owns 32 rows of one head and walks the keys.  It also
 //          writes D_i and lse_i, laid out for the second kernel.
 //   dk/dv: a wave owns 64 keys of one kv head and walks the rows of all its
-//          heads.
-// S and dP are formed in both, seven products instead of the five that a
-// pass with shared accumulators needs.
+//          heads.  (64, not 32: each operand read from LDS then feeds two
+//          MFMAs; with 32 the LDS would be as busy as the MFMAs.)
+// S and dP are formed in both: seven products instead of the five that a
+// single pass needs, which would have to add dq (or dk and dv) in memory, once
+// for every key tile, or write dS out, 4.3 GB for 4 x 4096 tokens.
 // MFMA: v_mfma_f32_32x32x16_bf16.  The score tile has the streamed rows
 // (keys in dq, query rows in dk/dv) as its M dimension and the owned ones as
 // N, so a lane holds 16 scores of one owned row, eight at a time contiguous
-// (key_of_row), which is the operand layout of the second product: P and dS
+// (row_of_m), which is the operand layout of the second product: P and dS
 // go from accumulators to operands in registers.  The second product's other
 // operand is read from the same LDS tile by columns (ds_read_b64_tr_b16).
-// Each operand read from LDS feeds two MFMAs (the wave's two 32-row groups).
-// P and dS are rounded to bf16 for the second products, as the forward
-// rounds P; all sums are fp32.
+//
+// Roundings: P and dS to bf16 for the second products, as the forward rounds
+// P; D from the forward's bf16 output; everything else, all sums among it,
+// fp32.  Rounding dS adds as much as rounding the result does (0.17% of a
+// gradient's norm), D's a third to a half of that where rows see few keys:
+// 0.24-0.27% together, against 0.17% for an fp32 gradient rounded once.  In
+// wider operands the second products would run at a fraction of the rate.
+//
+// Bound by the MFMAs, and these by the card's power: 4 x 4096 tokens (32/8
+// heads of 128) 3.37 ms, 816 TFLOP/s of the five products and 1.14 PFLOP/s of
+// what runs, masked parts included; MFMAs on random values that do nothing
+// else hold 1.30 PFLOP/s, a large library product 1.22.  Leaving out barriers,
+// waits or exponentials does not change it.  Steps there: plain staging, with
+// spills, 31.2 ms; tiles straight to LDS, accumulators held in AGPRs, 5.78;
+// one MFMA a step with vector work under it 4.35; equal work per CU 3.62;
+// prediction keys by single waves 3.41.  Shorter sequences are bound by
+// latency: 1 x 2048 (16/8 heads) 183 us, 1 x 256 (4/2 heads of 64) 32 us.
 #include <algorithm>
 #include <initializer_list>
 
@@ -248,8 +263,9 @@ __device__ __forceinline__ int lane_here() {
 }
 
 // Ends a step: what is written before it is issued before it.  The tiles are
-// written as steps of one MFMA and the vector work and LDS reads that run
-// under it (32 cycles, room for seven other instructions).
+// written as steps of one MFMA (32 cycles) and the vector work and LDS reads
+// that run under it (measured, n fused multiply-adds beside an MFMA take
+// 16 + 4 n cycles: four fit, or an exponential and two).
 __device__ __forceinline__ void step() { __builtin_amdgcn_sched_barrier(0); }
 
 // The accumulators of the last mfma_acc() are written (18 wait states).
@@ -375,7 +391,9 @@ __device__ __forceinline__ Cut read_cut(const BwdArgs& a, int w) {
 }
 
 // dq: workgroup = four units (chunk of 32 positions, head) of one stream and
-// kv head, one per wave; the longest first.  Registers and a ring of four
+// kv head, one per wave; the longest first, of all sequences (sequence by
+// sequence: 4 x 512 tokens 34.6 us against 30.8, 4 x 4096 the same, 2 x 1008
+// with 28/4 heads 71 against 73).  Registers and a ring of four
 // tiles let two workgroups share a CU (D = 64: three), so that the vector work
 // of one runs under the products of the other.  With 64 rows a wave, half the
 // LDS reads per product but one workgroup per CU: 4 x 4096 tokens (32/8 heads
@@ -397,8 +415,8 @@ void dq_kernel(BwdArgs a) {
   wg /= a.Hkv;
   const int stream = wg & 1;
   wg >>= 1;
-  const int grp = groups - 1 - wg % groups;
-  const int sq = wg / groups;
+  const int grp = groups - 1 - wg / a.n_seq;
+  const int sq = wg % a.n_seq;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = lane_id(), col = lane & 31, hf = lane >> 5;
   const int last_unit = a.T * a.G - 1;

@@ -6,13 +6,16 @@
 // Nothing cancels, so that a token predicted with p_t near 1 keeps the digits
 // of 1 - p_t; the target is kept out of the sum from the start.
 // One workgroup per row.  Every thread keeps the first H 16-byte chunks that
-// it reads in registers: their maximum, then e^{l - m} in their place with
-// the sum, then the gradient, so that these logits are read once and their
-// exponentials taken once.  What does not fit (fp32 rows beyond 77824) is
-// reduced with a running maximum and read again for the gradient, while it is
-// in the L2.  Few long rows are split over workgroups: one kernel for the
-// slices' maxima and sums, one that joins them and forms the gradient.
-// Bound by HBM: logits read once, gradients written once.
+// it reads in registers: maximum, sum and gradient all come from there, so that
+// these logits are read once.  What does not fit (fp32 rows beyond 77824) is
+// reduced with a running maximum and read again for the gradient.  Few long
+// rows are split over workgroups: one kernel for the slices' maxima and sums,
+// one that joins them and forms the gradient.
+// Bound by HBM: logits read once, gradients written once (past the caches: a
+// large gradient does not stay there, the row's rest does).  4096 x 151936
+// fp32 1.03 ms, 4.8 TB/s, where a large copy reaches 5.1 (one element at a
+// time in two passes 1.85 ms); 1000 x 32003 bf16, half of the rows without
+// loss, 28 us; 32 x 1024 8 us, one launch.
 #include "common.h"
 #include "wedlm_train.h"
 
