@@ -1,0 +1,117 @@
+"""The training operators on arrays of more than 2^31 elements: what they make
+of the last rows equals what a call on those rows alone makes of them (bit for
+bit where a row's result is its own; within two bf16 roundings of the norm
+where the order of a sum goes by the sizes)."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-6
+
+
+@pytest.fixture(autouse=True)
+def memory():
+    if torch.cuda.get_device_properties(0).total_memory < 100 << 30:
+        pytest.skip("needs 100 GiB")
+    yield
+    torch.cuda.empty_cache()
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _bf16(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda").bfloat16()
+
+
+def test_attention_backward():
+    from paper_2512_22737_amd import wedlm as W
+    n, L, block, Hq, Hkv, D = 1040, 1024, 64, 16, 2, 64
+    assert n * 2 * L * Hq * D > 1 << 31
+    print("attention backward, 2^31 elements", flush=True)
+    g = _gen(1)
+    q, dout = _bf16(g, 1, 2 * L, Hq, D), _bf16(g, 1, 2 * L, Hq, D)
+    k, v = _bf16(g, 1, 2 * L, Hkv, D), _bf16(g, 1, 2 * L, Hkv, D)
+    out, lse = torch.empty_like(q), torch.empty(1, 2 * L, Hq, device="cuda")
+    W.wedlm_dual_stream_attn(q, k, v, block, out, lse)
+    one = [torch.empty_like(x) for x in (q, k, v)]
+    W.wedlm_dual_stream_attn_backward(q, k, v, block, out, lse, dout, *one)
+    many = [x.expand(n, *x.shape[1:]).contiguous()
+            for x in (q, k, v, out, lse, dout)]
+    got = [torch.full_like(x, float("nan")) for x in many[:3]]
+    W.wedlm_dual_stream_attn_backward(*many[:3], block, *many[3:], *got)
+    for at in (0, n // 2, n - 1):
+        assert torch.equal(got[0][at], one[0][0])
+        for x, y in zip(got[1:], one[1:]):
+            err = (x[at].float() - y[0].float()).norm() / y.float().norm()
+            assert err <= 2.0 ** -7, err
+
+
+def test_rmsnorm_backward():
+    from paper_2512_22737_amd import wedlm as W
+    M, Hd = 530000, 4096
+    assert M * Hd > 1 << 31
+    print("RMSNorm backward, 2^31 elements", flush=True)
+    x = torch.randn(M, Hd, generator=_gen(2), device="cuda")
+    dy = torch.empty(M, Hd, dtype=torch.bfloat16, device="cuda").normal_(
+        generator=_gen(3))
+    gain = 1 + 0.1 * _bf16(_gen(4), Hd)
+    dx, dg = torch.empty_like(x), torch.empty(Hd, device="cuda")
+    W.wedlm_rmsnorm_backward(x, gain, EPS, dy, dx, dg)
+    part = torch.empty(7, Hd, device="cuda")
+    W.wedlm_rmsnorm_backward(x[-7:], gain, EPS, dy[-7:], part)
+    assert torch.equal(dx[-7:], part)
+    # the gain's gradient over everything, in stretches in 64 bits
+    want = torch.zeros(Hd, dtype=torch.float64, device="cuda")
+    for i in range(0, M, 50000):
+        y = x[i:i + 50000].double()
+        y *= torch.rsqrt(y.square().mean(1, keepdim=True) + EPS)
+        want += (y * dy[i:i + 50000].double()).sum(0)
+    # fp32 sums of 530000 products in 1024 parts of 518: a part of k products
+    # is of size sqrt(k), each addition is off by 2^-24 of it at most, errors
+    # of random sign add to 2^-24 * 518 / sqrt(2) a part, sqrt(1024) times
+    # that in all, 16 * 2^-24 of the sum's sqrt(530000); the roundings of x's
+    # norm are common to a row and as small. 2000 leaves two digits.
+    assert (dg.double() - want).norm() <= 2.0 ** -24 * 2000 * want.norm()
+
+
+def test_qk_norm_rope_backward():
+    from paper_2512_22737_amd import wedlm as W
+    M, Hq, Hkv, D = 360000, 32, 8, 128
+    assert M * (Hq + 2 * Hkv) * D > 1 << 31
+    print("q/k norm + RoPE backward, 2^31 elements", flush=True)
+    g = _gen(5)
+    fill = lambda *s: torch.empty(*s, dtype=torch.bfloat16,
+                                  device="cuda").normal_(generator=g)
+    qkv = fill(M, (Hq + 2 * Hkv) * D)
+    dq, dk, dv = fill(M, Hq, D), fill(M, Hkv, D), fill(M, Hkv, D)
+    gq, gk = fill(D), fill(D)
+    pos = torch.arange(M, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(qkv)
+    W.wedlm_qk_norm_rope_backward(qkv, gq, gk, pos, 1e6, EPS, dq, dk, dv, out)
+    part = torch.empty_like(out[-9:])
+    W.wedlm_qk_norm_rope_backward(qkv[-9:], gq, gk, pos[-9:], 1e6, EPS,
+                                  dq[-9:], dk[-9:], dv[-9:], part)
+    assert torch.equal(out[-9:], part)
+
+
+def test_token_loss():
+    from paper_2512_22737_amd import wedlm as W
+    R, V = 14200, 151936
+    assert R * V > 1 << 31
+    print("token loss, 2^31 elements", flush=True)
+    x = torch.empty(R, V, dtype=torch.bfloat16, device="cuda").normal_(
+        generator=_gen(6))
+    t = torch.randint(0, V, (R,), generator=_gen(7), device="cuda",
+                      dtype=torch.int32)
+    loss, d = torch.empty(R, device="cuda"), torch.empty_like(x)
+    W.wedlm_token_loss(x, t, loss, None, d)
+    # as many rows that the same kernel runs on
+    part, pd = torch.empty(200, device="cuda"), torch.empty_like(x[-200:])
+    W.wedlm_token_loss(x[-200:], t[-200:], part, None, pd)
+    assert torch.equal(loss[-200:], part) and torch.equal(d[-200:], pd)
+    want = torch.nn.functional.cross_entropy(x[-200:].double(), t[-200:].long(),
+                                             reduction="none")
+    assert (loss[-200:].double() - want).abs().max() <= 1e-5 * want.max()
