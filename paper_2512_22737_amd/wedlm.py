@@ -818,10 +818,12 @@ def wedlm_dual_stream_attn_backward(q, k, v, block: int, out, lse, dout, dq,
 
 
 def _workspace(workspace, need: int, device):
-    """Address and bytes of a workspace, allocated here if none is given."""
+    """A workspace's tensor (allocated here if none is given), address and
+    bytes.  The caller holds the tensor until its launches are enqueued: freed
+    earlier, another thread could be handed the memory for work before them."""
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    return _t(workspace, "workspace", _U8), workspace.numel()
+    return workspace, _t(workspace, "workspace", _U8), workspace.numel()
 
 
 def wedlm_rmsnorm_backward_workspace_size(M, Hd) -> int:
@@ -835,9 +837,9 @@ def wedlm_rmsnorm_backward(x, gain, eps: float, dy, dx, dgain=None, dres=None,
     dgain [Hd] fp32 (optional).  A workspace is allocated here if dgain needs
     one and none is given."""
     M, Hd = x.shape
-    ws, nbytes = None, 0
+    held, ws, nbytes = None, None, 0
     if dgain is not None:
-        ws, nbytes = _workspace(
+        held, ws, nbytes = _workspace(
             workspace, wedlm_rmsnorm_backward_workspace_size(M, Hd), x.device)
     code = _load().wedlm_rmsnorm_backward(
         _t(x, "x", _F32), _t(gain, "gain", _BF16, (Hd,)),
@@ -864,9 +866,9 @@ def wedlm_qk_norm_rope_backward(qkv, q_gain, k_gain, pos_ids,
     one and none is given."""
     M, Hq, D = dq.shape
     Hkv = dk.shape[1]
-    ws, nbytes = None, 0
+    held, ws, nbytes = None, None, 0
     if dq_gain is not None or dk_gain is not None:
-        ws, nbytes = _workspace(
+        held, ws, nbytes = _workspace(
             workspace,
             wedlm_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D),
             qkv.device)
@@ -903,9 +905,9 @@ def wedlm_token_loss(logits, target, loss, weight=None, dlogits=None,
     half = logits.dtype == torch.bfloat16
     types = (torch.bfloat16,) if half else _F32
     need = wedlm_token_loss_workspace_size(R, V)
-    ws, nbytes = None, 0
+    held, ws, nbytes = None, None, 0
     if need:
-        ws, nbytes = _workspace(workspace, need, logits.device)
+        held, ws, nbytes = _workspace(workspace, need, logits.device)
     code = _load().wedlm_token_loss(
         _t(logits, "logits", types), LOGITS_BF16 if half else LOGITS_F32,
         stride, _t(target, "target", _I32, (R,)),
