@@ -111,11 +111,12 @@ size_t wedlm_rmsnorm_backward_workspace_size(int32_t M, int32_t Hd);
  *   dx [M, Hd] fp32 (may be dres itself: the gradient is then added in
  *   place), dgain [Hd] fp32 or NULL (a frozen gain); both overwritten.
  *   Otherwise they must not overlap the inputs or each other.
- * Hd a multiple of 4; x, dres, dx and the workspace on 16-byte boundaries,
- * gain and dy on 8-byte ones (WEDLM_E_ARG).
- * workspace: wedlm_rmsnorm_backward_workspace_size() bytes (partial sums of dgain; none needed without it); its contents on entry do
- * not matter.  The sums' order is fixed by the sizes.  Two calls that overlap
- * in time must not share a workspace.
+ * M >= 1, Hd a multiple of 4 up to 2^20; x, dres, dx and the workspace on
+ * 16-byte boundaries, gain and dy on 8-byte ones (WEDLM_E_ARG).
+ * workspace: wedlm_rmsnorm_backward_workspace_size() bytes (partial sums of
+ * dgain; none needed without it); its contents on entry do not matter.  The
+ * sums' order is fixed by the sizes.  Two calls that overlap in time must not
+ * share a workspace.
  */
 int wedlm_rmsnorm_backward(const float* x, const uint16_t* gain,
                            const uint16_t* dy, const float* dres, int32_t M,

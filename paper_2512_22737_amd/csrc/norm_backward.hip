@@ -54,7 +54,9 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_kernel(
     }
   }
   int turn = 0;
-  for (int t = blockIdx.x; t < M; t += gridDim.x, turn ^= 1) {
+  // (unsigned: t may pass 2^31 - 1 once)
+  for (uint32_t t = blockIdx.x; t < static_cast<uint32_t>(M);
+       t += gridDim.x, turn ^= 1) {
     const int64_t row = static_cast<int64_t>(t) * Hd;
     floatx4_t v[CPT], d[CPT];
     float ss = 0.f, dot = 0.f;
@@ -124,7 +126,9 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_long_kernel(
   const int nc = Hd / 4;
   __shared__ float sums[2][2][kThreads / kWave];
   int turn = 0;
-  for (int t = blockIdx.x; t < M; t += gridDim.x, turn ^= 1) {
+  // (unsigned: t may pass 2^31 - 1 once)
+  for (uint32_t t = blockIdx.x; t < static_cast<uint32_t>(M);
+       t += gridDim.x, turn ^= 1) {
     const int64_t row = static_cast<int64_t>(t) * Hd;
     float ss = 0.f, dot = 0.f;
     for (int c = threadIdx.x; c < nc; c += kThreads) {
@@ -160,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_long_kernel(
       floatx4_t o, s = {};
       if (dres) s = *reinterpret_cast<const floatx4_t*>(dres + row + c * 4);
       floatx4_t p = {};
-      if (prow && t != static_cast<int>(blockIdx.x))
+      if (prow && t != blockIdx.x)
         p = *reinterpret_cast<const floatx4_t*>(prow + c * 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -348,6 +352,9 @@ bool aligned(std::initializer_list<const void*> ps, int bytes) {
 // four per CU for rows of up to 4096 (32768 x 4096 346 us; 512 workgroups 416,
 // 2048 370), two for longer ones, whose registers hold no more (4096 x 8192
 // 111 us; 1024 workgroups 119).
+bool norm_ok(int M, int Hd) {
+  return M >= 1 && Hd >= 4 && Hd <= 1 << 20 && Hd % 4 == 0;
+}
 int norm_parts(int M, int Hd) { return std::min(M, Hd > 4096 ? 512 : 1024); }
 
 // Rows that a workgroup of the q/k kernel takes at once: four where that
@@ -376,7 +383,7 @@ bool qk_ok(int M, int Hq, int Hkv, int D) {
 }  // namespace
 
 extern "C" size_t wedlm_rmsnorm_backward_workspace_size(int32_t M, int32_t Hd) {
-  if (M < 1 || Hd < 4 || Hd % 4 != 0) return 0;
+  if (!norm_ok(M, Hd)) return 0;
   return static_cast<size_t>(norm_parts(M, Hd)) * Hd * sizeof(float);
 }
 
@@ -388,7 +395,7 @@ extern "C" int wedlm_rmsnorm_backward(const float* x, const uint16_t* gain,
   if (!x || !gain || !dy || !dx || !(eps > 0.f)) return WEDLM_E_ARG;
   if (!aligned({x, dres, dx, workspace}, 16) || !aligned({gain, dy}, 8))
     return WEDLM_E_ARG;
-  if (M < 1 || Hd < 4 || Hd % 4 != 0) return WEDLM_E_SHAPE;
+  if (!norm_ok(M, Hd)) return WEDLM_E_SHAPE;
   if (dgain && (!workspace ||
                 workspace_bytes < wedlm_rmsnorm_backward_workspace_size(M, Hd)))
     return WEDLM_E_WORKSPACE;

@@ -77,6 +77,22 @@ def test_rmsnorm_backward():
     assert (dg.double() - want).norm() <= 2.0 ** -24 * 2000 * want.norm()
 
 
+def test_rmsnorm_backward_row_numbers():
+    from paper_2512_22737_amd import wedlm as W
+    M, Hd = (1 << 31) - 1, 4          # the next stride of rows passes 2^31
+    print("RMSNorm backward, 2^31 - 1 rows", flush=True)
+    x = torch.randn(M, Hd, generator=_gen(8), device="cuda")
+    dy = torch.empty(M, Hd, dtype=torch.bfloat16, device="cuda").normal_(
+        generator=_gen(9))
+    gain = 1 + 0.1 * _bf16(_gen(10), Hd)
+    dx = torch.empty_like(x)
+    W.wedlm_rmsnorm_backward(x, gain, EPS, dy, dx)
+    for rows in (slice(0, 9), slice(M - 2000, M)):
+        part = torch.empty_like(x[rows])
+        W.wedlm_rmsnorm_backward(x[rows], gain, EPS, dy[rows], part)
+        assert torch.equal(dx[rows], part)
+
+
 def test_qk_norm_rope_backward():
     from paper_2512_22737_amd import wedlm as W
     M, Hq, Hkv, D = 360000, 32, 8, 128

@@ -98,3 +98,12 @@ def test_token_loss_refusals():
     refusals(lib.wedlm_token_loss, args,
              [(i, None, -1) for i in (0, 3, 7)] +
              [(1, 2, -1), (1, -1, -1), (2, 63, -2), (5, 0, -2), (6, 0, -2)])
+
+
+def test_rmsnorm_backward_refuses_the_longest_rows():
+    """A launch over their columns would have more than 2^32 threads."""
+    lib = _lib()
+    ws = lib.wedlm_rmsnorm_backward_workspace_size
+    assert ws(1, 1 << 20) == 4 << 20 and ws(1, (1 << 20) + 4) == 0
+    args = [F] * 4 + [1, (1 << 20) + 4, 1e-6, F, F, F, 1 << 40, None]
+    assert lib.wedlm_rmsnorm_backward(*args) == -2
