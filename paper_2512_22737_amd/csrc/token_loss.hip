@@ -428,17 +428,35 @@ int row_slices(int R, int V, int per_chunk) {
   return V / len + (V % len != 0);
 }
 
+// One workgroup per row, in stretches of rows: a launch has fewer than 2^32
+// threads.
+constexpr int kRowsPerLaunch = 1 << 21;
+
+template <typename T>
+int launch_rows(void (*kernel)(LossArgs), int threads, const LossArgs& a,
+                hipStream_t st) {
+  for (int64_t r = 0; r < a.R; r += kRowsPerLaunch) {
+    LossArgs b = a;
+    b.logits = static_cast<const T*>(a.logits) + r * a.stride;
+    b.target = a.target + r;
+    b.weight = a.weight ? a.weight + r : nullptr;
+    b.loss = a.loss + r;
+    b.dlogits = a.dlogits ? static_cast<T*>(a.dlogits) + r * a.stride : nullptr;
+    const int64_t rows = std::min<int64_t>(a.R - r, kRowsPerLaunch);
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(rows)), dim3(threads),
+                       0, st, b);
+    WEDLM_LAUNCH_CHECK();
+  }
+  return WEDLM_OK;
+}
+
 template <typename T>
 int launch(const LossArgs& a0, hipStream_t st) {
   LossArgs a = a0;
   const uintptr_t x = reinterpret_cast<uintptr_t>(a.logits);
   const uintptr_t y = reinterpret_cast<uintptr_t>(a.dlogits);
-  if (y && (x ^ y) % 16 != 0) {
-    hipLaunchKernelGGL(token_loss_plain_kernel<T>, dim3(a.R),
-                       dim3(kSmallThreads), 0, st, a);
-    WEDLM_LAUNCH_CHECK();
-    return WEDLM_OK;
-  }
+  if (y && (x ^ y) % 16 != 0)
+    return launch_rows<T>(token_loss_plain_kernel<T>, kSmallThreads, a, st);
   a.slices = row_slices(a.R, a.V, Elem<T>::n);
   a.slice_len = slice_len(a.R, a.V, Elem<T>::n);
   if (a.slices > 1) {
@@ -456,16 +474,12 @@ int launch(const LossArgs& a0, hipStream_t st) {
   // 256, 9.6 with 1024
   const int chunks = a.V / Elem<T>::n;
   if (chunks <= kSmallThreads * 4)
-    hipLaunchKernelGGL((token_loss_kernel<T, kSmallThreads, 4>), dim3(a.R),
-                       dim3(kSmallThreads), 0, st, a);
-  else if (chunks <= kSmallChunks && a.R >= 128)
-    hipLaunchKernelGGL((token_loss_kernel<T, kSmallThreads, kSmallHeld>),
-                       dim3(a.R), dim3(kSmallThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((token_loss_kernel<T, 1024, 19>), dim3(a.R), dim3(1024),
-                       0, st, a);
-  WEDLM_LAUNCH_CHECK();
-  return WEDLM_OK;
+    return launch_rows<T>(token_loss_kernel<T, kSmallThreads, 4>,
+                          kSmallThreads, a, st);
+  if (chunks <= kSmallChunks && a.R >= 128)
+    return launch_rows<T>(token_loss_kernel<T, kSmallThreads, kSmallHeld>,
+                          kSmallThreads, a, st);
+  return launch_rows<T>(token_loss_kernel<T, 1024, 19>, 1024, a, st);
 }
 
 }  // namespace

@@ -131,3 +131,28 @@ def test_token_loss():
     want = torch.nn.functional.cross_entropy(x[-200:].double(), t[-200:].long(),
                                              reduction="none")
     assert (loss[-200:].double() - want).abs().max() <= 1e-5 * want.max()
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+def test_token_loss_of_many_rows(shift):
+    """More rows than one launch has threads for (shift: gradients at another
+    offset from 16 bytes than the logits)."""
+    from paper_2512_22737_amd import wedlm as W
+    R, V = (1 << 24) + 300, 8
+    print(f"token loss, 2^24 + 300 rows, shift {shift}", flush=True)
+    g = _gen(11)
+    x, weight = _bf16(g, R, V), torch.rand(R, generator=g, device="cuda")
+    t = torch.randint(-1, V, (R,), generator=g, device="cuda",
+                      dtype=torch.int32)
+    loss = torch.full((R,), float("nan"), device="cuda")
+    d = torch.full((R * V + shift,), float("nan"), dtype=torch.bfloat16,
+                   device="cuda")[shift:].view(R, V)
+    W.wedlm_token_loss(x, t, loss, weight, d)
+    assert not loss.isnan().any() and not d.isnan().any()
+    for at in (0, (1 << 21) - 100, R - 200):
+        rows = slice(at, at + 200)
+        part, pd = torch.empty(200, device="cuda"), torch.empty(
+            200 * V + shift, dtype=torch.bfloat16, device="cuda")[shift:]
+        pd = pd.view(200, V)
+        W.wedlm_token_loss(x[rows], t[rows], part, weight[rows], pd)
+        assert torch.equal(loss[rows], part) and torch.equal(d[rows], pd)
