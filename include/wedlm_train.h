@@ -141,7 +141,8 @@ size_t wedlm_qk_norm_rope_backward_workspace_size(int32_t M, int32_t Hq,
  * Out:
  *   dqkv [M, (Hq + 2 Hkv) D] bf16; dq_gain, dk_gain [D] fp32, each NULL if
  *   not wanted; all overwritten, no overlap with the inputs or each other.
- * D 64 or 128; bf16 arrays on 16-byte boundaries (WEDLM_E_ARG).
+ * M, Hq, Hkv >= 1, D 64 or 128; bf16 arrays on 16-byte boundaries
+ * (WEDLM_E_ARG).
  * workspace: wedlm_qk_norm_rope_backward_workspace_size() bytes (partial sums
  * of the gains' gradients; none needed without them); its contents on entry
  * do not matter.  The sums' order is fixed by the sizes.  Two calls that
@@ -169,7 +170,7 @@ size_t wedlm_token_loss_workspace_size(int32_t R, int32_t V);
  *   dlogits[r][v] = weight[r] (p[v] - [v = target[r]])
  * A row whose target is outside 0 .. V-1 (a position without loss) or whose
  * weight is 0 has loss 0 and gradient 0, and its logits are not used.
- * In:
+ * In (R, V >= 1):
  *   logits [R, row_stride] of logits_type (WEDLM_LOGITS_*), row_stride >= V;
  *   values finite or -inf (a token that is ruled out: p = 0).  A row of
  *   nothing but -inf has loss weight * inf and gradient 0.

@@ -9,8 +9,8 @@
 // Bound by HBM: every array is passed over once, rows stay in registers between
 // their sums and their gradients.  RMSNorm 32768 x 4096 338-346 us, 5.5 TB/s
 // (a large copy reaches 5.1), 8193 x 2560 without a residual gradient 47 us,
-// 4.4 TB/s; q/k norm with RoPE of 32768 rows of 32/8 heads of 128 236 us,
-// 4.8 TB/s.  Few rows are bound by the two launches, 10 to 13 us.
+// 4.4 TB/s; q/k norm with RoPE of 32768 rows of 32/8 heads of 128 233 us,
+// 4.9 TB/s.  Few rows are bound by the two launches, 10 to 13 us.
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -179,22 +179,22 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_backward_long_kernel(
 }
 
 // Columns of part [parts, n0 + n1] summed in a fixed order into out0 [n0] and
-// out1 [n1] (either may be null): 64 columns per workgroup, its 16 waves take
-// every 16th part, eight loads under way each, so that 1024 parts are eight
+// out1 [n1] (either may be null): C columns per workgroup, 1024 / C threads to a
+// column, eight loads under way each: with 64 columns 1024 parts are eight
 // round trips to memory.
 constexpr int kSumThreads = 1024;
 
+template <int C>
 __global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(
     const float* __restrict__ part, int parts, int n0, int n1,
     float* __restrict__ out0, float* __restrict__ out1) {
-  constexpr int W = kSumThreads / kWave;
-  const int n = n0 + n1;
-  const int c = blockIdx.x * kWave + lane_id();
-  const int w = threadIdx.x / kWave;
-  __shared__ float s[W][kWave];
+  constexpr int W = kSumThreads / C;
+  const int n = n0 + n1, col = threadIdx.x % C;
+  const int c = blockIdx.x * C + col;
+  __shared__ float s[kSumThreads / kWave][C];
   float v = 0.f;
   if (c < n) {
-    int p = w;
+    int p = threadIdx.x / C;
     for (; p + 7 * W < parts; p += 8 * W) {
       float x[8];
 #pragma unroll
@@ -205,13 +205,15 @@ __global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(
 #pragma unroll 4
     for (; p < parts; p += W) v += part[static_cast<int64_t>(p) * n + c];
   }
-  s[w][lane_id()] = v;
+#pragma unroll
+  for (int off = C; off < kWave; off <<= 1) v += __shfl_xor(v, off);
+  if (lane_id() < C) s[threadIdx.x / kWave][col] = v;
   __syncthreads();
   float* out = c < n0 ? out0 : out1;
-  if (w == 0 && c < n && out) {
+  if (threadIdx.x < C && c < n && out) {
     float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < W; ++i) t += s[i][lane_id()];
+    for (int i = 0; i < kSumThreads / kWave; ++i) t += s[i][col];
     out[c < n0 ? c : c - n0] = t;
   }
 }
@@ -359,7 +361,7 @@ int norm_parts(int M, int Hd) { return std::min(M, Hd > 4096 ? 512 : 1024); }
 
 // Rows that a workgroup of the q/k kernel takes at once: four where that
 // leaves a workgroup per CU (1024 rows of 32/8 heads of 128 24 us with one,
-// 19 with four; 512 rows 14.4, 17.0; 32768 rows 304, 236).
+// 19 with four; 512 rows 14.4, 17.0; 32768 rows 304, 233).
 constexpr int kQkRows = 4;
 int qk_rows(int M) { return M >= kQkRows * 256 ? kQkRows : 1; }
 int qk_parts(int M) {
@@ -367,10 +369,15 @@ int qk_parts(int M) {
   return groups < kQkParts ? groups : kQkParts;
 }
 
+// 64 columns per workgroup read 256 bytes together (1024 parts of 4096 5.6 us;
+// 16 columns 7.2); few columns would leave most CUs idle (2048 parts of 256
+// 11.8 us; 16 columns 8.4).
 int sum_parts(const float* part, int parts, int n0, int n1, float* out0,
               float* out1, hipStream_t st) {
-  hipLaunchKernelGGL(sum_parts_kernel, dim3((n0 + n1 + kWave - 1) / kWave),
-                     dim3(kSumThreads), 0, st, part, parts, n0, n1, out0, out1);
+  const int n = n0 + n1, cols = n <= 256 ? 16 : 64;
+  hipLaunchKernelGGL(cols == 16 ? sum_parts_kernel<16> : sum_parts_kernel<64>,
+                     dim3((n + cols - 1) / cols), dim3(kSumThreads), 0, st,
+                     part, parts, n0, n1, out0, out1);
   WEDLM_LAUNCH_CHECK();
   return WEDLM_OK;
 }
