@@ -44,7 +44,7 @@
 // spills, 31.2 ms; tiles straight to LDS, accumulators held in AGPRs, 5.78;
 // one MFMA a step with vector work under it 4.35; equal work per CU 3.62;
 // prediction keys by single waves 3.41.  Shorter sequences are bound by
-// latency: 1 x 2048 (16/8 heads) 183 us, 1 x 256 (4/2 heads of 64) 32 us.
+// latency: 1 x 2048 (16/8 heads) 163 us, 1 x 256 (4/2 heads of 64) 28.5 us.
 #include <algorithm>
 #include <initializer_list>
 
@@ -77,7 +77,7 @@ struct BwdArgs {
   uint16_t* dk;
   uint16_t* dv;
   float* ld;              // [n_seq, Hq, 2, T, 2, 32]: -lse (log2 units), -D
-  float* part;            // [2 W][2 (dk, dv)][256 keys][D] of cut tiles
+  float* part;            // [2 W] pieces of cut tiles: see Piece
   int n_seq, L, block, Hq, Hkv, G, T;
   int4* cuts;             // [W + 1]: see Cut
   int W;                  // workgroups of dkv_kernel
@@ -161,7 +161,9 @@ struct Reader {
 // Loads of a pair of tiles (32 rows of two arrays of the same row stride)
 // straight into LDS: of four waves two take the first array, two the second.
 // kCount load instructions per wave; rows past the last one re-read it.
-template <int D>
+// kOneRow: one register for the rows of all u, whose sums are then made at
+// every load.
+template <int D, bool kOneRow>
 struct PairLoader {
   using T = RowTile<D>;
   static constexpr int kCount = 2 * T::groups / kWaves;
@@ -182,8 +184,10 @@ struct PairLoader {
   // left rows from there to the last one; dst: bytes from lds0 to the pair
   __device__ __forceinline__ void load(int u, int64_t o, int left,
                                        uint32_t dst) const {
+    int r = row;
+    if (kOneRow) asm volatile("" : "+v"(r));
     load_to_lds16<false>(buffer_rsrc(src + o, 31 * stride + 2 * D),
-                         min(row + u * T::per_group * stride,
+                         min(r + u * T::per_group * stride,
                              min(left, kRows - 1) * stride) +
                              chunk,
                          lds + dst + u * T::group_bytes);
@@ -268,6 +272,26 @@ __device__ __forceinline__ int lane_here() {
 // 16 + 4 n cycles: four fit, or an exponential and two).
 __device__ __forceinline__ void step() { __builtin_amdgcn_sched_barrier(0); }
 
+// Sixteen columns 32 m + 16 j .. of the gradient of a lane's row, times scale,
+// from elements 8 j .. 8 j + 7 of its accumulator: half-waves hold four of
+// every eight columns each; after the exchange a lane has eight together.
+__device__ __forceinline__ void store_row(uint16_t* row, int m, int j, int hf,
+                                          const floatx16_t& acc, float scale) {
+  bf16x8_t v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(acc[8 * j + e] * scale);
+  const u32x4_t x = __builtin_bit_cast(u32x4_t, v);
+  u32x4_t y;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const auto z =
+        __builtin_amdgcn_permlane32_swap(x[e], x[2 + e], false, false);
+    y[e] = z[0];
+    y[2 + e] = z[1];
+  }
+  *reinterpret_cast<u32x4_t*>(row + 32 * m + 16 * j + 8 * hf) = y;
+}
+
 // The accumulators of the last mfma_acc() are written (18 wait states).
 template <int N>
 __device__ __forceinline__ void drain(floatx16_t (&acc)[N]) {
@@ -285,14 +309,20 @@ __device__ __forceinline__ void drain(floatx16_t (&acc)[N]) {
 // tile's end moves there, one inside a tile leaves two workgroups partial sums
 // of it, which a last kernel adds up in order.
 // ---------------------------------------------------------------------------
-constexpr int kTileCost = 4;     // a tile's fixed work, in items
+// Work in items of memory keys, from the clock at each part of 1 x 2048 tokens
+// (16/8 heads of 128): an item 1.9 us, a tile's start and end 5 + 4; prediction
+// keys, each wave its own tiles, 2.7 an item (1 / kPredMore more), 6 + 5.  With
+// 4 for every tile and equal items the slowest workgroup took 117 us where the
+// mean was 87.
+constexpr int kTileCost = 5, kPredTileCost = 7, kPredMore = 2;
 constexpr int kSnap = 3;         // items: no cut nearer to a tile's end
 
 // The key tile at position p of the list.
 struct KeyTile {
   int stream, j0;
   int t_hi, t_mid;               // memory keys: both streams see them from row
-  int items;                     // tile t_mid on, memory rows alone before
+                                 // tile t_mid on, memory rows alone before
+  int items, fixed, cost;        // cost: of the tile and of its items
 };
 
 __host__ __device__ inline int key_list(int L) {
@@ -316,6 +346,10 @@ __host__ __device__ inline KeyTile key_tile(int L, int block, int G, int p) {
   x.items = (p & 1) && other == i ? 0
             : x.stream            ? own * G
                        : ((T - x.t_mid) * 2 + (x.t_mid - x.j0 / kRows)) * G;
+  x.fixed = x.stream ? kPredTileCost : kTileCost;
+  x.cost = x.items == 0 ? 0
+                        : x.fixed + (x.stream ? x.items + x.items / kPredMore
+                                              : x.items);
   return x;
 }
 
@@ -338,15 +372,11 @@ __device__ inline Cut cut_at(const BwdArgs& a, int w) {
   const int64_t raw = static_cast<int64_t>(a.group_cost) * groups * w / a.W;
   int g = static_cast<int>(raw / a.group_cost);
   const int x = static_cast<int>(raw - static_cast<int64_t>(g) * a.group_cost);
-  int base = 0, p = 0, off = 0, cost = 0;
+  int base = 0, p = 0, off = 0;
   for (int p0 = 0; p0 < list; p0 += kWave) {
     const int lp = p0 + lane_id();
-    int c = 0;
-    if (lp < list) {
-      c = key_tile(a.L, a.block, a.G, lp).items;
-      if (c) c += kTileCost;
-    }
-    int sum = c;
+    int sum = lp < list ? key_tile(a.L, a.block, a.G, lp).cost : 0;
+    const int c = sum;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
       const int y = __shfl_up(sum, o);
@@ -355,17 +385,18 @@ __device__ inline Cut cut_at(const BwdArgs& a, int w) {
     const uint64_t past = ballot(base + sum > x);
     if (past) {
       const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
-      cost = __builtin_amdgcn_readlane(c, l);
-      off = x - base - (__builtin_amdgcn_readlane(sum, l) - cost);
+      off = x - base - __builtin_amdgcn_readlane(sum - c, l);
       p = p0 + l;
       break;
     }
     base += __builtin_amdgcn_readlane(sum, kWave - 1);
   }
-  Cut r{g, p, off - kTileCost};
+  const KeyTile kt = key_tile(a.L, a.block, a.G, p);
+  Cut r{g, p, off - kt.fixed};
+  if (kt.stream && r.item > 0) r.item -= r.item / (kPredMore + 1);
   if (r.item < kSnap) {
     r.item = 0;
-  } else if (cost - off < kSnap) {
+  } else if (kt.items - r.item < kSnap) {
     r.item = 0;
     if (++r.p == list) {
       r.p = 0;
@@ -407,7 +438,7 @@ void dq_kernel(BwdArgs a) {
   constexpr int NK = D / 16, NM = D / 32;
   using T = RowTile<D>;
   constexpr int kPair = 2 * T::bytes;
-  constexpr int kLoads = PairLoader<D>::kCount;
+  constexpr int kLoads = PairLoader<D, false>::kCount;
   __shared__ __attribute__((aligned(1024))) char smem[kDqSlots * kPair];
   const int groups = (a.T * a.G + kWaves - 1) / kWaves;
   int wg = blockIdx.x;
@@ -438,7 +469,7 @@ void dq_kernel(BwdArgs a) {
   // memory keys that all of the wave's rows see
   const int full = stream ? p0 / a.block * a.block : p0 + 1;
   const int64_t kv0 = (static_cast<int64_t>(sq) * 2 * a.L * a.Hkv + kvh) * D;
-  const PairLoader<D> loader(a.k + kv0, a.v + kv0, a.Hkv * D, wave,
+  const PairLoader<D, false> loader(a.k + kv0, a.v + kv0, a.Hkv * D, wave,
                              lds_address(smem));
   // the tile that is loaded next, and its first key's row
   int ahead = 0, ahead_p = n_mem == 0 ? a.L + own0 * kRows : 0;
@@ -569,13 +600,20 @@ void dq_kernel(BwdArgs a) {
 #pragma unroll
   for (int m = 0; m < NM; ++m)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      u16x4_t x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = f32_to_bf16(acc[m][4 * g + e] * a.scale);
-      *reinterpret_cast<u16x4_t*>(dst + 32 * m + 8 * g + 4 * hf) = x;
-    }
+    for (int j = 0; j < 2; ++j) store_row(dst, m, j, hf, acc[m], a.scale);
 }
+
+// Partial sums of one tile, float4 by float4 as the waves' lanes hold them (a
+// lane's keys are rows of memory apart, its own order is whole lines):
+// [wave][dk, dv][b][m][g][lane], dk without the scale.
+template <int D>
+struct Piece {
+  static constexpr int per_wave = 2 * kOwn * D / 4;
+  static constexpr int n = kWaves * per_wave;
+  __device__ static __forceinline__ int64_t at(int piece, int wave) {
+    return static_cast<int64_t>(piece) * n + wave * per_wave;
+  }
+};
 
 // dk and dv: workgroup w walks stretch w; workgroups of one XCD take
 // neighbouring stretches, of kv heads whose rows then stay in its L2.
@@ -673,8 +711,9 @@ void dkv_kernel(BwdArgs a) {
   };
   const uint32_t lds0 = lds_address(smem);
   const int64_t q0 = (static_cast<int64_t>(sq) * 2 * a.L * a.Hq + kvh * a.G) * D;
-  const PairLoader<D> loader(a.q + q0, a.dout + q0, a.Hq * D, wave, lds0);
-  constexpr int kLoads = PairLoader<D>::kCount + 1;
+  const PairLoader<D, true> loader(a.q + q0, a.dout + q0, a.Hq * D, wave,
+                                   lds0);
+  constexpr int kLoads = PairLoader<D, true>::kCount + 1;
   const float* ld0 = a.ld + (static_cast<int64_t>(sq) * a.Hq + kvh * a.G) * 2 *
                                 a.T * 2 * kRows;
   // the item that is loaded next
@@ -690,7 +729,7 @@ void dkv_kernel(BwdArgs a) {
   };
   auto fetch = [&](int u, int slot) {
     const int left = a.L - 1 - min(ahead.t, a.T - 1) * kRows;
-    if (u < PairLoader<D>::kCount)
+    if (u < PairLoader<D, true>::kCount)
       loader.load(u, rows_at(), left, slot * kSlot);
     else
       // every wave the same 256 bytes, so that all wait for as many loads
@@ -913,19 +952,13 @@ void dkv_kernel(BwdArgs a) {
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          u16x4_t x, y;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[e] = f32_to_bf16(dk[b][m][4 * g + e] * a.scale);
-            y[e] = f32_to_bf16(dv[b][m][4 * g + e]);
-          }
-          *reinterpret_cast<u16x4_t*>(a.dk + o + 32 * m + 8 * g + 4 * hf) = x;
-          *reinterpret_cast<u16x4_t*>(a.dv + o + 32 * m + 8 * g + 4 * hf) = y;
+        for (int j = 0; j < 2; ++j) {
+          store_row(a.dk + o, m, j, hf, dk[b][m], a.scale);
+          store_row(a.dv + o, m, j, hf, dv[b][m], 1.f);
         }
     } else {
-      float* o = a.part + (static_cast<int64_t>(2 * w + (it0 == 0)) * 2 *
-                               kKeysPerWg + key - j0) * D;
+      floatx4_t* o = reinterpret_cast<floatx4_t*>(a.part) +
+                     Piece<D>::at(2 * w + (it0 == 0), (kw0 - j0) / kOwn) + l;
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
@@ -933,12 +966,11 @@ void dkv_kernel(BwdArgs a) {
           floatx4_t x, y;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            x[e] = dk[b][m][4 * g + e] * a.scale;
+            x[e] = dk[b][m][4 * g + e];
             y[e] = dv[b][m][4 * g + e];
           }
-          *reinterpret_cast<floatx4_t*>(o + 32 * m + 8 * g + 4 * hf) = x;
-          *reinterpret_cast<floatx4_t*>(o + kKeysPerWg * D + 32 * m + 8 * g +
-                                        4 * hf) = y;
+          o[((b * NM + m) * 4 + g) * kWave] = x;
+          o[(((2 + b) * NM + m) * 4 + g) * kWave] = y;
         }
     }
   }
@@ -956,36 +988,36 @@ __global__ __launch_bounds__(kThreads) void join_kernel(BwdArgs a) {
   int n = 1;
   while (w + n < a.W && read_cut(a, w + n).shares(c)) ++n;
   const KeyTile kt = key_tile(a.L, a.block, a.G, c.p);
-  const int keys = min(kKeysPerWg, a.L - kt.j0);
   const int kvh = c.g / a.n_seq, sq = c.g - kvh * a.n_seq;
-  constexpr int64_t kPiece = 2 * kKeysPerWg * D;
-  const float* first = a.part + (2 * w - 1) * kPiece;
-  const float* others = a.part + 2 * w * kPiece;
-  for (int i = blockIdx.y * kThreads + threadIdx.x; i < 2 * keys * (D / 4);
+  const floatx4_t* part = reinterpret_cast<const floatx4_t*>(a.part);
+  const floatx4_t* first = part + Piece<D>::at(2 * w - 1, 0);
+  const floatx4_t* others = part + Piece<D>::at(2 * w, 0);
+  for (int i = blockIdx.y * kThreads + threadIdx.x; i < Piece<D>::n;
        i += gridDim.y * kThreads) {
-    const int which = i >= keys * (D / 4) ? 1 : 0;
-    const int e0 = (i - which * keys * (D / 4)) * 4;
-    const int64_t at = static_cast<int64_t>(which) * kKeysPerWg * D + e0;
-    floatx4_t s = *reinterpret_cast<const floatx4_t*>(first + at);
+    const int lane = i % kWave, g = i / kWave % 4;
+    const int m = i / (4 * kWave) % (D / 32), x2 = i / (2 * kWave * D / 16);
+    const int key = kt.j0 + x2 / 4 * kOwn + x2 % 2 * 32 + lane % 32;
+    if (key >= a.L) continue;
+    floatx4_t s = first[i];
     // in order, four loads under way
     for (int k0 = 0; k0 < n; k0 += 4) {
       floatx4_t x[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        x[k] = *reinterpret_cast<const floatx4_t*>(
-            others + 2 * min(k0 + k, n - 1) * kPiece + at);
+        x[k] = others[Piece<D>::at(2 * min(k0 + k, n - 1), 0) + i];
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] += k0 + k < n ? x[k][e] : 0.f;
     }
+    const float scale = x2 & 2 ? 1.f : a.scale;
     u16x4_t o;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = f32_to_bf16(s[e]);
+    for (int e = 0; e < 4; ++e) o[e] = f32_to_bf16(s[e] * scale);
     *reinterpret_cast<u16x4_t*>(
-        (which ? a.dv : a.dk) +
-        (((static_cast<int64_t>(sq) * 2 + kt.stream) * a.L + kt.j0 + e0 / D) *
-             a.Hkv + kvh) * D + e0 % D) = o;
+        (x2 & 2 ? a.dv : a.dk) +
+        (((static_cast<int64_t>(sq) * 2 + kt.stream) * a.L + key) * a.Hkv +
+         kvh) * D + 32 * m + 8 * g + lane / 32 * 4) = o;
   }
 }
 
@@ -1012,14 +1044,13 @@ bool bwd_plan(int n_seq, int L, int block, int Hq, int Hkv, int D,
                      ((static_cast<int64_t>(p->T) * G + kWaves - 1) / kWaves);
   int64_t cost = 0;
   for (int i = 0; i < key_list(L); ++i) {
-    const int items = key_tile(L, block, G, i).items;
-    if (items) cost += items + kTileCost;
+    cost += key_tile(L, block, G, i).cost;
   }
   if (dq > 0x7fffffffll || cost > 0x7fffffffll) return false;
   // One workgroup per CU, but none with less than six items' work.  (At least
   // 16 items, longer walks but fewer partial sums: 1 x 256 tokens, 4/2 heads of
-  // 64, dk and dv 36 us against 19; 1 x 1024, 8/2 heads of 128, 60 against 35
-  // with a join of 7 against 15)
+  // 64, dk and dv 28 us against 15; 1 x 1024, 8/2 heads of 128, 42 against 28
+  // with a join of 8 against 16; eight items tie)
   const int64_t all = cost * n_seq * Hkv;
   p->W = static_cast<int>(std::min<int64_t>(256, std::max<int64_t>(1, all / 6)));
   p->group_cost = static_cast<int>(cost);
