@@ -1013,7 +1013,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(BwdArgs a) {
     const float scale = x2 & 2 ? 1.f : a.scale;
     u16x4_t o;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = f32_to_bf16(s[e] * scale);
+    for (int e = 0; e < 4; ++e) o[e] = to_bf16(s[e] * scale);
     *reinterpret_cast<u16x4_t*>(
         (x2 & 2 ? a.dv : a.dk) +
         (((static_cast<int64_t>(sq) * 2 + kt.stream) * a.L + key) * a.Hkv +

@@ -35,6 +35,11 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
   return static_cast<uint16_t>(u >> 16);
 }
 
+// The same by the conversion instruction.
+__device__ __forceinline__ uint16_t to_bf16(float v) {
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+}
+
 __device__ __forceinline__ uint64_t ballot(bool p) {
   return __ballot(p);
 }

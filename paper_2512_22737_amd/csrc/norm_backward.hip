@@ -313,8 +313,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(
         dgb[0][e] += isq ? gb : 0.f;
         dga[1][e] += isq ? 0.f : ga;
         dgb[1][e] += isq ? 0.f : gb;
-        ol[e] = f32_to_bf16(r * (za[e] * bf16_to_f32(gl[e]) - x[e] * k));
-        oh[e] = f32_to_bf16(r * (zb[e] * bf16_to_f32(gh[e]) - y[e] * k));
+        ol[e] = to_bf16(r * (za[e] * bf16_to_f32(gl[e]) - x[e] * k));
+        oh[e] = to_bf16(r * (zb[e] * bf16_to_f32(gh[e]) - y[e] * k));
       }
       *reinterpret_cast<u16x8_t*>(a.dqkv + o) = ol;
       *reinterpret_cast<u16x8_t*>(a.dqkv + o + half) = oh;

@@ -15,7 +15,7 @@
 // large gradient does not stay there, the row's rest does).  4096 x 151936
 // fp32 1.03 ms, 4.8 TB/s, where a large copy reaches 5.1 (one element at a
 // time in two passes 1.85 ms); 1000 x 32003 bf16, half of the rows without
-// loss, 28 us; 32 x 1024 8 us, one launch.
+// loss, 24 us; 32 x 1024 8 us, one launch.
 #include "common.h"
 #include "wedlm_train.h"
 
@@ -73,9 +73,9 @@ struct Elem<uint16_t> {
   static constexpr int n = 8;
   typedef u16x8_t chunk;
   __device__ static float get(const chunk& c, int e) { return bf16_to_f32(c[e]); }
-  __device__ static void set(chunk& c, int e, float v) { c[e] = f32_to_bf16(v); }
+  __device__ static void set(chunk& c, int e, float v) { c[e] = to_bf16(v); }
   __device__ static float get(const uint16_t* p) { return bf16_to_f32(*p); }
-  __device__ static void set(uint16_t* p, float v) { *p = f32_to_bf16(v); }
+  __device__ static void set(uint16_t* p, float v) { *p = to_bf16(v); }
 };
 
 // A stretch of a row: elements up to the first 16-byte boundary, whole
