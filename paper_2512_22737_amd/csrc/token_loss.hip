@@ -413,8 +413,9 @@ __global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
 // Elements of a row's slices, or V (one slice).  Rows of more than 16384 chunks
 // (262144 bytes) are cut when they are fewer than 128, so that there are about
 // 512 workgroups, of 1024 chunks each at least.  In us, whole rows and slices:
-// 8 x 151936 fp32 22.9, 9.7, bf16 27.4, 9.9; 64 x 151936 25.4, 22.6 and 27.8,
-// 18.0; 200 x 151936 51.6, 59 and 34.8, 36.6; 64 x 32000 fp32 8.8, 10.4.
+// 8 x 151936 fp32 22.9, 9.7, bf16 22.6, 9.5; 64 x 151936 25.4, 22.6 and 23.0,
+// 16.4; 128 x 151936 bf16 25.4, 26.0; 200 x 151936 51.6, 59 and 29.7, 35.6;
+// 64 x 32000 fp32 8.8, 10.4.
 int slice_len(int R, int V, int per_chunk) {
   const int64_t chunks = V / per_chunk;
   if (R >= 128 || chunks <= 4 * kSmallChunks) return V;
@@ -470,13 +471,13 @@ int launch(const LossArgs& a0, hipStream_t st) {
   }
   // 256 threads as long as they hold the row: 1000 x 8000 fp32 10.3 us against
   // 20.8 with 1024; four chunks each where those do (4000 x 1000 9.6, 15.3).
-  // Few rows of more than that have CUs to spare: 64 x 32000 bf16 13.5 with
-  // 256, 9.6 with 1024
+  // Up to a row per CU 1024 are as many as the row has use for: 256 x 32000 bf16
+  // 12.9 with 256, 9.6 with 1024; 384 x 32000 14.8, 17.1
   const int chunks = a.V / Elem<T>::n;
   if (chunks <= kSmallThreads * 4)
     return launch_rows<T>(token_loss_kernel<T, kSmallThreads, 4>,
                           kSmallThreads, a, st);
-  if (chunks <= kSmallChunks && a.R >= 128)
+  if (chunks <= kSmallChunks && a.R > 256)
     return launch_rows<T>(token_loss_kernel<T, kSmallThreads, kSmallHeld>,
                           kSmallThreads, a, st);
   return launch_rows<T>(token_loss_kernel<T, 1024, 19>, 1024, a, st);

@@ -53,7 +53,8 @@ def _check(x, t, w, V, loss, d, dtype):
 @pytest.mark.parametrize("R,V,stride", [
     (1, 1, 1), (2, 3, 3), (5, 7, 8), (33, 1000, 1000), (9, 1021, 1021),
     (64, 4096, 4160), (3, 32003, 32064), (2, 151936, 151936),
-    (7, 50257, 50257), (700, 513, 520), (600, 20000, 20000)])
+    (7, 50257, 50257), (700, 513, 520), (600, 20000, 20000),
+    (300, 12001, 12004)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_token_loss(R, V, stride, dtype):
     from paper_2512_22737_amd import wedlm
