@@ -406,9 +406,10 @@ __device__ inline Cut cut_at(const BwdArgs& a, int w) {
   return r;
 }
 
-// The cuts are found once, by dq_kernel's workgroups, for the kernels after it.
+// The cuts are found once, by dq_kernel's workgroups, the shortest walks first,
+// at their ends, for the kernels after it.
 __device__ inline void write_cuts(const BwdArgs& a) {
-  for (int w = blockIdx.x; w <= a.W; w += gridDim.x) {
+  for (int w = gridDim.x - 1 - blockIdx.x; w <= a.W; w += gridDim.x) {
     const Cut c = cut_at(a, w);
     if (lane_id() == 0) a.cuts[w] = make_int4(c.g, c.p, c.item, 0);
   }
@@ -520,7 +521,6 @@ void dq_kernel(BwdArgs a) {
 #pragma unroll
   for (int m = 0; m < NM; ++m) acc[m] = floatx16_t{};
 
-  if (wave == 0) write_cuts(a);
   // take delivery of the rows: no wait for them in the loop
 #pragma unroll
   for (int kk = 0; kk < NK; ++kk)
@@ -595,6 +595,7 @@ void dq_kernel(BwdArgs a) {
   } while (++i < n);
   wait_vmcnt<0>();      // surplus loads land before the LDS is given up
   drain(acc);
+  if (wave == 0) write_cuts(a);
   if (!live || p >= a.L) return;
   uint16_t* dst = a.dq + o;
 #pragma unroll
