@@ -9,7 +9,7 @@
 // Bound by HBM: every array is passed over once, rows stay in registers between
 // their sums and their gradients.  RMSNorm 32768 x 4096 338-346 us, 5.5 TB/s
 // (a large copy reaches 5.1), 8193 x 2560 without a residual gradient 47 us,
-// 4.4 TB/s; q/k norm with RoPE of 32768 rows of 32/8 heads of 128 233 us,
+// 4.4 TB/s; q/k norm with RoPE of 32768 rows of 32/8 heads of 128 231 us,
 // 4.9 TB/s.  Few rows are bound by the two launches, 10 to 13 us.
 #include <algorithm>
 #include <cmath>
@@ -321,21 +321,24 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_backward_kernel(
     }
   }
   if (!a.part) return;
-  // lanes of equal j0, then the waves
+  // lanes of equal j0 (all values a step at a time: the kernel on 512 rows of
+  // 4/2 heads of 64 7.7 us, one value after the other 10.4), then the waves
+  for (int off = per_head; off < kWave; off <<= 1)
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float va = dga[s][e], vb = dgb[s][e];
-      for (int off = per_head; off < kWave; off <<= 1) {
-        va += __shfl_xor(va, off);
-        vb += __shfl_xor(vb, off);
+      for (int e = 0; e < 8; ++e) {
+        dga[s][e] += __shfl_xor(dga[s][e], off);
+        dgb[s][e] += __shfl_xor(dgb[s][e], off);
       }
-      if (lane_id() < per_head) {
-        s_dg[threadIdx.x / kWave][s][j0 + e] = va;
-        s_dg[threadIdx.x / kWave][s][half + j0 + e] = vb;
+  if (lane_id() < per_head)
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s_dg[threadIdx.x / kWave][s][j0 + e] = dga[s][e];
+        s_dg[threadIdx.x / kWave][s][half + j0 + e] = dgb[s][e];
       }
-    }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * a.D; i += kThreads) {
     const int s = i / a.D, d = i % a.D;
@@ -361,7 +364,7 @@ int norm_parts(int M, int Hd) { return std::min(M, Hd > 4096 ? 512 : 1024); }
 
 // Rows that a workgroup of the q/k kernel takes at once: four where that
 // leaves a workgroup per CU (1024 rows of 32/8 heads of 128 24 us with one,
-// 19 with four; 512 rows 14.4, 17.0; 32768 rows 304, 233).
+// 19 with four; 512 rows 14.4, 17.0; 32768 rows 304, 231).
 constexpr int kQkRows = 4;
 int qk_rows(int M) { return M >= kQkRows * 256 ? kQkRows : 1; }
 int qk_parts(int M) {
