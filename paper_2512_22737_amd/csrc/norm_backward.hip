@@ -9,8 +9,8 @@
 // Bound by HBM: every array is passed over once, rows stay in registers between
 // their sums and their gradients.  RMSNorm 32768 x 4096 338-346 us, 5.5 TB/s
 // (a large copy reaches 5.1), 8193 x 2560 without a residual gradient 47 us,
-// 4.4 TB/s; q/k norm with RoPE of 32768 rows of 32/8 heads of 128 231 us,
-// 4.9 TB/s.  Few rows are bound by the two launches, 10 to 13 us.
+// 4.4 TB/s; q/k norm with RoPE of 32768 rows of 32/8 heads of 128 229 us,
+// 4.9 TB/s.  Few rows are bound by the two launches, 8 to 12 us.
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -23,7 +23,9 @@ using namespace wedlm;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kQkParts = 2048;    // workgroups of the q/k kernel, at most
+// Workgroups of the q/k kernel, at most: four per CU (32768 rows of 16/2 heads
+// of 64 54 us; 512 workgroups 73, 2048 59)
+constexpr int kQkParts = 1024;
 
 // Sum over the wave.
 __device__ __forceinline__ float wave_sum(float v) {
@@ -222,9 +224,8 @@ __global__ __launch_bounds__(kSumThreads) void sum_parts_kernel(
 // rotation pairs of one head of one row, the D/16 items of a head sit on
 // neighbouring lanes.  A thread meets the same pairs j0 .. j0+7 of D in every
 // item (the strides are multiples of a head's items), so the gains' gradients
-// stay in its registers until the end.  Four rows at once give every thread
-// an angle (64 bits: positions are far) and enough items to hide the loads;
-// one, where there are fewer rows than that fills the card with.
+// stay in its registers until the end.  Several rows at once give every
+// thread an angle (64 bits: positions are far) and items to hide the loads.
 constexpr int kMaxHalf = 64;
 
 struct QkArgs {
@@ -362,14 +363,20 @@ bool norm_ok(int M, int Hd) {
 }
 int norm_parts(int M, int Hd) { return std::min(M, Hd > 4096 ? 512 : 1024); }
 
-// Rows that a workgroup of the q/k kernel takes at once: four where that
-// leaves a workgroup per CU (1024 rows of 32/8 heads of 128 24 us with one,
-// 19 with four; 512 rows 14.4, 17.0; 32768 rows 304, 231).
-constexpr int kQkRows = 4;
-int qk_rows(int M) { return M >= kQkRows * 256 ? kQkRows : 1; }
-int qk_parts(int M) {
-  const int groups = (M - 1) / qk_rows(M) + 1;
-  return groups < kQkParts ? groups : kQkParts;
+// Rows that a workgroup of the q/k kernel takes at once.  Four, so that its
+// threads have work (512 rows of 4/2 heads of 64, 24 items each, 7.8 us; one
+// row 9.0), but one where four have more items than threads and there is not a
+// workgroup per CU (512 rows of 32/8 heads of 128, 320 items, 10.7 us; four
+// 13.4; 1024 rows 18.7, 15.5; 32768 rows 282, 229).  Eight of few items, two
+// workgroups per CU (4096 rows of 4/2 heads of 64 10.4 us; four 14.0; 32768 of
+// 16/2 49.6, 54.5; 8192 of 32/8 heads of 128 59.7, 57.5).
+int qk_rows(int M, int items) {
+  if (items <= 96 && M >= 8 * 512) return 8;
+  return M >= 4 * 256 || 4 * items <= kThreads ? 4 : 1;
+}
+int qk_items(int Hq, int Hkv, int D) { return (Hq + Hkv) * (D / 16); }
+int qk_parts(int M, int items) {
+  return std::min((M - 1) / qk_rows(M, items) + 1, kQkParts);
 }
 
 // 64 columns per workgroup read 256 bytes together (1024 parts of 4096 5.6 us;
@@ -430,7 +437,8 @@ extern "C" size_t wedlm_qk_norm_rope_backward_workspace_size(int32_t M,
                                                              int32_t Hkv,
                                                              int32_t D) {
   if (!qk_ok(M, Hq, Hkv, D)) return 0;
-  return static_cast<size_t>(qk_parts(M)) * 2 * D * sizeof(float);
+  return static_cast<size_t>(qk_parts(M, qk_items(Hq, Hkv, D))) * 2 * D *
+         sizeof(float);
 }
 
 extern "C" int wedlm_qk_norm_rope_backward(
@@ -454,13 +462,12 @@ extern "C" int wedlm_qk_norm_rope_backward(
   QkArgs a{qkv, q_gain, k_gain, pos_ids, dq, dk, dv, dqkv, part, M, Hq, Hkv,
            D, eps, {}};
   for (int j = 0; j < D / 2; ++j) a.omega[j] = std::pow(rope_theta, -2.0 * j / D);
-  const int parts = qk_parts(M);
-  if (qk_rows(M) > 1)
-    hipLaunchKernelGGL(qk_norm_rope_backward_kernel<kQkRows>, dim3(parts),
-                       dim3(kThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL(qk_norm_rope_backward_kernel<1>, dim3(parts),
-                       dim3(kThreads), 0, st, a);
+  const int items = qk_items(Hq, Hkv, D), parts = qk_parts(M, items);
+  const int rows = qk_rows(M, items);
+  auto k = rows == 8   ? qk_norm_rope_backward_kernel<8>
+           : rows == 4 ? qk_norm_rope_backward_kernel<4>
+                       : qk_norm_rope_backward_kernel<1>;
+  hipLaunchKernelGGL(k, dim3(parts), dim3(kThreads), 0, st, a);
   WEDLM_LAUNCH_CHECK();
   return gains ? sum_parts(part, parts, D, D, dq_gain, dk_gain, st) : WEDLM_OK;
 }

@@ -87,7 +87,8 @@ def test_rmsnorm_backward_in_place_and_without_gain():
 @pytest.mark.parametrize("M,Hq,Hkv,D,far", [
     (1, 1, 1, 64, 10), (3, 4, 2, 64, 1000), (9, 28, 4, 128, 40000),
     (1100, 4, 4, 64, 1100), (520, 32, 8, 128, 2000000), (2, 40, 1, 128, 5),
-    (5, 100, 3, 64, 9), (513, 1, 3, 128, 300)])
+    (5, 100, 3, 64, 9), (513, 1, 3, 128, 300),
+    (4099, 4, 2, 64, 4099)])
 def test_qk_norm_rope_backward(M, Hq, Hkv, D, far):
     from paper_2512_22737_amd import wedlm
     print(f"qk norm rope backward {M} {Hq}/{Hkv}x{D}", flush=True)
