@@ -354,14 +354,19 @@ bool aligned(std::initializer_list<const void*> ps, int bytes) {
   return true;
 }
 
-// Workgroups of the RMSNorm kernel, each with its part of the gain's gradient:
-// four per CU for rows of up to 4096 (32768 x 4096 346 us; 512 workgroups 416,
-// 2048 370), two for longer ones, whose registers hold no more (4096 x 8192
-// 111 us; 1024 workgroups 119).
 bool norm_ok(int M, int Hd) {
   return M >= 1 && Hd >= 4 && Hd <= 1 << 20 && Hd % 4 == 0;
 }
-int norm_parts(int M, int Hd) { return std::min(M, Hd > 4096 ? 512 : 1024); }
+// Workgroups of the RMSNorm kernel, each with its part of the gain's gradient:
+// four per CU for many rows of up to 4096 (32768 x 4096 249 us in a graph; 512
+// workgroups 279, 2048 276), two for longer ones, whose registers hold no more
+// (4096 x 8192 78 us; 2048 workgroups 103), and two rows each where they are
+// few, for fewer parts to add up (1024 x 4096 15.5 us; a row each 18.7; 512 x
+// 16384 31.9, 40.5; 2048 x 1024 10.3 with 512 workgroups, 11.2 with 1024).
+int norm_parts(int M, int Hd) {
+  const int most = M < 4096 || Hd > 4096 ? 512 : 1024;
+  return std::min({M, most, std::max(256, M - M / 2)});
+}
 
 // Rows that a workgroup of the q/k kernel takes at once.  Four, so that its
 // threads have work (512 rows of 4/2 heads of 64, 24 items each, 7.8 us; one
