@@ -94,7 +94,8 @@ def test_accumulators_are_read_after_a_wait(kernels):
         for l in lines[max(i for i, _ in loop) + 1:]:
             if re.search(r"s_nop 15", l):
                 waited = True
-            m = re.search(r"v_accvgpr_read\S* \S+ a(\d+)", l)
+            m = (re.search(r"v_accvgpr_read\S* \S+ a(\d+)", l) or
+                 re.search(r"(?:store|write)\S* .*\ba\[?(\d+)", l))
             if m and int(m.group(1)) in regs:
                 assert waited, (name, l)
                 break
