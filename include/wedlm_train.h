@@ -82,9 +82,9 @@ size_t wedlm_dual_stream_attn_backward_workspace_size(int32_t n_seq, int32_t L,
  * ceil(L / 32) * Hq/Hkv < 2^29.  bf16 arrays and the workspace on 16-byte
  * boundaries (WEDLM_E_ARG).
  * workspace: wedlm_dual_stream_attn_backward_workspace_size() bytes (each
- * row's normaliser and product of out and dout; fp32 sums of keys whose work
- * is split over workgroups); its contents on entry do not matter.  Two calls
- * that overlap in time must not share a workspace.
+ * row's normaliser and sum of P dP; fp32 sums of keys whose work is split over
+ * workgroups); its contents on entry do not matter.  Two calls that overlap in
+ * time must not share a workspace.
  */
 int wedlm_dual_stream_attn_backward(
     const uint16_t* q, const uint16_t* k, const uint16_t* v,

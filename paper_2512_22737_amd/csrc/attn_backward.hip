@@ -30,11 +30,11 @@
 // operand is read from the same LDS tile by columns (ds_read_b64_tr_b16).
 //
 // Roundings: P and dS to bf16 for the second products, as the forward rounds
-// P; D from the forward's bf16 output; everything else, all sums among it,
-// fp32.  Rounding dS adds as much as rounding the result does (0.17% of a
-// gradient's norm), D's a third to a half of that where rows see few keys:
-// 0.24-0.27% together, against 0.17% for an fp32 gradient rounded once.  In
-// wider operands the second products would run at a fraction of the rate.
+// P; D from the forward's bf16 output, but exact where rows see few keys (see
+// kExactRows); everything else, all sums among it, fp32.  Rounding dS adds as
+// much as rounding the result does (0.17% of a gradient's norm): 0.23-0.24%
+// together.  In wider operands the second products would run at a fraction of
+// the rate.
 //
 // Bound by the MFMAs, and these by the card's power: 4 x 4096 tokens (32/8
 // heads of 128) 3.37 ms, 816 TFLOP/s of the five products and 1.14 PFLOP/s of
@@ -44,7 +44,7 @@
 // spills, 31.2 ms; tiles straight to LDS, accumulators held in AGPRs, 5.78;
 // one MFMA a step with vector work under it 4.35; equal work per CU 3.62;
 // prediction keys by single waves 3.41.  Shorter sequences are bound by
-// latency: 1 x 2048 (16/8 heads) 163 us, 1 x 256 (4/2 heads of 64) 28.5 us.
+// latency: 1 x 2048 (16/8 heads) 160 us, 1 x 256 (4/2 heads of 64) 28.6 us.
 #include <algorithm>
 #include <initializer_list>
 
@@ -432,6 +432,14 @@ __device__ __forceinline__ Cut read_cut(const BwdArgs& a, int w) {
 // of 128) 1.53 ms against 1.47, 1 x 2048 (16/8) 92 us against 68.
 constexpr int kDqSlots = 4;
 
+// D from out carries out's rounding, which counts where rows see few keys:
+// gradients of 16 to 64 tokens (N(0,1) inputs) were off by 1.5 to 1.8 times one
+// rounding of the result.  With the exact D of the first 64 positions it is
+// 1.38 to 1.48 at all lengths, of which 1.41 are dS's and the result's own.  The
+// walks concerned are the shortest: 1 x 64 tokens (4/2 heads of 64) 27.6 us
+// with it, 25.4 without; 1 x 256 28.6, 28.3; longer sequences the same.
+constexpr int kExactRows = 64;
+
 template <int D>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(1, 2)))
@@ -485,12 +493,15 @@ void dq_kernel(BwdArgs a) {
     ahead_p = ahead >= n_mem ? a.L + (own0 + ahead - n_mem) * kRows
                              : ahead * kRows;
   };
+  auto prime = [&]() {
 #pragma unroll
-  for (int i = 0; i < kDqSlots - 1; ++i) {
+    for (int i = 0; i < kDqSlots - 1; ++i) {
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) fetch(u, i);
-    advance();
-  }
+      for (int u = 0; u < kLoads; ++u) fetch(u, i);
+      advance();
+    }
+  };
+  prime();
 
   // the lane's row: q, dout, lse and D; it sees memory keys below lo
   // (prediction) or hi (memory), and the own stream's lo .. hi-1
@@ -511,6 +522,50 @@ void dq_kernel(BwdArgs a) {
   }
   delta += __shfl_xor(delta, 32);
   const float lse2 = a.lse[(row0 + pc) * a.Hq + head] * kLog2e;
+  const Reader<D> rd;
+  // keys of tile i that the lane's row sees
+  auto hide = [=](int i, floatx16_t& x) {
+    const bool own = i >= n_mem;
+    const int k0 = (own ? own0 + i - n_mem : i) * kRows + 8 * (lane_here() >> 5);
+    const uint32_t see =
+        rows_between((own ? lo : 0) - k0, (own || !stream ? hi : lo) - k0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = seen(see, e, x[e]);
+  };
+  // rows that see few keys: D from the probabilities, in a walk of its own
+  if (first < kExactRows) {
+    delta = 0.f;
+    for (int i = 0; i < n; ++i) {
+      // tile i has landed; everybody is done with the slot of tile i - 1
+      wait_vmcnt<0>();
+      __syncthreads();
+      if (i + kDqSlots - 1 < n) {
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) fetch(u, (i + kDqSlots - 1) % kDqSlots);
+        advance();
+      }
+      const char* kt = smem + i % kDqSlots * kPair;
+      floatx16_t s{}, dp{};
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        s = mfma(rd.rows(kt, kk), qf[kk], s);
+        dp = mfma(rd.rows(kt + T::bytes, kk), dof[kk], dp);
+      }
+      hide(i, s);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        delta += dp[e] * __builtin_amdgcn_exp2f(
+                             __builtin_fmaf(s[e], a.scale_log2, -lse2));
+    }
+    delta += __shfl_xor(delta, 32);
+    // (tiles that all fit are still where prime() put them)
+    if (n >= kDqSlots) {
+      __syncthreads();
+      ahead = 0;
+      ahead_p = n_mem == 0 ? a.L + own0 * kRows : 0;
+      prime();
+    }
+  }
   if (live && hf == 0) {
     float* ld = a.ld + ((((static_cast<int64_t>(sq) * a.Hq + head) * 2 + stream) *
                          a.T + p / kRows) * 2) * kRows + col;
@@ -527,7 +582,6 @@ void dq_kernel(BwdArgs a) {
     asm volatile("" : "+v"(qf[kk]), "+v"(dof[kk]));
   wait_vmcnt<(kDqSlots - 2) * kLoads>();
   __syncthreads();
-  const Reader<D> rd;
   constexpr int kE = 16 / NK;              // elements per step
   bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
 #pragma unroll
@@ -543,8 +597,6 @@ void dq_kernel(BwdArgs a) {
     const char* vt = kt + T::bytes;
     // A tile that this wave's rows do not see is computed all the same, P = 0:
     // the waves are in step, and a branch around the accumulators costs copies
-    const bool own = i >= n_mem;
-    const int j0 = (own ? own0 + i - n_mem : i) * kRows;
     floatx16_t s, dp;
     float w[16];
     bf16x8_t ds[2];
@@ -557,13 +609,7 @@ void dq_kernel(BwdArgs a) {
       if (kk >= 1 && kk <= kLoads) fetch(kk - 1, load_slot);
       step();
     }
-    if (own || j0 + kRows > full) {
-      const int k0 = j0 + 8 * (lane_here() >> 5);
-      const int from = own ? lo : 0, to = own || !stream ? hi : lo;
-      const uint32_t see = rows_between(from - k0, to - k0);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = seen(see, e, s[e]);
-    }
+    if (i >= n_mem || (i + 1) * kRows > full) hide(i, s);
     step();
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
