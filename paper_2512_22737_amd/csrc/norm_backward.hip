@@ -466,7 +466,12 @@ extern "C" int wedlm_qk_norm_rope_backward(
   float* part = gains ? static_cast<float*>(workspace) : nullptr;
   QkArgs a{qkv, q_gain, k_gain, pos_ids, dq, dk, dv, dqkv, part, M, Hq, Hkv,
            D, eps, {}};
-  for (int j = 0; j < D / 2; ++j) a.omega[j] = std::pow(rope_theta, -2.0 * j / D);
+  // theta^(-2 j / D) as products of two powers (off by 2^-52 at most), not one
+  // power each: they cost the host as much as a launch
+  double low[8], high[kMaxHalf / 8];
+  for (int j = 0; j < 8; ++j) low[j] = std::pow(rope_theta, -2.0 * j / D);
+  for (int j = 0; j < D / 16; ++j) high[j] = std::pow(rope_theta, -16.0 * j / D);
+  for (int j = 0; j < D / 2; ++j) a.omega[j] = high[j / 8] * low[j % 8];
   const int items = qk_items(Hq, Hkv, D), parts = qk_parts(M, items);
   const int rows = qk_rows(M, items);
   auto k = rows == 8   ? qk_norm_rope_backward_kernel<8>

@@ -782,6 +782,20 @@ def wedlm_dual_stream_attn(q, k, v, block: int, out, lse=None, workspace=None,
     _check(code, "wedlm_dual_stream_attn")
 
 
+def _workspace(workspace, device, size, *shape):
+    """A workspace's tensor (of size(*shape) bytes if none is given; the
+    library refuses a given one that is too small), address and bytes.  The
+    caller holds the tensor until its launches are enqueued: freed earlier,
+    another thread could be handed the memory for work before them."""
+    if workspace is not None:
+        return workspace, _t(workspace, "workspace", _U8), workspace.numel()
+    n = size(*shape)
+    if n == 0:           # none needed, or sizes that the library refuses
+        return None, None, 0
+    workspace = torch.empty(n, dtype=torch.uint8, device=device)
+    return workspace, workspace.data_ptr(), n
+
+
 def wedlm_dual_stream_attn_backward_workspace_size(n_seq, L, block, Hq, Hkv,
                                                    D) -> int:
     return int(_load().wedlm_dual_stream_attn_backward_workspace_size(
@@ -800,12 +814,9 @@ def wedlm_dual_stream_attn_backward(q, k, v, block: int, out, lse, dout, dq,
     L = L2 // 2
     if softmax_scale is None:
         softmax_scale = 1.0 / math.sqrt(D)
-    need = wedlm_dual_stream_attn_backward_workspace_size(n_seq, L, block, Hq,
-                                                          Hkv, D)
-    if need == 0:
-        raise WedlmError("unsupported dual-stream shape")
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    held, ws, nbytes = _workspace(
+        workspace, q.device, wedlm_dual_stream_attn_backward_workspace_size,
+        n_seq, L, block, Hq, Hkv, D)
     qs, ks = (n_seq, 2 * L, Hq, D), (n_seq, 2 * L, Hkv, D)
     code = _load().wedlm_dual_stream_attn_backward(
         _t(q, "q", _BF16, qs), _t(k, "k", _BF16, ks), _t(v, "v", _BF16, ks),
@@ -813,17 +824,8 @@ def wedlm_dual_stream_attn_backward(q, k, v, block: int, out, lse, dout, dq,
         _t(dout, "dout", _BF16, qs), n_seq, L, int(block), Hq, Hkv, D,
         float(softmax_scale), _t(dq, "dq", _BF16, qs),
         _t(dk, "dk", _BF16, ks), _t(dv, "dv", _BF16, ks),
-        _t(workspace, "workspace", _U8), workspace.numel(), _stream())
+        ws, nbytes, _stream())
     _check(code, "wedlm_dual_stream_attn_backward")
-
-
-def _workspace(workspace, need: int, device):
-    """A workspace's tensor (allocated here if none is given), address and
-    bytes.  The caller holds the tensor until its launches are enqueued: freed
-    earlier, another thread could be handed the memory for work before them."""
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    return workspace, _t(workspace, "workspace", _U8), workspace.numel()
 
 
 def wedlm_rmsnorm_backward_workspace_size(M, Hd) -> int:
@@ -840,7 +842,7 @@ def wedlm_rmsnorm_backward(x, gain, eps: float, dy, dx, dgain=None, dres=None,
     held, ws, nbytes = None, None, 0
     if dgain is not None:
         held, ws, nbytes = _workspace(
-            workspace, wedlm_rmsnorm_backward_workspace_size(M, Hd), x.device)
+            workspace, x.device, wedlm_rmsnorm_backward_workspace_size, M, Hd)
     code = _load().wedlm_rmsnorm_backward(
         _t(x, "x", _F32), _t(gain, "gain", _BF16, (Hd,)),
         _t(dy, "dy", _BF16, (M, Hd)),
@@ -869,9 +871,8 @@ def wedlm_qk_norm_rope_backward(qkv, q_gain, k_gain, pos_ids,
     held, ws, nbytes = None, None, 0
     if dq_gain is not None or dk_gain is not None:
         held, ws, nbytes = _workspace(
-            workspace,
-            wedlm_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D),
-            qkv.device)
+            workspace, qkv.device, wedlm_qk_norm_rope_backward_workspace_size,
+            M, Hq, Hkv, D)
     rows = (M, (Hq + 2 * Hkv) * D)
     code = _load().wedlm_qk_norm_rope_backward(
         _t(qkv, "qkv", _BF16, rows), _t(q_gain, "q_gain", _BF16, (D,)),
@@ -904,10 +905,8 @@ def wedlm_token_loss(logits, target, loss, weight=None, dlogits=None,
     V = stride if V is None else V
     half = logits.dtype == torch.bfloat16
     types = (torch.bfloat16,) if half else _F32
-    need = wedlm_token_loss_workspace_size(R, V)
-    held, ws, nbytes = None, None, 0
-    if need:
-        held, ws, nbytes = _workspace(workspace, need, logits.device)
+    held, ws, nbytes = _workspace(workspace, logits.device,
+                                  wedlm_token_loss_workspace_size, R, V)
     code = _load().wedlm_token_loss(
         _t(logits, "logits", types), LOGITS_BF16 if half else LOGITS_F32,
         stride, _t(target, "target", _I32, (R,)),
