@@ -37,7 +37,7 @@
 // the rate.
 //
 // Bound by the MFMAs, and these by the card's power: 4 x 4096 tokens (32/8
-// heads of 128) 3.37 ms, 816 TFLOP/s of the five products and 1.14 PFLOP/s of
+// heads of 128) 3.35 ms, 821 TFLOP/s of the five products and 1.20 PFLOP/s of
 // what runs, masked parts included; MFMAs on random values that do nothing
 // else hold 1.30 PFLOP/s, a large library product 1.22.  Leaving out barriers,
 // waits or exponentials does not change it.  Steps there: plain staging, with
