@@ -676,6 +676,9 @@ void dkv_kernel(BwdArgs a) {
   constexpr int kAll = 2 * kWaves + 1;
   static_assert(kAll >= kSlots, "the ring");
   __shared__ __attribute__((aligned(1024))) char smem[kAll * kSlot];
+  // the first row of the block after a lane's key's (divisions, and no register
+  // is left for their results in the loop)
+  __shared__ int s_next[2][kThreads];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int W = a.W, list = key_list(a.L);
   const int w = W % 8 == 0 ? blockIdx.x % 8 * (W / 8) + blockIdx.x / 8
@@ -806,6 +809,11 @@ void dkv_kernel(BwdArgs a) {
   constexpr int kE = 16 / NK;              // elements per step
   bf16x8_t f[NK];          // the operands from LDS, read a phase ahead
   const int kwl = min(kw0 + kOwn, a.L) - 1;         // the wave's last key
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int k0 = min(kw0 + 32 * b + (lane_here() & 31), a.L - 1);
+    s_next[b][threadIdx.x] = min(a.L, (k0 / a.block + 1) * a.block);
+  }
   const int next_hi = (kwl / a.block + 1) * a.block;
   Item cur = item_at(it0);
   int slot, next_slot, load_slot;
@@ -873,7 +881,7 @@ void dkv_kernel(BwdArgs a) {
       // the prediction by prediction rows k0 .. next-1
       const int l = lane_here();
       const int k0 = kw0 + 32 * b + (l & 31), i0 = p0 + 8 * (l >> 5);
-      const int next = min(a.L, (min(k0, a.L - 1) / a.block + 1) * a.block);
+      const int next = s_next[b][threadIdx.x];
       const int from = pred ? next : k0;
       const int to = k0 < a.L ? stream ? next : a.L : 0;
       const uint32_t see = rows_between(from - i0, to - i0);
