@@ -44,7 +44,7 @@
 // spills, 31.2 ms; tiles straight to LDS, accumulators held in AGPRs, 5.78;
 // one MFMA a step with vector work under it 4.35; equal work per CU 3.62;
 // prediction keys by single waves 3.41.  Shorter sequences are bound by
-// latency: 1 x 2048 (16/8 heads) 160 us, 1 x 256 (4/2 heads of 64) 28.6 us.
+// latency: 1 x 2048 (16/8 heads) 155 us, 1 x 256 (4/2 heads of 64) 28.1 us.
 #include <algorithm>
 #include <initializer_list>
 
@@ -310,11 +310,14 @@ __device__ __forceinline__ void drain(floatx16_t (&acc)[N]) {
 // of it, which a last kernel adds up in order.
 // ---------------------------------------------------------------------------
 // Work in items of memory keys, from the clock at each part of 1 x 2048 tokens
-// (16/8 heads of 128): an item 1.9 us, a tile's start and end 5 + 4; prediction
-// keys, each wave its own tiles, 2.7 an item (1 / kPredMore more), 6 + 5.  With
-// 4 for every tile and equal items the slowest workgroup took 117 us where the
-// mean was 87.
+// (16/8 heads of 128): an item 1.7 us, 2.1 where scores are masked (1 /
+// kMaskMore more), a tile's start and end 5 + 4; prediction keys, each wave its
+// own tiles, 2.7 an item (1 / kPredMore more), 6 + 5.  With 4 for every tile
+// and equal items the slowest workgroup took 117 us where the mean was 87;
+// without the masked items' share 160 us in all, 155 with it (2 x 2048 tokens,
+// 32/8 heads, 516 and 500).
 constexpr int kTileCost = 5, kPredTileCost = 7, kPredMore = 2;
+constexpr int kMaskMore = 3;
 constexpr int kSnap = 3;         // items: no cut nearer to a tile's end
 
 // The key tile at position p of the list.
@@ -323,6 +326,7 @@ struct KeyTile {
   int t_hi, t_mid;               // memory keys: both streams see them from row
                                  // tile t_mid on, memory rows alone before
   int items, fixed, cost;        // cost: of the tile and of its items
+  int masked;                    // the last of them, in which some wave masks
 };
 
 __host__ __device__ inline int key_list(int L) {
@@ -346,10 +350,16 @@ __host__ __device__ inline KeyTile key_tile(int L, int block, int G, int p) {
   x.items = (p & 1) && other == i ? 0
             : x.stream            ? own * G
                        : ((T - x.t_mid) * 2 + (x.t_mid - x.j0 / kRows)) * G;
+  // the row tiles of the keys' own positions end here
+  const int diag = x.t_hi < (x.j0 + kKeysPerWg) / kRows
+                       ? x.t_hi : (x.j0 + kKeysPerWg) / kRows;
+  x.masked = x.stream ? 0
+                      : ((x.t_mid < diag ? (diag - x.t_mid) * 2 : 0) +
+                         (x.t_mid < diag ? x.t_mid : diag) - x.j0 / kRows) * G;
   x.fixed = x.stream ? kPredTileCost : kTileCost;
   x.cost = x.items == 0 ? 0
                         : x.fixed + (x.stream ? x.items + x.items / kPredMore
-                                              : x.items);
+                                              : x.items + x.masked / kMaskMore);
   return x;
 }
 
@@ -393,7 +403,11 @@ __device__ inline Cut cut_at(const BwdArgs& a, int w) {
   }
   const KeyTile kt = key_tile(a.L, a.block, a.G, p);
   Cut r{g, p, off - kt.fixed};
-  if (kt.stream && r.item > 0) r.item -= r.item / (kPredMore + 1);
+  const int slow = r.item - (kt.items - kt.masked);
+  if (kt.stream && r.item > 0)
+    r.item -= r.item / (kPredMore + 1);
+  else if (slow > 0)
+    r.item -= slow / (kMaskMore + 1);
   if (r.item < kSnap) {
     r.item = 0;
   } else if (kt.items - r.item < kSnap) {
