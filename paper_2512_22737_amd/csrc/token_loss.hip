@@ -371,7 +371,8 @@ __global__ __launch_bounds__(kSmallThreads) void slice_grad_kernel(LossArgs a) {
 }
 
 // Logits and gradients at different offsets from 16-byte boundaries: element
-// by element, a running maximum and sum, then the gradient.
+// by element, a running maximum and sum, then the gradient.  (Unsigned: the
+// column after a row's last one may pass 2^31 - 1.)
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
     LossArgs a) {
@@ -379,7 +380,7 @@ __global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
   const int r = blockIdx.x;
   const T* row = static_cast<const T*>(a.logits) + r * a.stride;
   T* drow = static_cast<T*>(a.dlogits) + r * a.stride;
-  const int tid = threadIdx.x;
+  const uint32_t tid = threadIdx.x, V = static_cast<uint32_t>(a.V);
   int t;
   float w;
   if (no_loss(a, r, t, w)) {
@@ -389,9 +390,10 @@ __global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
   }
   __shared__ float lds[2][kSmallThreads / kWave];
   const float lt = E::get(row + t);
+  const uint32_t target = static_cast<uint32_t>(t);      // (0 .. V-1)
   MaxSum x{kNegInf, 0.f};
-  for (int v = tid; v < a.V; v += kSmallThreads) {
-    const float l = v == t ? kNegInf : E::get(row + v);
+  for (uint32_t v = tid; v < V; v += kSmallThreads) {
+    const float l = v == target ? kNegInf : E::get(row + v);
     if (l > x.m) {
       x.s *= exp_below(x.m, l);
       x.m = l;
@@ -405,9 +407,9 @@ __global__ __launch_bounds__(kSmallThreads) void token_loss_plain_kernel(
       [](float y, float z) { return y + z; });
   const RowStats q(w, m, s, lt);
   if (tid == 0) a.loss[r] = q.loss;
-  for (int v = tid; v < a.V; v += kSmallThreads)
+  for (uint32_t v = tid; v < V; v += kSmallThreads)
     E::set(drow + v,
-           v == t ? q.hit : exp_below(E::get(row + v), q.ref) * q.k);
+           v == target ? q.hit : exp_below(E::get(row + v), q.ref) * q.k);
 }
 
 // Elements of a row's slices, or V (one slice).  Rows of more than 16384 chunks
