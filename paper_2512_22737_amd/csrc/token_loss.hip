@@ -50,10 +50,15 @@ __device__ __forceinline__ float exp_below(float x, float m) {
   return __builtin_amdgcn_exp2f((x - m) * kLog2e);
 }
 
+// The same to the bit whichever way round: the one with the larger maximum
+// enters as it is.  (With both scaled, one product would be rounded and the
+// other fused into the sum, by its place.)
 __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b) {
-  const float m = fmaxf(a.m, b.m);
-  if (m == kNegInf) return {m, 0.f};
-  return {m, a.s * exp_below(a.m, m) + b.s * exp_below(b.m, m)};
+  const bool first = a.m >= b.m;
+  const MaxSum hi{first ? a.m : b.m, first ? a.s : b.s};
+  const MaxSum lo{first ? b.m : a.m, first ? b.s : a.s};
+  if (lo.m == kNegInf) return hi;
+  return {hi.m, __builtin_fmaf(lo.s, exp_below(lo.m, hi.m), hi.s)};
 }
 
 // One element type: values of a 16-byte chunk and of a single element.
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(kSmallThreads) void slice_grad_kernel(LossArgs a) {
   const bool mine = t >= v0 && t < v0 + n;
   if (!dp && !mine) return;
   const float2* part = a.part + static_cast<int64_t>(r) * (a.slices + 1);
-  // merge() is commutative to the bit: every lane ends with the same value
+  // (every lane ends with the same value: merge() does not ask for an order)
   MaxSum x{kNegInf, 0.f};
   for (int i = lane_id(); i < a.slices; i += kWave)
     x = merge(x, MaxSum{part[i].x, part[i].y});
