@@ -399,7 +399,7 @@ int sum_parts(const float* part, int parts, int n0, int n1, float* out0,
 
 bool qk_ok(int M, int Hq, int Hkv, int D) {
   return M >= 1 && Hq >= 1 && Hkv >= 1 && (D == 64 || D == 128) &&
-         (static_cast<int64_t>(Hq) + 2 * Hkv) * D <= 0x7fffffff / 8;
+         (Hq + 2ll * Hkv) * D <= 0x7fffffff / 8;
 }
 
 }  // namespace
