@@ -143,10 +143,11 @@ size_t wedlm_qk_norm_rope_backward_workspace_size(int32_t M, int32_t Hq,
  *   not wanted; all overwritten, no overlap with the inputs or each other.
  * M, Hq, Hkv >= 1, D 64 or 128; bf16 arrays on 16-byte boundaries
  * (WEDLM_E_ARG).
- * workspace: wedlm_qk_norm_rope_backward_workspace_size() bytes (partial sums
- * of the gains' gradients; none needed without them); its contents on entry
- * do not matter.  The sums' order is fixed by the sizes.  Two calls that
- * overlap in time must not share a workspace.
+ * workspace: wedlm_qk_norm_rope_backward_workspace_size() bytes on a 4-byte
+ * boundary (WEDLM_E_ARG; partial sums of the gains' gradients, none needed
+ * without them); its contents on entry do not matter.  The sums' order is
+ * fixed by the sizes.  Two calls that overlap in time must not share a
+ * workspace.
  */
 int wedlm_qk_norm_rope_backward(
     const uint16_t* qkv, const uint16_t* q_gain, const uint16_t* k_gain,

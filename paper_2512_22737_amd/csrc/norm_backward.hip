@@ -458,6 +458,7 @@ extern "C" int wedlm_qk_norm_rope_backward(
   if (!aligned({qkv, q_gain, k_gain, dq, dk, dv, dqkv}, 16)) return WEDLM_E_ARG;
   if (!qk_ok(M, Hq, Hkv, D)) return WEDLM_E_SHAPE;
   const bool gains = dq_gain || dk_gain;
+  if (gains && !aligned({workspace}, alignof(float))) return WEDLM_E_ARG;
   if (gains && (!workspace ||
                 workspace_bytes <
                     wedlm_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D)))
