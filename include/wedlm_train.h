@@ -183,9 +183,9 @@ size_t wedlm_token_loss_workspace_size(int32_t R, int32_t V);
  * Maxima, sums and the loss are fp32; the gradient is rounded once.  The
  * sums' order is fixed by the sizes and the arrays' alignment.  Rows on
  * 16-byte boundaries (logits and dlogits) are read and written faster.
- * workspace: wedlm_token_loss_workspace_size() bytes (NULL when that is 0);
- * its contents on entry do not matter.  Two calls that overlap in time must
- * not share a workspace.
+ * workspace: wedlm_token_loss_workspace_size() bytes on an 8-byte boundary
+ * (WEDLM_E_ARG; NULL when that is 0); its contents on entry do not matter.  Two
+ * calls that overlap in time must not share a workspace.
  */
 int wedlm_token_loss(const void* logits, int32_t logits_type,
                      int64_t row_stride, const int32_t* target,

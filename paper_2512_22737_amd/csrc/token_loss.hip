@@ -509,6 +509,9 @@ extern "C" int wedlm_token_loss(const void* logits, int32_t logits_type,
     return WEDLM_E_ARG;
   if (R < 1 || V < 1 || row_stride < V) return WEDLM_E_SHAPE;
   const size_t need = wedlm_token_loss_workspace_size(R, V);
+  // (a float2 for every slice)
+  if (need && reinterpret_cast<uintptr_t>(workspace) % sizeof(float2) != 0)
+    return WEDLM_E_ARG;
   if (need && (!workspace || workspace_bytes < need)) return WEDLM_E_WORKSPACE;
   LossArgs a{};
   a.logits = logits;

@@ -32,3 +32,13 @@ def test_qk_norm_rope_backward():
     check(lib.wedlm_qk_norm_rope_backward, args, 16, 4)
     args[14] = None               # one gain's gradient
     check(lib.wedlm_qk_norm_rope_backward, args, 16, 4)
+
+
+@pytest.mark.parametrize("logits_type", [0, 1])
+def test_token_loss(logits_type):
+    from paper_2512_22737_amd import wedlm
+    lib = wedlm.lib()
+    need = lib.wedlm_token_loss_workspace_size(3, 151936)
+    assert need > 0               # rows in slices
+    args = [F, logits_type, 151936, F, F, 3, 151936, F, F, F, need - 1, None]
+    check(lib.wedlm_token_loss, args, 9, 8)
