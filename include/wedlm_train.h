@@ -79,8 +79,10 @@ size_t wedlm_dual_stream_attn_backward_workspace_size(int32_t n_seq, int32_t L,
  * are rounded to it) with fp32 sums, in an order that the sizes fix: the
  * result does not depend on the run.
  * Limits: those of the forward, Hq * D < 2^25 and
- * ceil(L / 32) * Hq/Hkv < 2^29.  bf16 arrays and the workspace on 16-byte
- * boundaries (WEDLM_E_ARG).
+ * ceil(L / 256) * (ceil(L / 32) + 24) * Hq/Hkv < 2^31.  The last is the work
+ * of one kv head; somewhat beyond it shapes are refused (workspace size 0,
+ * WEDLM_E_SHAPE).  bf16 arrays and the workspace on 16-byte boundaries
+ * (WEDLM_E_ARG).
  * workspace: wedlm_dual_stream_attn_backward_workspace_size() bytes (each
  * row's normaliser and sum of P dP; fp32 sums of keys whose work is split over
  * workgroups); its contents on entry do not matter.  Two calls that overlap in

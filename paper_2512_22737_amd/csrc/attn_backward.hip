@@ -1115,6 +1115,8 @@ bool bwd_plan(int n_seq, int L, int block, int Hq, int Hkv, int D,
   for (int i = 0; i < key_list(L); ++i) {
     cost += key_tile(L, block, G, i).cost;
   }
+  // cut_at() counts a (sequence, kv head)'s work in 32 bits; beyond them a call
+  // would take the card more than ten seconds
   if (dq > 0x7fffffffll || cost > 0x7fffffffll) return false;
   // One workgroup per CU, but none with less than six items' work.  (At least
   // 16 items, longer walks but fewer partial sums: 1 x 256 tokens, 4/2 heads of
