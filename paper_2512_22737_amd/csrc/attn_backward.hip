@@ -440,8 +440,9 @@ __device__ __forceinline__ Cut read_cut(const BwdArgs& a, int w) {
 // kv head, one per wave; the longest first, of all sequences (sequence by
 // sequence: 4 x 512 tokens 34.6 us against 30.8, 4 x 4096 the same, 2 x 1008
 // with 28/4 heads 71 against 73).  Registers and a ring of four
-// tiles let two workgroups share a CU (D = 64: three), so that the vector work
-// of one runs under the products of the other.  With 64 rows a wave, half the
+// tiles let two workgroups share a CU (D = 64: three, 4 x 4096 tokens with 32/8
+// heads 2.03 ms in all; with two, 2.07), so that the vector work
+// of one runs under the products of the others.  With 64 rows a wave, half the
 // LDS reads per product but one workgroup per CU: 4 x 4096 tokens (32/8 heads
 // of 128) 1.53 ms against 1.47, 1 x 2048 (16/8) 92 us against 68.
 constexpr int kDqSlots = 4;
@@ -456,7 +457,7 @@ constexpr int kExactRows = 64;
 
 template <int D>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(1, 2)))
+__attribute__((amdgpu_waves_per_eu(1, D == 64 ? 3 : 2)))
 void dq_kernel(BwdArgs a) {
   constexpr int NK = D / 16, NM = D / 32;
   using T = RowTile<D>;
