@@ -782,6 +782,21 @@ def wedlm_dual_stream_attn(q, k, v, block: int, out, lse=None, workspace=None,
     _check(code, "wedlm_dual_stream_attn")
 
 
+def _fit(*sizes) -> bool:
+    """The library takes sizes in 32 bits (ctypes would cut what is longer)."""
+    return max(sizes) < 1 << 31 and min(sizes) >= -1 << 31
+
+
+def _sizes(what, *sizes) -> None:
+    if not _fit(*sizes):
+        raise WedlmError(f"{what}: a size of {sizes} is beyond 2^31 - 1")
+
+
+def _size(name, *shape) -> int:
+    """Bytes of a workspace (0: a shape that is not supported)."""
+    return int(getattr(_load(), name)(*shape)) if _fit(*shape) else 0
+
+
 def _workspace(workspace, device, size, *shape):
     """A workspace's tensor (of size(*shape) bytes if none is given; the
     library refuses a given one that is too small), address and bytes.  The
@@ -798,8 +813,8 @@ def _workspace(workspace, device, size, *shape):
 
 def wedlm_dual_stream_attn_backward_workspace_size(n_seq, L, block, Hq, Hkv,
                                                    D) -> int:
-    return int(_load().wedlm_dual_stream_attn_backward_workspace_size(
-        n_seq, L, block, Hq, Hkv, D))
+    return _size("wedlm_dual_stream_attn_backward_workspace_size", n_seq, L,
+                 block, Hq, Hkv, D)
 
 
 def wedlm_dual_stream_attn_backward(q, k, v, block: int, out, lse, dout, dq,
@@ -812,6 +827,7 @@ def wedlm_dual_stream_attn_backward(q, k, v, block: int, out, lse, dout, dq,
     n_seq, L2, Hq, D = q.shape
     Hkv = k.shape[2]
     L = L2 // 2
+    _sizes("wedlm_dual_stream_attn_backward", n_seq, L, block, Hq, Hkv, D)
     if softmax_scale is None:
         softmax_scale = 1.0 / math.sqrt(D)
     held, ws, nbytes = _workspace(
@@ -829,7 +845,7 @@ def wedlm_dual_stream_attn_backward(q, k, v, block: int, out, lse, dout, dq,
 
 
 def wedlm_rmsnorm_backward_workspace_size(M, Hd) -> int:
-    return int(_load().wedlm_rmsnorm_backward_workspace_size(M, Hd))
+    return _size("wedlm_rmsnorm_backward_workspace_size", M, Hd)
 
 
 def wedlm_rmsnorm_backward(x, gain, eps: float, dy, dx, dgain=None, dres=None,
@@ -839,6 +855,7 @@ def wedlm_rmsnorm_backward(x, gain, eps: float, dy, dx, dgain=None, dres=None,
     dgain [Hd] fp32 (optional).  A workspace is allocated here if dgain needs
     one and none is given."""
     M, Hd = x.shape
+    _sizes("wedlm_rmsnorm_backward", M, Hd)
     held, ws, nbytes = None, None, 0
     if dgain is not None:
         held, ws, nbytes = _workspace(
@@ -854,8 +871,7 @@ def wedlm_rmsnorm_backward(x, gain, eps: float, dy, dx, dgain=None, dres=None,
 
 
 def wedlm_qk_norm_rope_backward_workspace_size(M, Hq, Hkv, D) -> int:
-    return int(_load().wedlm_qk_norm_rope_backward_workspace_size(M, Hq, Hkv,
-                                                                  D))
+    return _size("wedlm_qk_norm_rope_backward_workspace_size", M, Hq, Hkv, D)
 
 
 def wedlm_qk_norm_rope_backward(qkv, q_gain, k_gain, pos_ids,
@@ -868,6 +884,7 @@ def wedlm_qk_norm_rope_backward(qkv, q_gain, k_gain, pos_ids,
     one and none is given."""
     M, Hq, D = dq.shape
     Hkv = dk.shape[1]
+    _sizes("wedlm_qk_norm_rope_backward", M, Hq, Hkv, D)
     held, ws, nbytes = None, None, 0
     if dq_gain is not None or dk_gain is not None:
         held, ws, nbytes = _workspace(
@@ -891,7 +908,7 @@ LOGITS_F32, LOGITS_BF16 = 0, 1
 
 
 def wedlm_token_loss_workspace_size(R, V) -> int:
-    return int(_load().wedlm_token_loss_workspace_size(R, V))
+    return _size("wedlm_token_loss_workspace_size", R, V)
 
 
 def wedlm_token_loss(logits, target, loss, weight=None, dlogits=None,
@@ -903,6 +920,7 @@ def wedlm_token_loss(logits, target, loss, weight=None, dlogits=None,
     given."""
     R, stride = logits.shape
     V = stride if V is None else V
+    _sizes("wedlm_token_loss", R, V)
     half = logits.dtype == torch.bfloat16
     types = (torch.bfloat16,) if half else _F32
     held, ws, nbytes = _workspace(workspace, logits.device,
