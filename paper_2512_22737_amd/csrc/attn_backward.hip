@@ -37,14 +37,18 @@
 // the rate.
 //
 // Bound by the MFMAs, and these by the card's power: 4 x 4096 tokens (32/8
-// heads of 128) 3.35 ms, 821 TFLOP/s of the five products and 1.20 PFLOP/s of
-// what runs, masked parts included; MFMAs on random values that do nothing
-// else hold 1.30 PFLOP/s, a large library product 1.22.  Leaving out barriers,
-// waits or exponentials does not change it.  Steps there: plain staging, with
+// heads of 128) 3.30 to 3.45 ms from card to card, 797 to 834 TFLOP/s of the
+// five products and 1.16 to 1.22 PFLOP/s of what runs, masked parts included;
+// MFMAs on random values that do nothing else hold 1.30 PFLOP/s, a large
+// library product 1.22.  Leaving out barriers, waits or exponentials does not
+// change it.  Steps there (on one card): plain staging, with
 // spills, 31.2 ms; tiles straight to LDS, accumulators held in AGPRs, 5.78;
 // one MFMA a step with vector work under it 4.35; equal work per CU 3.62;
-// prediction keys by single waves 3.41.  Shorter sequences are bound by
-// latency: 1 x 2048 (16/8 heads) 155 us, 1 x 256 (4/2 heads of 64) 28.1 us.
+// prediction keys by single waves 3.41.  Heads of 64 are bound by the vector
+// work of twice as many scores per product: 2.03 ms, of what runs dq at 0.99
+// PFLOP/s, dk and dv at 0.87.  Shorter sequences are bound by latency: 1 x
+// 2048 (16/8 heads) 160 us with other inputs from call to call, 155 with the
+// same ones (as below), 1 x 256 (4/2 heads of 64) 27.9 us.
 #include <algorithm>
 #include <initializer_list>
 
@@ -89,8 +93,9 @@ struct BwdArgs {
 // fills a group of 512 / D whole rows, groups are 16 bytes apart.  Chunk c (16
 // bytes) of row i of its group sits in slot c ^ swz(i).  Rows read together
 // (16 rows of one chunk; four rows of 64 bytes by columns) then hit different
-// banks, and the reads of a lane differ by constants but for the exclusive or
-// with its row: few address registers.
+// banks with D = 128 (counted: no conflict; with D = 64 conflicts take 40% of
+// dq's LDS cycles and 22% of dk's and dv's), and the reads of a lane differ by
+// constants but for the exclusive or with its row: few address registers.
 template <int D>
 struct RowTile {
   static constexpr int per_group = 512 / D;         // rows: 4 or 8

@@ -362,7 +362,8 @@ bool norm_ok(int M, int Hd) {
 // workgroups 279, 2048 276), two for longer ones, whose registers hold no more
 // (4096 x 8192 78 us; 2048 workgroups 103), and two rows each where they are
 // few, for fewer parts to add up (1024 x 4096 15.5 us; a row each 18.7; 512 x
-// 16384 31.9, 40.5; 2048 x 1024 10.3 with 512 workgroups, 11.2 with 1024).
+// 16384 31.9, 40.5; 2048 x 1024 10.3 with 512 workgroups, 11.2 with 1024).  All
+// without a residual gradient; with one 32768 x 4096 takes 338 us.
 int norm_parts(int M, int Hd) {
   const int most = M < 4096 || Hd > 4096 ? 512 : 1024;
   return std::min({M, most, std::max(256, M - M / 2)});
@@ -467,8 +468,9 @@ extern "C" int wedlm_qk_norm_rope_backward(
   float* part = gains ? static_cast<float*>(workspace) : nullptr;
   QkArgs a{qkv, q_gain, k_gain, pos_ids, dq, dk, dv, dqkv, part, M, Hq, Hkv,
            D, eps, {}};
-  // theta^(-2 j / D) as products of two powers (off by 2^-52 at most), not one
-  // power each: they cost the host as much as a launch
+  // theta^(-2 j / D) as products of two powers, not one power each: they cost
+  // the host as much as a launch.  Three roundings: off by 3 2^-53 at most beside
+  // pow()'s own error (found: 1.3 2^-52)
   double low[8], high[kMaxHalf / 8];
   for (int j = 0; j < 8; ++j) low[j] = std::pow(rope_theta, -2.0 * j / D);
   for (int j = 0; j < D / 16; ++j) high[j] = std::pow(rope_theta, -16.0 * j / D);
