@@ -22,7 +22,8 @@ LIB = os.path.join(PKG, "libwedlm.so")
 SOURCES = ["reorder.hip", "window_attn.hip", "score.hip", "commit.hip",
            "lm_head.hip", "model.hip", "dual_stream.hip",
            "attn_backward.hip", "norm_backward.hip",
-           "token_loss.hip", "abi.hip"]
+           "token_loss.hip", "cache8.hip", "window_attn8.hip", "pages.hip",
+           "sample.hip", "abi.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -46,6 +47,7 @@ def hipcc() -> str:
 # its accumulators in the accumulation registers by itself; there the
 # compiler's MFMAs write plain ones.
 FILE_FLAGS = {"window_attn.hip": ["-fno-honor-nans"],
+              "window_attn8.hip": ["-fno-honor-nans"],
               "attn_backward.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

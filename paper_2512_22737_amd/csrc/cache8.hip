@@ -1,0 +1,321 @@
+// Rows appended to the 8-bit paged cache: e4m3 codes, one power-of-two scale
+// per page and kv head (wedlm_cache8_append, wedlm_commit_cache8).
+//
+// One wave per (layer, sequence, page, kv head).  Its rows' largest finite
+// magnitude is an integer maximum over the bf16 patterns without their sign;
+// the exponent is read off that pattern, so the scale is exact and does not
+// depend on any rounding.  x * 2^(127 - e) is exact in fp32 and rounded once,
+// to e4m3.
+// Bound by HBM where rows are many (6 bytes per element and half a page more
+// where V pages are filled in part); by latency where a step commits a few
+// tokens: the chain is start/count, block table, rows, stores.
+#include "common.h"
+#include "internal.h"
+#include "wedlm_serve.h"
+
+using namespace wedlm;
+
+namespace {
+
+constexpr int kWavesPerGroup = 4;
+
+struct AppendArgs {
+  const uint16_t* k;      // [L, B, T, Hkv, D]
+  const uint16_t* v;
+  const int32_t* start;   // [B]
+  const int32_t* count;   // [B]
+  const int32_t* bt;      // [B, max_pages]
+  uint8_t* k8;            // [L, P, Hkv, 16, D]
+  uint8_t* v8;            // [L, P, Hkv, D, 16]
+  uint8_t* ke;            // [L, P, Hkv]
+  uint8_t* ve;
+  int32_t* status;        // [B] or null
+  int64_t num_pages;
+  int L, B, T, Hkv, max_pages;
+  int spans;              // pages that a sequence's rows can touch
+  uint32_t units;         // waves
+  int behind;             // start is the position behind the last row
+};
+
+// Smallest exponent >= 1 whose 448 * 2^(e - 127) holds the bf16 magnitude a
+// (a finite pattern without its sign): 448 = 1.75 * 2^8.
+__device__ __forceinline__ int need_exp(int a) {
+  const int e = (a >> 7) - 8 + ((a & 0x7f) > 0x60 ? 1 : 0);
+  return max(e, 1);
+}
+
+// Largest finite magnitude of eight bf16 values, with m.
+__device__ __forceinline__ int mag_max(u16x8_t x, int m) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int a = x[i] & 0x7fff;
+    m = max(m, a < 0x7f80 ? a : 0);
+  }
+  return m;
+}
+
+__device__ __forceinline__ int wave_max_int(int v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = max(v, __shfl_xor(v, off));
+  return v;
+}
+
+// Two e4m3 codes (in the low half) of a * 2^s, b * 2^s; what is not finite
+// becomes NaN (the format has no infinity).
+__device__ __forceinline__ uint32_t pack2(float a, float b, int s) {
+  const float nan = __builtin_nanf("");
+  a = __builtin_fabsf(a) < __builtin_huge_valf() ? a : nan;
+  b = __builtin_fabsf(b) < __builtin_huge_valf() ? b : nan;
+  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(
+             __builtin_amdgcn_ldexpf(a, s), __builtin_amdgcn_ldexpf(b, s), 0,
+             false)) & 0xffffu;
+}
+
+__device__ __forceinline__ uint2 pack8(u16x8_t x, int s) {
+  uint2 r;
+  r.x = pack2(bf16_to_f32(x[0]), bf16_to_f32(x[1]), s) |
+        pack2(bf16_to_f32(x[2]), bf16_to_f32(x[3]), s) << 16;
+  r.y = pack2(bf16_to_f32(x[4]), bf16_to_f32(x[5]), s) |
+        pack2(bf16_to_f32(x[6]), bf16_to_f32(x[7]), s) << 16;
+  return r;
+}
+
+// Four codes at another scale: value * 2^s, rounded again.
+__device__ __forceinline__ uint32_t again4(uint32_t c, int s) {
+  return pack2(__builtin_amdgcn_cvt_f32_fp8(c, 0),
+               __builtin_amdgcn_cvt_f32_fp8(c, 1), s) |
+         pack2(__builtin_amdgcn_cvt_f32_fp8(c, 2),
+               __builtin_amdgcn_cvt_f32_fp8(c, 3), s) << 16;
+}
+
+// Bytes lo .. hi-1 of a 16-byte vector, as masks of its words.
+__device__ __forceinline__ uint32_t byte_mask(int word, int lo, int hi) {
+  const int a = min(max(lo - 4 * word, 0), 4), b = min(max(hi - 4 * word, 0), 4);
+  const uint32_t below_b = b == 4 ? ~0u : (1u << (8 * b)) - 1;
+  const uint32_t below_a = a == 4 ? ~0u : (1u << (8 * a)) - 1;
+  return below_b & ~below_a;
+}
+
+template <int D>
+__global__ __launch_bounds__(kWavesPerGroup * kWave) void append8_kernel(
+    AppendArgs a) {
+  constexpr int LPR = D / 8;            // lanes per row, 8 values each
+  constexpr int RPI = kWave / LPR;      // rows per load
+  constexpr int NI = kPage / RPI;       // loads per page
+  // a page's V^T, bytes, per wave.  Rows of 16 bytes: a lane's 8 stores go to
+  // 8 consecutive rows
+  __shared__ __attribute__((aligned(16))) uint8_t vt[kWavesPerGroup][D * kPage];
+  const int wave = threadIdx.x / kWave, lane = lane_id();
+  const uint32_t unit = blockIdx.x * kWavesPerGroup + wave;
+  if (unit >= a.units) return;
+  const int h = unit % a.Hkv;
+  uint32_t w = unit / a.Hkv;
+  const int span = w % a.spans;
+  w /= a.spans;
+  const int l = w % a.L, b = w / a.L;
+
+  const int n = a.count[b];
+  int64_t s0 = a.start[b];
+  if (a.behind) s0 -= n;
+  const bool tell = a.status && l == 0 && h == 0 && lane == 0;
+  if (n < 0 || n > a.T || s0 < 0) {
+    if (tell && span == 0) atomicOr(a.status + b, WEDLM_SEQ_BAD_LEN);
+    return;
+  }
+  const int64_t page0 = (s0 / kPage + span) * kPage;     // its first position
+  const int r0 = static_cast<int>(max(s0 - page0, static_cast<int64_t>(0)));
+  const int r1 = static_cast<int>(
+      min(s0 + n - page0, static_cast<int64_t>(kPage)));
+  if (r1 <= r0) return;
+  const int64_t entry = page0 / kPage;
+  if (entry >= a.max_pages) {
+    if (tell) atomicOr(a.status + b, WEDLM_SEQ_CAPACITY);
+    return;
+  }
+  const int64_t id = a.bt[static_cast<int64_t>(b) * a.max_pages + entry];
+  if (id < 0 || id >= a.num_pages) {
+    if (tell) atomicOr(a.status + b, WEDLM_SEQ_BAD_PAGE);
+    return;
+  }
+  const int64_t ph = (l * a.num_pages + id) * a.Hkv + h;
+  uint8_t* kp = a.k8 + ph * (kPage * D);
+  uint8_t* vp = a.v8 + ph * (kPage * D);
+
+  // ---- the new rows
+  const int row = lane / LPR, d = (lane % LPR) * 8;
+  u16x8_t xk[NI], xv[NI];
+  int mk = 0, mv = 0;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int r = row + i * RPI;
+    u16x8_t z = {0, 0, 0, 0, 0, 0, 0, 0};
+    xk[i] = xv[i] = z;
+    if (r >= r0 && r < r1) {
+      const int64_t src =
+          (((static_cast<int64_t>(l) * a.B + b) * a.T + (page0 + r - s0)) *
+               a.Hkv + h) * D + d;
+      xk[i] = *reinterpret_cast<const u16x8_t*>(a.k + src);
+      xv[i] = *reinterpret_cast<const u16x8_t*>(a.v + src);
+    }
+    mk = mag_max(xk[i], mk);
+    mv = mag_max(xv[i], mv);
+  }
+  int ek = need_exp(wave_max_int(mk)), ev = need_exp(wave_max_int(mv));
+  int ek0 = ek, ev0 = ev;
+  if (r0 > 0) {
+    ek0 = a.ke[ph];
+    ev0 = a.ve[ph];
+    ek = max(ek, ek0);
+    ev = max(ev, ev0);
+  }
+  if (lane == 0) {
+    a.ke[ph] = static_cast<uint8_t>(ek);
+    a.ve[ph] = static_cast<uint8_t>(ev);
+  }
+
+  // ---- keys: rows are contiguous
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int r = row + i * RPI;
+    uint2* dst = reinterpret_cast<uint2*>(kp + r * D + d);
+    if (r >= r0 && r < r1) {
+      *dst = pack8(xk[i], 127 - ek);
+    } else if (r < r0 && ek > ek0) {
+      uint2 c = *dst;
+      c.x = again4(c.x, ek0 - ek);
+      c.y = again4(c.y, ek0 - ek);
+      *dst = c;
+    }
+  }
+
+  // ---- values: transposed through LDS, then whole 16-byte rows of the page,
+  // merged with what the page holds where not all 16 rows are new
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int r = row + i * RPI;
+    const uint2 c = pack8(xv[i], 127 - ev);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      vt[wave][(d + k) * kPage + r] =
+          static_cast<uint8_t>((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
+  }
+  // the wave's own LDS writes are complete before its reads (in order)
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < D / kWave; ++i) {
+    const int dd = i * kWave + lane;
+    u32x4_t c = *reinterpret_cast<const u32x4_t*>(&vt[wave][dd * kPage]);
+    u32x4_t* dst = reinterpret_cast<u32x4_t*>(vp + dd * kPage);
+    if (r1 - r0 < kPage) {
+      const u32x4_t old = *dst;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t fresh = byte_mask(q, r0, r1);
+        uint32_t o = old[q];
+        if (ev > ev0) {
+          const uint32_t before = byte_mask(q, 0, r0);
+          o = (again4(o, ev0 - ev) & before) | (o & ~before);
+        }
+        c[q] = (c[q] & fresh) | (o & ~fresh);
+      }
+    }
+    *dst = c;
+  }
+}
+
+bool aligned(const void* p, size_t n) {
+  return reinterpret_cast<uintptr_t>(p) % n == 0;
+}
+
+// The sizes' checks of both entry points.
+int append_shape(int64_t L, int64_t B, int64_t T, int64_t Hkv, int32_t D,
+                 int64_t num_pages, int32_t max_pages, int64_t* units) {
+  if (L < 1 || B < 1 || T < 1 || Hkv < 1 || (D != 64 && D != 128) ||
+      num_pages < 1 || num_pages >= (1ll << 31) || max_pages < 1)
+    return WEDLM_E_SHAPE;
+  const int64_t spans = (T + kPage - 1) / kPage + 1;
+  // a launch has fewer than 2^32 threads
+  int64_t u = L;
+  for (const int64_t f : {B, Hkv, spans}) {
+    if (u > (1ll << 26) / f) return WEDLM_E_SHAPE;
+    u *= f;
+  }
+  if (u >= (1ll << 26)) return WEDLM_E_SHAPE;
+  *units = u;
+  return WEDLM_OK;
+}
+
+int launch_append(AppendArgs& a, int D, int64_t units, hipStream_t st) {
+  a.spans = (a.T + kPage - 1) / kPage + 1;
+  a.units = static_cast<uint32_t>(units);
+  const dim3 grid(static_cast<unsigned>((units + kWavesPerGroup - 1) /
+                                        kWavesPerGroup));
+  if (D == 128)
+    hipLaunchKernelGGL(append8_kernel<128>, grid,
+                       dim3(kWavesPerGroup * kWave), 0, st, a);
+  else
+    hipLaunchKernelGGL(append8_kernel<64>, grid, dim3(kWavesPerGroup * kWave),
+                       0, st, a);
+  WEDLM_LAUNCH_CHECK();
+  return WEDLM_OK;
+}
+
+}  // namespace
+
+extern "C" int wedlm_cache8_append(
+    const uint16_t* k, const uint16_t* v, const int32_t* start,
+    const int32_t* count, int32_t n_layers, int32_t B, int32_t T, int32_t Hkv,
+    int32_t D, uint8_t* k8, uint8_t* v8, uint8_t* k_exp, uint8_t* v_exp,
+    int64_t num_pages, const int32_t* block_table, int32_t max_pages,
+    int32_t* status, void* stream) {
+  if (!k || !v || !start || !count || !k8 || !v8 || !k_exp || !v_exp ||
+      !block_table)
+    return WEDLM_E_ARG;
+  int64_t units = 0;
+  const int e = append_shape(n_layers, B, T, Hkv, D, num_pages, max_pages,
+                             &units);
+  if (e != WEDLM_OK) return e;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k8, 16) ||
+      !aligned(v8, 16))
+    return WEDLM_E_ARG;
+  AppendArgs a{};
+  a.k = k; a.v = v; a.start = start; a.count = count; a.bt = block_table;
+  a.k8 = k8; a.v8 = v8; a.ke = k_exp; a.ve = v_exp; a.status = status;
+  a.num_pages = num_pages; a.L = n_layers; a.B = B; a.T = T; a.Hkv = Hkv;
+  a.max_pages = max_pages;
+  return launch_append(a, D, units, static_cast<hipStream_t>(stream));
+}
+
+// The window's update first (it finds the committed run and checks that its
+// positions have pages), then the rows of the run, which ends at the new
+// win_start.
+extern "C" int wedlm_commit_cache8(
+    int32_t* win_tok, int32_t* win_start, const int32_t* argmax,
+    const float* entropy, double tau, double lambda, const uint16_t* k_win,
+    const uint16_t* v_win, uint8_t* k8, uint8_t* v8, uint8_t* k_exp,
+    uint8_t* v_exp, int64_t num_pages, const int32_t* block_table,
+    int32_t max_pages, int32_t B, int32_t W, int32_t Hkv, int32_t D,
+    int32_t n_layers, int32_t* n_commit, int32_t* committed_tok,
+    int32_t* committed_slot, uint8_t* selected, int32_t* status, int32_t rule,
+    void* stream) {
+  if (!k_win || !v_win || !k8 || !v8 || !k_exp || !v_exp) return WEDLM_E_ARG;
+  if (W > WEDLM_MAX_WINDOW) return WEDLM_E_SHAPE;
+  int64_t units = 0;
+  int e = append_shape(n_layers, B, W, Hkv, D, num_pages, max_pages, &units);
+  if (e != WEDLM_OK) return e;
+  if (!aligned(k_win, 16) || !aligned(v_win, 16) || !aligned(k8, 16) ||
+      !aligned(v8, 16))
+    return WEDLM_E_ARG;
+  e = commit_window(win_tok, win_start, argmax, entropy, tau, lambda,
+                    num_pages, block_table, max_pages, B, W, n_commit,
+                    committed_tok, committed_slot, selected, status, rule,
+                    stream);
+  if (e != WEDLM_OK) return e;
+  AppendArgs a{};
+  a.k = k_win; a.v = v_win; a.start = win_start; a.count = n_commit;
+  a.bt = block_table;
+  a.k8 = k8; a.v8 = v8; a.ke = k_exp; a.ve = v_exp;
+  a.num_pages = num_pages; a.L = n_layers; a.B = B; a.T = W; a.Hkv = Hkv;
+  a.max_pages = max_pages; a.behind = 1;
+  return launch_append(a, D, units, static_cast<hipStream_t>(stream));
+}

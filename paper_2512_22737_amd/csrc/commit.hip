@@ -22,6 +22,7 @@
 // into their cache slots (V transposed, per the page layout), 16 bytes of
 // one row and head at a time.
 #include "common.h"
+#include "internal.h"
 #include "wedlm_model.h"
 
 using namespace wedlm;
@@ -278,10 +279,11 @@ int commit_impl(int32_t* win_tok, int32_t* win_start, const int32_t* argmax,
                 int32_t W, int32_t Hkv, int32_t D, int32_t* n_commit,
                 int32_t* committed_tok, int32_t* committed_slot,
                 uint8_t* selected, int32_t* status, int32_t rule,
-                int32_t n_layers, void* stream) {
-  if (!win_tok || !win_start || !argmax || !entropy || !k_phys || !v_phys ||
-      !k_cache || !v_cache || !block_table || !n_commit || !committed_tok ||
-      !committed_slot || !selected || !status)
+                int32_t n_layers, void* stream, bool extend = true) {
+  if (!win_tok || !win_start || !argmax || !entropy || !block_table ||
+      !n_commit || !committed_tok || !committed_slot || !selected || !status)
+    return WEDLM_E_ARG;
+  if (extend && (!k_phys || !v_phys || !k_cache || !v_cache))
     return WEDLM_E_ARG;
   if (tau != tau || lambda != lambda || num_pages < 1 || max_pages < 1)
     return WEDLM_E_ARG;
@@ -306,7 +308,9 @@ int commit_impl(int32_t* win_tok, int32_t* win_start, const int32_t* argmax,
   a.win_lstride = static_cast<int64_t>(B) * W * Hkv * D;
   a.cache_lstride = num_pages * Hkv * kPage * D;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (n_layers > 1 || B >= 4) {
+  if (!extend) {
+    a.n_layers = 0;
+  } else if (n_layers > 1 || B >= 4) {
     // one workgroup per (sequence, layer, kv head), before the window
     // changes; the commit kernel then extends no cache.  (With fewer
     // sequences and one layer the commit kernel's own workgroup copies the
@@ -368,4 +372,21 @@ extern "C" int wedlm_commit_layers(
                      max_pages, B, W, Hkv, D, n_commit, committed_tok,
                      committed_slot, selected, status, rule, n_layers,
                      stream);
+}
+
+// The window's part of the commit: no cache is extended (the run's length and
+// its end are left in n_commit and win_start).
+int wedlm::commit_window(int32_t* win_tok, int32_t* win_start,
+                         const int32_t* argmax, const float* entropy,
+                         double tau, double lambda, int64_t num_pages,
+                         const int32_t* block_table, int32_t max_pages,
+                         int32_t B, int32_t W, int32_t* n_commit,
+                         int32_t* committed_tok, int32_t* committed_slot,
+                         uint8_t* selected, int32_t* status, int32_t rule,
+                         void* stream) {
+  return commit_impl(win_tok, win_start, argmax, entropy, tau, lambda, nullptr,
+                     nullptr, nullptr, nullptr, num_pages, block_table,
+                     max_pages, B, W, 1, 64, n_commit, committed_tok,
+                     committed_slot, selected, status, rule, 1, stream,
+                     false);
 }

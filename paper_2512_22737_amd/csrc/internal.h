@@ -41,4 +41,13 @@ __attribute__((visibility("hidden"))) size_t window_attn_pairs_workspace_size(
     int32_t n_seq, int32_t blocks, int32_t P, int32_t Hq, int32_t Hkv,
     int32_t D, int32_t max_prefix_len);
 
+// wedlm_commit_rule without the caches: the window, its run and its status
+// (the caller appends n_commit rows, which end at the new win_start).
+__attribute__((visibility("hidden"))) int commit_window(
+    int32_t* win_tok, int32_t* win_start, const int32_t* argmax,
+    const float* entropy, double tau, double lambda, int64_t num_pages,
+    const int32_t* block_table, int32_t max_pages, int32_t B, int32_t W,
+    int32_t* n_commit, int32_t* committed_tok, int32_t* committed_slot,
+    uint8_t* selected, int32_t* status, int32_t rule, void* stream);
+
 }  // namespace wedlm

@@ -1,5 +1,5 @@
 """Thin Python binding of libwedlm.so (include/wedlm.h, include/wedlm_model.h,
-include/wedlm_train.h).
+include/wedlm_train.h, include/wedlm_serve.h).
 
 Argument marshalling only: each function checks the tensors it is handed
 (device, dtype, contiguity, shape), reads the sizes off them and calls the C
@@ -24,7 +24,7 @@ WEDLM_OK = 0
 MASK_TOKEN = -1
 PAGE_SIZE = 16
 MAX_WINDOW = 64
-SEQ_CAPACITY, SEQ_BAD_PAGE, SEQ_BAD_LEN = 1, 2, 4
+SEQ_CAPACITY, SEQ_BAD_PAGE, SEQ_BAD_LEN, SEQ_BAD_ROW = 1, 2, 4, 8
 
 _lib = None
 
@@ -122,6 +122,35 @@ def _load():
     lib.wedlm_token_loss.argtypes = [P, I32, I64, P, P, I32, I32, P, P, P, SZ,
                                      P]
     lib.wedlm_token_loss.restype = ctypes.c_int
+    lib.wedlm_cache8_append.argtypes = ([P] * 4 + [I32] * 5 + [P] * 4 +
+                                        [I64, P, I32, P, P])
+    lib.wedlm_cache8_append.restype = ctypes.c_int
+    lib.wedlm_window_attn_cache8_workspace_size.argtypes = [I32] * 6
+    lib.wedlm_window_attn_cache8_workspace_size.restype = SZ
+    lib.wedlm_window_attn_cache8.argtypes = (
+        [P] * 7 + [I64, P, I32, P] + [I32] * 6 + [F, P, P, P, P, SZ, P])
+    lib.wedlm_window_attn_cache8.restype = ctypes.c_int
+    lib.wedlm_commit_cache8.argtypes = (
+        [P] * 4 + [D_, D_] + [P] * 6 + [I64, P] + [I32] * 6 + [P] * 5 +
+        [I32, P])
+    lib.wedlm_commit_cache8.restype = ctypes.c_int
+    lib.wedlm_cache_free.argtypes = [P, I32, P, I32, I32, P, I64, P, P]
+    lib.wedlm_cache_free.restype = ctypes.c_int
+    lib.wedlm_cache_fork_workspace_size.argtypes = [I32, I32, I64]
+    lib.wedlm_cache_fork_workspace_size.restype = SZ
+    lib.wedlm_cache_fork.argtypes = [P, P, P, I32, P, P, I32, I32, P, I64, P,
+                                     I32, I32, P, P, SZ, P]
+    lib.wedlm_cache_fork.restype = ctypes.c_int
+    lib.wedlm_cache_compact_workspace_size.argtypes = [I64]
+    lib.wedlm_cache_compact_workspace_size.restype = SZ
+    lib.wedlm_cache_compact.argtypes = [P, I32, I32, P, I64, P, I32, I32, P,
+                                        P, P, P, SZ, P]
+    lib.wedlm_cache_compact.restype = ctypes.c_int
+    lib.wedlm_sample_workspace_size.argtypes = [I32] * 3
+    lib.wedlm_sample_workspace_size.restype = SZ
+    lib.wedlm_sample.argtypes = [P, I32, I64] + [P] * 6 + [I32] * 3 + [
+        P, P, P, SZ, P]
+    lib.wedlm_sample.restype = ctypes.c_int
     lib.wedlm_strerror.argtypes = [ctypes.c_int]
     lib.wedlm_strerror.restype = ctypes.c_char_p
     lib.wedlm_version.argtypes = []
@@ -150,7 +179,13 @@ EXPORTED = ["wedlm_reorder", "wedlm_window_attn_workspace_size",
             "wedlm_rmsnorm_backward_workspace_size", "wedlm_rmsnorm_backward",
             "wedlm_qk_norm_rope_backward_workspace_size",
             "wedlm_qk_norm_rope_backward", "wedlm_token_loss_workspace_size",
-            "wedlm_token_loss"]
+            "wedlm_token_loss", "wedlm_cache8_append",
+            "wedlm_window_attn_cache8_workspace_size",
+            "wedlm_window_attn_cache8", "wedlm_commit_cache8",
+            "wedlm_cache_free", "wedlm_cache_fork_workspace_size",
+            "wedlm_cache_fork", "wedlm_cache_compact_workspace_size",
+            "wedlm_cache_compact", "wedlm_sample_workspace_size",
+            "wedlm_sample"]
 
 # decoding rules of wedlm_commit_rule (include/wedlm.h)
 RULE_STREAMING, RULE_BLOCK, RULE_ONE_TOKEN = 0, 1, 2
@@ -399,13 +434,21 @@ class DecodeStep:
 
     state: win_tok [B,W] int32, win_start [B] int32, k_cache/v_cache pages,
     block_table.  Per-step inputs: qkv_in [B,W,Hq+2Hkv,D] bf16 and logits
-    [B,W,V] fp32 (physical row order)."""
+    [B,W,V] fp32 (physical row order).
+
+    cache="e4m3": k_cache/v_cache are the codes of an 8-bit cache, and the
+    calls take its exponents too (include/wedlm_serve.h).  With random numbers
+    u [B,W] the tokens that fill masks are sampled instead of greedy ones;
+    settings: temperature, top_k, top_p, min_p as in wedlm_sample."""
 
     def __init__(self, B, W, Hq, Hkv, D, V, max_prefix_len, theta=1e6,
                  tau=0.9, lam=0.01, temperature=0.1, device="cuda",
-                 rule="stream"):
+                 rule="stream", cache="bf16"):
+        if cache not in ("bf16", "e4m3"):
+            raise WedlmError(f"cache: {cache!r} is neither bf16 nor e4m3")
         self.B, self.W, self.Hq, self.Hkv, self.D, self.V = B, W, Hq, Hkv, D, V
         self.rule = RULES[rule]
+        self.eight_bits = cache == "e4m3"
         self.theta, self.tau, self.lam, self.temperature = (theta, tau, lam,
                                                             temperature)
         self.max_prefix_len = int(max_prefix_len)
@@ -438,8 +481,10 @@ class DecodeStep:
 
     def set_max_prefix(self, max_prefix_len: int):
         self.max_prefix_len = int(max_prefix_len)
-        n = wedlm_window_attn_workspace_size(self.B, self.W, self.Hq, self.Hkv,
-                                             self.D, self.max_prefix_len)
+        size = (wedlm_window_attn_cache8_workspace_size if self.eight_bits
+                else wedlm_window_attn_workspace_size)
+        n = size(self.B, self.W, self.Hq, self.Hkv, self.D,
+                 self.max_prefix_len)
         cur = getattr(self, "attn_ws", None)
         if cur is None or cur.numel() < n:
             self.attn_ws = torch.empty(max(n, 1), dtype=torch.uint8,
@@ -450,7 +495,20 @@ class DecodeStep:
                       self.theta, self.perm, self.pos_ids, self.tok_phys,
                       self.n_obs, self.q_phys, self.k_phys, self.v_phys)
 
-    def attn(self, k_cache, v_cache, block_table, win_start):
+    def _pages(self, k_exp, v_exp):
+        """Whether the calls are those of an 8-bit cache."""
+        if self.eight_bits != (k_exp is not None and v_exp is not None):
+            raise WedlmError("exponents go with cache='e4m3', and only there")
+        return self.eight_bits
+
+    def attn(self, k_cache, v_cache, block_table, win_start, k_exp=None,
+             v_exp=None):
+        if self._pages(k_exp, v_exp):
+            wedlm_window_attn_cache8(
+                self.q_phys, self.k_phys, self.v_phys, k_cache, v_cache, k_exp,
+                v_exp, block_table, win_start, self.max_prefix_len, self.out,
+                self.lse, self.attn_status, self.attn_ws)
+            return
         wedlm_window_attn(self.q_phys, self.k_phys, self.v_phys, k_cache,
                           v_cache, block_table, win_start,
                           self.max_prefix_len, self.out, self.lse,
@@ -460,7 +518,21 @@ class DecodeStep:
         wedlm_score(logits, self.n_obs, self.temperature, self.argmax,
                     self.entropy, self.pmax, self.score_ws, V=self.V)
 
-    def commit(self, win_tok, win_start, k_cache, v_cache, block_table):
+    def sample(self, logits, u, **settings):
+        """Sampled tokens in the place of the greedy ones (after score())."""
+        wedlm_sample(logits, u, self.argmax, n_obs=self.n_obs, V=self.V,
+                     **settings)
+
+    def commit(self, win_tok, win_start, k_cache, v_cache, block_table,
+               k_exp=None, v_exp=None):
+        if self._pages(k_exp, v_exp):
+            wedlm_commit_cache8(
+                win_tok, win_start, self.argmax, self.entropy, self.tau,
+                self.lam, self.k_phys[None], self.v_phys[None], k_cache[None],
+                v_cache[None], k_exp[None], v_exp[None], block_table,
+                self.n_commit, self.committed_tok, self.committed_slot,
+                self.selected, self.status, self.rule)
+            return
         args = (win_tok, win_start, self.argmax, self.entropy, self.tau,
                 self.lam, self.k_phys, self.v_phys, k_cache, v_cache,
                 block_table, self.n_commit, self.committed_tok,
@@ -471,11 +543,16 @@ class DecodeStep:
             wedlm_commit_rule(*args, self.rule)
 
     def __call__(self, win_tok, win_start, qkv_in, logits, k_cache, v_cache,
-                 block_table):
+                 block_table, k_exp=None, v_exp=None, u=None, **settings):
         self.reorder(win_tok, win_start, qkv_in)
-        self.attn(k_cache, v_cache, block_table, win_start)
+        self.attn(k_cache, v_cache, block_table, win_start, k_exp, v_exp)
         self.score(logits)
-        self.commit(win_tok, win_start, k_cache, v_cache, block_table)
+        if u is not None:
+            self.sample(logits, u, **settings)
+        elif settings:
+            raise WedlmError("sampling needs random numbers u")
+        self.commit(win_tok, win_start, k_cache, v_cache, block_table, k_exp,
+                    v_exp)
 
 
 # ---------------------------------------------------------------------------
@@ -933,3 +1010,223 @@ def wedlm_token_loss(logits, target, loss, weight=None, dlogits=None,
         _t(dlogits, "dlogits", types, (R, stride), allow_none=True), ws,
         nbytes, _stream())
     _check(code, "wedlm_token_loss")
+
+
+# ---------------------------------------------------------------------------
+# serving (include/wedlm_serve.h)
+# ---------------------------------------------------------------------------
+
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def wedlm_cache8_append(k_rows, v_rows, start, count, k8, v8, k_exp, v_exp,
+                        block_table, status=None) -> None:
+    """k_rows, v_rows [L, B, T, Hkv, D] bf16, start and count [B] int32 ->
+    rows 0 .. count[b]-1 at positions start[b] .. of the 8-bit caches k8 [L, P,
+    Hkv, 16, D], v8 [L, P, Hkv, D, 16] (e4m3 or uint8) with the exponents
+    k_exp, v_exp [L, P, Hkv] uint8."""
+    L, B, T, Hkv, D = k_rows.shape
+    P, maxp = k8.shape[1], block_table.shape[1]
+    _sizes("wedlm_cache8_append", L, B, T, Hkv, D, maxp)
+    code = _load().wedlm_cache8_append(
+        _t(k_rows, "k_rows", _BF16), _t(v_rows, "v_rows", _BF16,
+                                        (L, B, T, Hkv, D)),
+        _t(start, "start", _I32, (B,)), _t(count, "count", _I32, (B,)), L, B,
+        T, Hkv, D, _t(k8, "k8", _CODES, (L, P, Hkv, PAGE_SIZE, D)),
+        _t(v8, "v8", _CODES, (L, P, Hkv, D, PAGE_SIZE)),
+        _t(k_exp, "k_exp", _U8, (L, P, Hkv)),
+        _t(v_exp, "v_exp", _U8, (L, P, Hkv)), P,
+        _t(block_table, "block_table", _I32, (B, maxp)), maxp,
+        _t(status, "status", _I32, (B,), allow_none=True), _stream())
+    _check(code, "wedlm_cache8_append")
+
+
+def wedlm_window_attn_cache8_workspace_size(B, W, Hq, Hkv, D,
+                                            max_prefix_len) -> int:
+    return _size("wedlm_window_attn_cache8_workspace_size", B, W, Hq, Hkv, D,
+                 max_prefix_len)
+
+
+def wedlm_window_attn_cache8(q_phys, k_phys, v_phys, k8, v8, k_exp, v_exp,
+                             block_table, prefix_len, max_prefix_len: int, out,
+                             lse=None, status=None, workspace=None,
+                             softmax_scale: Optional[float] = None) -> None:
+    """wedlm_window_attn over an 8-bit cache: k8 [P, Hkv, 16, D], v8 [P, Hkv,
+    D, 16] (e4m3 or uint8), k_exp, v_exp [P, Hkv] uint8.  A workspace is
+    allocated here if one is needed and none is given."""
+    B, W, Hq, D = q_phys.shape
+    Hkv = k_phys.shape[2]
+    P, maxp = k8.shape[0], block_table.shape[1]
+    max_prefix_len = int(max_prefix_len)
+    _sizes("wedlm_window_attn_cache8", B, W, Hq, Hkv, D, maxp, max_prefix_len)
+    if softmax_scale is None:
+        softmax_scale = 1.0 / math.sqrt(D)
+    held, ws, nbytes = _workspace(
+        workspace, q_phys.device, wedlm_window_attn_cache8_workspace_size, B,
+        W, Hq, Hkv, D, max_prefix_len)
+    code = _load().wedlm_window_attn_cache8(
+        _t(q_phys, "q_phys", _BF16),
+        _t(k_phys, "k_phys", _BF16, (B, W, Hkv, D)),
+        _t(v_phys, "v_phys", _BF16, (B, W, Hkv, D)),
+        _t(k8, "k8", _CODES, (P, Hkv, PAGE_SIZE, D)),
+        _t(v8, "v8", _CODES, (P, Hkv, D, PAGE_SIZE)),
+        _t(k_exp, "k_exp", _U8, (P, Hkv)), _t(v_exp, "v_exp", _U8, (P, Hkv)),
+        P, _t(block_table, "block_table", _I32, (B, maxp)), maxp,
+        _t(prefix_len, "prefix_len", _I32, (B,)), B, W, Hq, Hkv, D,
+        max_prefix_len, float(softmax_scale),
+        _t(out, "out", _BF16, (B, W, Hq, D)),
+        _t(lse, "lse", _F32, (B, W, Hq), allow_none=True),
+        _t(status, "status", _I32, (B,), allow_none=True), ws, nbytes,
+        _stream())
+    _check(code, "wedlm_window_attn_cache8")
+
+
+def wedlm_commit_cache8(win_tok, win_start, argmax, entropy, tau: float,
+                        lam: float, k_win, v_win, k8, v8, k_exp, v_exp,
+                        block_table, n_commit, committed_tok, committed_slot,
+                        selected, status, rule: int = RULE_STREAMING) -> None:
+    """wedlm_commit_layers for 8-bit caches: k_win, v_win [L, B, W, Hkv, D]
+    bf16, the caches as in wedlm_cache8_append."""
+    B, W = win_tok.shape
+    L, _, _, Hkv, D = k_win.shape
+    P, maxp = k8.shape[1], block_table.shape[1]
+    _sizes("wedlm_commit_cache8", L, B, W, Hkv, D, maxp)
+    code = _load().wedlm_commit_cache8(
+        _t(win_tok, "win_tok", _I32, (B, W)),
+        _t(win_start, "win_start", _I32, (B,)),
+        _t(argmax, "argmax", _I32, (B, W)),
+        _t(entropy, "entropy", _F32, (B, W)), float(tau), float(lam),
+        _t(k_win, "k_win", _BF16, (L, B, W, Hkv, D)),
+        _t(v_win, "v_win", _BF16, (L, B, W, Hkv, D)),
+        _t(k8, "k8", _CODES, (L, P, Hkv, PAGE_SIZE, D)),
+        _t(v8, "v8", _CODES, (L, P, Hkv, D, PAGE_SIZE)),
+        _t(k_exp, "k_exp", _U8, (L, P, Hkv)),
+        _t(v_exp, "v_exp", _U8, (L, P, Hkv)), P,
+        _t(block_table, "block_table", _I32, (B, maxp)), maxp, B, W, Hkv, D, L,
+        _t(n_commit, "n_commit", _I32, (B,)),
+        _t(committed_tok, "committed_tok", _I32, (B, W)),
+        _t(committed_slot, "committed_slot", _I32, (B, W)),
+        _t(selected, "selected", _U8, (B, W)),
+        _t(status, "status", _I32, (B,)), int(rule), _stream())
+    _check(code, "wedlm_commit_cache8")
+
+
+class PageArray(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
+
+
+def _page_arrays(arrays, P):
+    """The library's list of a pool's arrays [L, P, ...], and their L."""
+    if not arrays:
+        return None, 0, 1
+    L = arrays[0].shape[0]
+    made = (PageArray * len(arrays))()
+    for i, x in enumerate(arrays):
+        if not x.is_cuda or not x.is_contiguous():
+            raise WedlmError(f"arrays[{i}] must be a contiguous device tensor")
+        if x.dim() < 2 or x.shape[:2] != (L, P):
+            raise WedlmError(f"arrays[{i}]: shape {tuple(x.shape)} is not "
+                             f"[{L}, {P}, ...]")
+        made[i] = PageArray(x.data_ptr(), x.nbytes // (L * P) if L * P else 0)
+    return made, len(arrays), L
+
+
+def wedlm_cache_free(rows, block_table, ref, prefix_len=None) -> None:
+    """The rows [n] int32 of block_table [B, max_pages] give their pages back:
+    ref [P] int32 counts the entries that hold a page."""
+    B, maxp = block_table.shape
+    n, P = rows.numel(), ref.shape[0]
+    _sizes("wedlm_cache_free", n, B, maxp)
+    code = _load().wedlm_cache_free(
+        _t(rows, "rows", _I32, (n,)), n, _t(block_table, "block_table", _I32),
+        B, maxp, _t(ref, "ref", _I32, (P,)), P,
+        _t(prefix_len, "prefix_len", _I32, (B,), allow_none=True), _stream())
+    _check(code, "wedlm_cache_free")
+
+
+def wedlm_cache_fork_workspace_size(n, max_pages, num_pages) -> int:
+    return _size("wedlm_cache_fork_workspace_size", n, max_pages, num_pages)
+
+
+def wedlm_cache_fork(parent, child, reserve, prefix_len, block_table, ref,
+                     arrays, status, workspace=None) -> None:
+    """Rows child[i] of block_table [B, max_pages] get the prefix of rows
+    parent[i] (-1: none; child[i] itself: more pages) and pages for reserve[i]
+    positions; parent, child, reserve, status [n] int32, prefix_len [B], ref
+    [P] int32, arrays: the pool's tensors [L, P, ...].  A workspace is
+    allocated here if none is given."""
+    B, maxp = block_table.shape
+    n, P = parent.numel(), ref.shape[0]
+    _sizes("wedlm_cache_fork", n, B, maxp)
+    made, na, L = _page_arrays(arrays, P)
+    held, ws, nbytes = _workspace(workspace, ref.device,
+                                  wedlm_cache_fork_workspace_size, n, maxp, P)
+    code = _load().wedlm_cache_fork(
+        _t(parent, "parent", _I32, (n,)), _t(child, "child", _I32, (n,)),
+        _t(reserve, "reserve", _I32, (n,)), n,
+        _t(prefix_len, "prefix_len", _I32, (B,)),
+        _t(block_table, "block_table", _I32), B, maxp,
+        _t(ref, "ref", _I32, (P,)), P, made, na, L,
+        _t(status, "status", _I32, (n,)), ws, nbytes, _stream())
+    _check(code, "wedlm_cache_fork")
+
+
+def wedlm_cache_compact_workspace_size(num_pages) -> int:
+    return _size("wedlm_cache_compact_workspace_size", num_pages)
+
+
+def wedlm_cache_compact(block_table, ref, arrays, new_table, new_ref, n_used,
+                        workspace=None) -> None:
+    """The pages in use (ref [P] int32 > 0) move to the lowest numbers in the
+    pool's arrays [L, P, ...]; new_table like block_table and new_ref like ref
+    (which they may be) get the new numbers and counts, n_used [1] how many.
+    A workspace is allocated here if none is given."""
+    B, maxp = block_table.shape
+    P = ref.shape[0]
+    _sizes("wedlm_cache_compact", B, maxp)
+    made, na, L = _page_arrays(arrays, P)
+    held, ws, nbytes = _workspace(workspace, ref.device,
+                                  wedlm_cache_compact_workspace_size, P)
+    code = _load().wedlm_cache_compact(
+        _t(block_table, "block_table", _I32), B, maxp,
+        _t(ref, "ref", _I32, (P,)), P, made, na, L,
+        _t(new_table, "new_table", _I32, (B, maxp)),
+        _t(new_ref, "new_ref", _I32, (P,)), _t(n_used, "n_used", _I32, (1,)),
+        ws, nbytes, _stream())
+    _check(code, "wedlm_cache_compact")
+
+
+SAMPLE_F32, SAMPLE_BF16 = 0, 1
+
+
+def wedlm_sample_workspace_size(B, W, V) -> int:
+    return _size("wedlm_sample_workspace_size", B, W, V)
+
+
+def wedlm_sample(logits, u, token, temperature=None, top_k=None, top_p=None,
+                 min_p=None, n_obs=None, logp=None, workspace=None,
+                 V: Optional[int] = None) -> None:
+    """logits [B, W, row_stride] fp32 or bf16, u [B, W] fp32 in [0, 1) ->
+    token [B, W] int32 and logp [B, W] fp32 (optional) of rows i >= n_obs[b]
+    (all without n_obs).  temperature, top_p, min_p [B] fp32 and top_k [B]
+    int32 are optional.  V defaults to the last dimension.  A workspace is
+    allocated here if one is needed and none is given."""
+    B, W, stride = logits.shape
+    V = stride if V is None else V
+    _sizes("wedlm_sample", B, W, V)
+    half = logits.dtype == torch.bfloat16
+    types = (torch.bfloat16,) if half else _F32
+    held, ws, nbytes = _workspace(workspace, logits.device,
+                                  wedlm_sample_workspace_size, B, W, V)
+    code = _load().wedlm_sample(
+        _t(logits, "logits", types), SAMPLE_BF16 if half else SAMPLE_F32,
+        stride, _t(u, "u", _F32, (B, W)),
+        _t(n_obs, "n_obs", _I32, (B,), allow_none=True),
+        _t(temperature, "temperature", _F32, (B,), allow_none=True),
+        _t(top_k, "top_k", _I32, (B,), allow_none=True),
+        _t(top_p, "top_p", _F32, (B,), allow_none=True),
+        _t(min_p, "min_p", _F32, (B,), allow_none=True), B, W, V,
+        _t(token, "token", _I32, (B, W)),
+        _t(logp, "logp", _F32, (B, W), allow_none=True), ws, nbytes,
+        _stream())
+    _check(code, "wedlm_sample")
