@@ -4,14 +4,20 @@
 // One workgroup per row.  What a row keeps is a leading run of its tokens in
 // falling order, so it is described by a key (the order-preserving pattern of
 // a logit) and a number of ties: tokens above the key, and the first m ids at
-// it.  top-k's key is found by counts, top-p's by sums of weights, each by a
-// radix search over the key's 32 bits (11, 11 and 10 at a time).  Then the
-// kept weights are summed by segments of consecutive ids, and the drawn
-// segment is walked.
-// Weights w = 2^((x - max) log2(e) / T) are fp64 values rounded to whole
+// it.  Weights w = 2^((x - max) log2(e) / T) are fp64 values rounded to whole
 // multiples of 2^-shift (shift >= 41, so that V of them fit 64 bits): sums
-// are exact and the same in any order, which both the histogram's atomics and
+// are exact and the same in any order, which both the histograms' atomics and
 // the comparison of running sums with u * total need.
+// Passes over a row (the first from HBM, the others from the caches):
+//   1. the largest logit and its id;
+//   2. with top-k or top-p: a histogram over 2048 equal bins of (max - x) / T,
+//      tokens and weights per bin, which tells the bins that the ends of
+//      top-k's and top-p's runs lie in;
+//   3. the weights in the bins above them, summed by segments of consecutive
+//      ids, and the tokens of those bins collected in LDS, where a radix search
+//      over the keys finds the exact ends.  (Where they are too many, as in a
+//      flat row, the search passes over the row itself.)
+//   4. the segment that the draw falls into, walked by one wave.
 #include "common.h"
 #include "wedlm_serve.h"
 
@@ -22,7 +28,7 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
-constexpr int kSegs = 1024;             // segments of a row at most
+constexpr int kSegs = 256;              // segments of a row at most
 
 struct Args {
   const void* x;
@@ -36,7 +42,7 @@ struct Args {
   int32_t* token;
   float* logp;
   int W, V, shift;
-  int seg;                // tokens per segment, a multiple of 256
+  int seg;                // tokens per segment, whole vectors of a wave
 };
 
 // Order-preserving pattern of a logit (NaN: -inf; +inf: the largest number).
@@ -50,30 +56,64 @@ __device__ __forceinline__ float of_key(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-template <bool HALF>
-__device__ __forceinline__ float load(const void* x, int64_t i) {
-  if constexpr (HALF) return bf16_to_f32(static_cast<const uint16_t*>(x)[i]);
-  else return static_cast<const float*>(x)[i];
-}
+constexpr int kList = 2048;             // tokens of the bins at the runs' ends
+constexpr int kFine = 256;              // steps of the table of powers
+// bins per log2 unit: bin kBins - 1 holds what is 48 units below the top and
+// more, whose weight is zero (shift <= 46)
+constexpr float kBinsPerUnit = (kBins - 1) / 48.f;
 
+// 2^(i / 256), and weights from it: t = k + i / 256 + r, |r| <= 2^-9, with
+// 2^r by its series to r^4 (what is left out is below 2^-54).
 struct Row {
   double max, rate;       // largest logit; log2(e) / T
   int shift;
-  // weight of a key, in units of 2^-shift
-  __device__ __forceinline__ uint64_t weight(uint32_t key) const {
-    const double t = (static_cast<double>(of_key(key)) - max) * rate;
-    if (!(t > -static_cast<double>(shift) - 2)) return 0;
-    return static_cast<uint64_t>(rint(ldexp(exp2(t), shift)));
+  float cut;              // logits below it have a weight of zero
+  const double* powers;   // LDS
+  // weight of a logit, in units of 2^-shift
+  __device__ __forceinline__ uint64_t weight(float x) const {
+    if (!(x >= cut)) return 0;
+    const double t = (static_cast<double>(x) - max) * rate;
+    if (t < -48.0) return 0;
+    constexpr double kMagic = 6755399441055744.0 / kFine;   // 1.5 * 2^52 / 256
+    const double y = t + kMagic;
+    const int n = static_cast<int>(__double2loint(y));       // round(256 t)
+    const double r = t - (y - kMagic);
+    double e = 9.618129107628477e-3;                         // ln2^4 / 24
+    e = __builtin_fma(e, r, 5.550410866482158e-2);           // ln2^3 / 6
+    e = __builtin_fma(e, r, 2.402265069591007e-1);           // ln2^2 / 2
+    e = __builtin_fma(e, r, 6.931471805599453e-1);
+    e = __builtin_fma(e, r, 1.0);
+    e *= powers[n & (kFine - 1)];
+    // (n >> 8) + shift > -2 - 46 and at most 46: whole numbers by adding 2^52
+    const double q = __builtin_amdgcn_ldexp(e, (n >> 8) + shift);
+    return static_cast<uint64_t>(__double_as_longlong(q + 4503599627370496.0)) &
+           ((1ull << 52) - 1);
   }
 };
 
 struct Lds {
   uint64_t sum[kBins];
   uint32_t count[kBins];
+  uint64_t list[kList];   // key << 32 | id
+  double powers[kFine];
   uint64_t part[kWaves];
   uint64_t found_before, found_ties;
-  uint32_t found;
+  uint32_t found, listed;
 };
+
+// Sum over the workgroup, to all threads.
+__device__ __forceinline__ uint64_t group_sum(uint64_t v, uint64_t* part) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1)
+    v += __shfl_xor(static_cast<unsigned long long>(v), off);
+  __syncthreads();
+  if (lane_id() == 0) part[threadIdx.x / kWave] = v;
+  __syncthreads();
+  uint64_t all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) all += part[w];
+  return all;
+}
 
 // Exclusive sums over the workgroup; `total` to all threads.
 __device__ __forceinline__ uint64_t group_scan(uint64_t v, uint64_t* part,
@@ -99,26 +139,168 @@ __device__ __forceinline__ uint64_t group_scan(uint64_t v, uint64_t* part,
   return before + s - v;
 }
 
-// The bin, from the highest down, at which the sum of `value` over the bins
-// reaches `want` (>= 1, at most the sum of all); `before` gets the sum of the
-// bins above it.
-template <typename F>
-__device__ __forceinline__ uint32_t find_bin(Lds& l, F value, uint64_t want,
-                                             uint64_t& before) {
-  const int b1 = kBins - 1 - 2 * static_cast<int>(threadIdx.x);   // and b1 - 1
-  const uint64_t hi = value(b1), lo = value(b1 - 1);
+// The first bin, in the order of `bin_at` (place 0 .. kBins-1 -> bin), at
+// which the running sum of `value` reaches `want` (>= 1); `before` gets the
+// sum ahead of it.  kBins if the sum of all is less.  Every thread has two
+// places.
+template <typename F, typename G>
+__device__ __forceinline__ uint32_t find_bin(Lds& l, F value, G bin_at,
+                                             uint64_t want, uint64_t& before) {
+  const int p0 = 2 * static_cast<int>(threadIdx.x);
+  const uint64_t v0 = value(bin_at(p0)), v1 = value(bin_at(p0 + 1));
   uint64_t total;
-  const uint64_t at = group_scan(hi + lo, l.part, total);
-  if (at < want && at + hi >= want) {
-    l.found = b1;
+  const uint64_t at = group_scan(v0 + v1, l.part, total);
+  if (threadIdx.x == 0 && total < want) {
+    l.found = kBins;
+    l.found_before = total;
+  }
+  if (at < want && at + v0 >= want) {
+    l.found = bin_at(p0);
     l.found_before = at;
-  } else if (at + hi < want && at + hi + lo >= want) {
-    l.found = b1 - 1;
-    l.found_before = at + hi;
+  } else if (at + v0 < want && at + v0 + v1 >= want) {
+    l.found = bin_at(p0 + 1);
+    l.found_before = at + v0;
   }
   __syncthreads();
   before = l.found_before;
   return l.found;
+}
+
+// The logits of a row: `head` of them before the first 16-byte boundary, then
+// vectors.
+template <bool HALF>
+struct Logits {
+  static constexpr int VEC = HALF ? 8 : 4;
+  const void* x;
+  int V, head;
+
+  __device__ __forceinline__ float one(int i) const {
+    if constexpr (HALF) return bf16_to_f32(static_cast<const uint16_t*>(x)[i]);
+    else return static_cast<const float*>(x)[i];
+  }
+  __device__ __forceinline__ void many(int i, float (&f)[VEC]) const {
+    if constexpr (HALF) {
+      const u16x8_t v = *reinterpret_cast<const u16x8_t*>(
+          static_cast<const uint16_t*>(x) + i);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] = bf16_to_f32(v[k]);
+    } else {
+      const floatx4_t v = *reinterpret_cast<const floatx4_t*>(
+          static_cast<const float*>(x) + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[k] = v[k];
+    }
+  }
+  // f(logit, id) of every token, over the workgroup; four vectors of a thread
+  // under way at a time
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    const int tid = threadIdx.x;
+    if (tid < head) f(one(tid), tid);
+    constexpr int kStep = kThreads * VEC;
+    int i = head + tid * VEC;
+    for (; i + 3 * kStep + VEC <= V; i += 4 * kStep) {
+      float v[4][VEC];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) many(i + u * kStep, v[u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) f(v[u][k], i + u * kStep + k);
+    }
+    for (; i + VEC <= V; i += kStep) {
+      float v[VEC];
+      many(i, v);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) f(v[k], i + k);
+    }
+    if (i < V)
+      for (int k = i; k < V; ++k) f(one(k), k);
+  }
+};
+
+// Digits of a radix search: bits [down, up) of the key.
+__device__ __forceinline__ int digit_up(int level) {
+  return level == 0 ? 32 : level == 1 ? 21 : 10;
+}
+__device__ __forceinline__ int digit_down(int level) {
+  return level == 0 ? 21 : level == 1 ? 10 : 0;
+}
+__device__ __forceinline__ bool in_prefix(uint32_t key, uint32_t prefix,
+                                          int level) {
+  return level == 0 || key >> digit_up(level) == prefix >> digit_up(level);
+}
+__device__ __forceinline__ int digit_of(uint32_t key, int level) {
+  return (key >> digit_down(level)) &
+         ((1u << (digit_up(level) - digit_down(level))) - 1);
+}
+
+// Key of the want-th largest of the tokens that each(f) visits (f(key)), and
+// how many of its ties are among the first `want`.
+template <typename E>
+__device__ __forceinline__ void kth_key(Lds& l, E each, uint64_t want,
+                                        uint32_t& key, uint32_t& ties) {
+  uint32_t prefix = 0;
+  for (int level = 0; level < 3; ++level) {
+    __syncthreads();
+    for (int j = threadIdx.x; j < kBins; j += kThreads) l.count[j] = 0;
+    __syncthreads();
+    each([&](uint32_t k) {
+      if (in_prefix(k, prefix, level)) atomicAdd(&l.count[digit_of(k, level)], 1u);
+    });
+    __syncthreads();
+    uint64_t before;
+    prefix |= find_bin(
+                  l, [&](int j) { return static_cast<uint64_t>(l.count[j]); },
+                  [](int p) { return kBins - 1 - p; }, want, before)
+              << digit_down(level);
+    want -= before;
+  }
+  key = prefix;
+  ties = static_cast<uint32_t>(want);
+}
+
+// Key at which the weights of the tokens above kkey, with the first kties ties
+// at it, reach `want` in falling order, and how many of its ties that takes.
+template <typename E>
+__device__ __forceinline__ void pth_key(Lds& l, const Row& r, E each,
+                                        uint32_t kkey, uint32_t kties,
+                                        uint64_t want, uint32_t& key,
+                                        uint32_t& ties) {
+  uint32_t prefix = 0;
+  for (int level = 0; level < 3; ++level) {
+    __syncthreads();
+    for (int j = threadIdx.x; j < kBins; j += kThreads) l.sum[j] = 0;
+    __syncthreads();
+    each([&](uint32_t k) {
+      if (k > kkey && in_prefix(k, prefix, level)) {
+        const uint64_t q = r.weight(of_key(k));
+        if (q)
+          atomicAdd(reinterpret_cast<unsigned long long*>(
+                        &l.sum[digit_of(k, level)]),
+                    static_cast<unsigned long long>(q));
+      }
+    });
+    __syncthreads();
+    if (threadIdx.x == 0 && kkey != 0 && in_prefix(kkey, prefix, level))
+      l.sum[digit_of(kkey, level)] += kties * r.weight(of_key(kkey));
+    __syncthreads();
+    uint64_t before;
+    prefix |= find_bin(l, [&](int j) { return l.sum[j]; },
+                       [](int p) { return kBins - 1 - p; }, want, before)
+              << digit_down(level);
+    want -= before;
+  }
+  key = prefix;
+  const uint64_t q = r.weight(of_key(key));
+  ties = static_cast<uint32_t>((want + q - 1) / q);
+}
+
+// The least whole number >= p * total, one at least (0 <= p < 1).
+__device__ __forceinline__ uint64_t share(double p, uint64_t total) {
+  const uint64_t f = static_cast<uint64_t>(ldexp(p, 63)) << 1;
+  const uint64_t s = __umul64hi(total, f) + (total * f != 0 ? 1 : 0);
+  return s < 1 ? 1 : s;
 }
 
 template <bool HALF>
@@ -126,21 +308,31 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
   __shared__ Lds l;
   const int row = blockIdx.x, b = row / a.W, i = row - b * a.W;
   if (a.n_obs && i < a.n_obs[b]) return;
-  const void* x;
+  Logits<HALF> x;
+  constexpr int VEC = Logits<HALF>::VEC;
   if constexpr (HALF)
-    x = static_cast<const uint16_t*>(a.x) + row * a.stride;
+    x.x = static_cast<const uint16_t*>(a.x) + row * a.stride;
   else
-    x = static_cast<const float*>(a.x) + row * a.stride;
+    x.x = static_cast<const float*>(a.x) + row * a.stride;
   const int V = a.V, tid = threadIdx.x, lane = lane_id();
   const int wave = tid / kWave;
+  x.V = V;
+  x.head = min(V, static_cast<int>((-reinterpret_cast<uintptr_t>(x.x) & 15) /
+                                   (16 / VEC)));
 
   // ---- the largest logit and its first id
-  uint64_t best = 0;
-  for (int v = tid; v < V; v += kThreads) {
-    const uint64_t k = static_cast<uint64_t>(key_of(load<HALF>(x, v))) << 32 |
-                       static_cast<uint32_t>(~v);
-    best = k > best ? k : best;
-  }
+  if (tid < kFine) l.powers[tid] = exp2(tid / static_cast<double>(kFine));
+  uint32_t top = 0;
+  int first = 0x7fffffff;
+  // (a thread meets its ids in rising order, but for its last few)
+  x.each([&](float f, int v) {
+    const uint32_t k = key_of(f);
+    if (k > top || (k == top && v < first)) {
+      top = k;
+      first = v;
+    }
+  });
+  uint64_t best = static_cast<uint64_t>(top) << 32 | static_cast<uint32_t>(~first);
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
     const uint64_t o = __shfl_xor(static_cast<unsigned long long>(best), off);
@@ -150,9 +342,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) best = l.part[w] > best ? l.part[w] : best;
-  __syncthreads();
-  const uint32_t top = static_cast<uint32_t>(best >> 32);
-  const int first = static_cast<int>(~static_cast<uint32_t>(best));
+  top = static_cast<uint32_t>(best >> 32);
+  first = static_cast<int>(~static_cast<uint32_t>(best));
   const float T = a.temp ? a.temp[b] : 1.f;
   if (!(T > 0.f) || of_key(top) == kNegInf) {
     if (tid == 0) {
@@ -161,96 +352,23 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
     }
     return;
   }
+  const float fmax_ = of_key(top);
   Row r;
-  r.max = of_key(top);
+  r.max = fmax_;
   r.rate = 1.4426950408889634 / static_cast<double>(T);
   r.shift = a.shift;
+  r.powers = l.powers;
   const int k_raw = a.top_k ? a.top_k[b] : 0;
+  const bool use_k = k_raw > 0 && k_raw < V;
   const float p = a.top_p ? a.top_p[b] : 1.f;
+  const bool use_p = p < 1.f;
+  const double pd = p > 0.f ? static_cast<double>(p) : 0.0;
   const float least = a.min_p ? a.min_p[b] : 0.f;
-
-  // ---- top-k: tokens with keys above tkey, and the first ties at it
-  uint32_t tkey = 0;
-  uint32_t ties = 0xffffffffu;
-  if (k_raw > 0 && k_raw < V) {
-    uint32_t prefix = 0;
-    uint64_t want = k_raw;
-    for (int level = 0; level < 3; ++level) {
-      const int down = level == 0 ? 21 : level == 1 ? 10 : 0;
-      const int up = level == 0 ? 32 : level == 1 ? 21 : 10;
-      for (int j = tid; j < kBins; j += kThreads) l.count[j] = 0;
-      __syncthreads();
-      for (int v = tid; v < V; v += kThreads) {
-        const uint32_t k = key_of(load<HALF>(x, v));
-        if (level == 0 || k >> up == prefix >> up)
-          atomicAdd(&l.count[(k >> down) & ((1u << (up - down)) - 1)], 1u);
-      }
-      __syncthreads();
-      uint64_t before;
-      const uint32_t bin = find_bin(
-          l, [&](int j) { return static_cast<uint64_t>(l.count[j]); }, want,
-          before);
-      prefix |= bin << down;
-      want -= before;
-      __syncthreads();
-    }
-    tkey = prefix;
-    ties = static_cast<uint32_t>(want);
-  }
-
-  // ---- top-p, over what top-k left
-  if (p < 1.f) {
-    const uint32_t kkey = tkey, kties = ties;
-    uint32_t prefix = 0;
-    uint64_t want = 0;
-    for (int level = 0; level < 3; ++level) {
-      const int down = level == 0 ? 21 : level == 1 ? 10 : 0;
-      const int up = level == 0 ? 32 : level == 1 ? 21 : 10;
-      for (int j = tid; j < kBins; j += kThreads) {
-        l.sum[j] = 0;
-        l.count[j] = 0;
-      }
-      __syncthreads();
-      for (int v = tid; v < V; v += kThreads) {
-        const uint32_t k = key_of(load<HALF>(x, v));
-        if (k > kkey && (level == 0 || k >> up == prefix >> up)) {
-          const uint64_t q = r.weight(k);
-          if (q) {
-            atomicAdd(reinterpret_cast<unsigned long long*>(
-                          &l.sum[(k >> down) & ((1u << (up - down)) - 1)]),
-                      static_cast<unsigned long long>(q));
-          }
-        }
-      }
-      __syncthreads();
-      // the ties that top-k kept (without top-k kkey is below every key)
-      if (tid == 0 && kties != 0xffffffffu &&
-          (level == 0 || kkey >> up == prefix >> up))
-        l.sum[(kkey >> down) & ((1u << (up - down)) - 1)] +=
-            kties * r.weight(kkey);
-      __syncthreads();
-      if (level == 0) {
-        uint64_t total;
-        group_scan(l.sum[2 * tid] + l.sum[2 * tid + 1], l.part, total);
-        // the least whole number >= p * total, one at least
-        const double ps = p > 0.f ? static_cast<double>(p) : 0.0;
-        const uint64_t pf = static_cast<uint64_t>(ldexp(ps, 63)) << 1;
-        want = __umul64hi(total, pf) + (total * pf != 0 ? 1 : 0);
-        want = want < 1 ? 1 : want;
-      }
-      uint64_t before;
-      const uint32_t bin =
-          find_bin(l, [&](int j) { return l.sum[j]; }, want, before);
-      prefix |= bin << down;
-      want -= before;
-      __syncthreads();
-    }
-    tkey = prefix;
-    const uint64_t q = r.weight(tkey);
-    ties = static_cast<uint32_t>((want + q - 1) / q);
-  }
-
-  // ---- min-p
+  // weights of less than half a unit are zero: those of logits below `cut` (by
+  // a margin that its rounding to fp32 cannot reach); that of -inf always
+  r.cut = static_cast<float>(
+      fmax(r.max - (r.shift + 1.01) / r.rate - 1e-6 * fabs(r.max),
+           -3.4028234663852886e38));
   uint64_t qmin = 1;
   if (least > 0.f) {
     const double m = least < 1.f ? static_cast<double>(least) : 1.0;
@@ -258,39 +376,194 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
     qmin = q > 1 ? q : 1;
   }
 
-  // ---- sums and ties of each segment
-  const int nseg = (V + a.seg - 1) / a.seg;
-  for (int s = wave; s < nseg; s += kWaves) {
-    const int end = min(V, (s + 1) * a.seg);
-    uint64_t sum = 0;
-    uint32_t at = 0;
-    for (int v = s * a.seg + lane; v < end; v += kWave) {
-      const uint32_t k = key_of(load<HALF>(x, v));
-      if (k > tkey) {
-        const uint64_t q = r.weight(k);
-        sum += q >= qmin ? q : 0;
+  // ---- the bins of the runs' ends
+  const float rate = static_cast<float>(fmin(r.rate * kBinsPerUnit, 1e30));
+  auto bin_of = [&](uint32_t key) {
+    return static_cast<int>(
+        fminf((fmax_ - of_key(key)) * rate, static_cast<float>(kBins - 1)));
+  };
+  int lo = kBins - 1, hi = lo - 1;      // bins lo .. hi and kb are collected,
+  int kb = -1;                          // those below lo are kept whole
+  uint64_t k_left = 0, k_above = 0;     // tokens of bin kb; weights above it
+  uint64_t p_above = 0;                 // weights above bin lo
+  if (use_k || use_p) {
+    for (int j = tid; j < kBins; j += kThreads) {
+      l.sum[j] = 0;
+      l.count[j] = 0;
+    }
+    if (tid == 0) l.listed = 0;
+    __syncthreads();
+    x.each([&](float f, int) {
+      const uint32_t k = key_of(f);
+      const int bin = bin_of(k);
+      if (bin >= kBins - 1) return;
+      if (use_k) atomicAdd(&l.count[bin], 1u);
+      if (use_p) {
+        const uint64_t q = r.weight(of_key(k));
+        if (q)
+          atomicAdd(reinterpret_cast<unsigned long long*>(&l.sum[bin]),
+                    static_cast<unsigned long long>(q));
       }
-      at += k == tkey ? 1 : 0;
+    });
+    __syncthreads();
+    auto same = [](int j) { return j; };
+    auto sums = [&](int j) { return l.sum[j]; };
+    if (use_k) {
+      uint64_t before;
+      const uint32_t f = find_bin(
+          l, [&](int j) { return static_cast<uint64_t>(l.count[j]); }, same,
+          static_cast<uint64_t>(k_raw), before);
+      // (fewer tokens than k have a weight: no limit)
+      if (f < kBins) {
+        kb = static_cast<int>(f);
+        k_left = k_raw - before;
+      }
     }
+    if (use_p) {
+      // what top-k leaves weighs at least the bins above kb, at most kb too
+      uint64_t most = l.sum[2 * tid] * (kb < 0 || 2 * tid <= kb) +
+                      l.sum[2 * tid + 1] * (kb < 0 || 2 * tid + 1 <= kb);
+      most = group_sum(most, l.part);
+      k_above = kb < 0 ? most : most - l.sum[kb];
+      uint64_t before;
+      lo = static_cast<int>(find_bin(l, sums, same, share(pd, k_above), before));
+      p_above = before;
+      hi = lo;
+      if (kb >= 0) {
+        __syncthreads();
+        hi = static_cast<int>(find_bin(l, sums, same, share(pd, most), before));
+      }
+    } else if (kb >= 0) {
+      lo = hi = kb;
+    }
+    __syncthreads();
+  }
+
+  // ---- sums of each segment: what is above the ends' bins; those bins' tokens
+  // into the list.  Segment s is seg tokens from head + s * seg on, the first
+  // has the head too.
+  const int seg = a.seg;
+  const int nseg = max(1, (V - x.head + seg - 1) / seg);
+  uint32_t tkey = 0, ties = 0;
+  const bool ends = lo <= hi || kb >= 0;
+  auto in_list = [&](int bin) { return (bin >= lo && bin <= hi) || bin == kb; };
+  for (int s = wave; s < nseg; s += kWaves) {
+    uint64_t sum = 0;
+    auto take = [&](float f, int v) {
+      const uint32_t k = key_of(f);
+      if (ends) {
+        const int bin = bin_of(k);
+        if (bin >= lo) {
+          if (in_list(bin)) {
+            const uint32_t at = atomicAdd(&l.listed, 1u);
+            if (at < kList)
+              l.list[at] = static_cast<uint64_t>(k) << 32 |
+                           static_cast<uint32_t>(v);
+          }
+          return;
+        }
+      }
+      const uint64_t q = r.weight(of_key(k));
+      sum += q >= qmin ? q : 0;
+    };
+    if (s == 0 && lane < x.head) take(x.one(lane), lane);
+    const int end = min(V, x.head + (s + 1) * seg);
+    int v = x.head + s * seg + lane * VEC;
+    for (; v + VEC <= end; v += kWave * VEC) {
+      float f[VEC];
+      x.many(v, f);
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-      sum += __shfl_xor(static_cast<unsigned long long>(sum), off);
-      at += __shfl_xor(at, off);
+      for (int k = 0; k < VEC; ++k) take(f[k], v + k);
     }
-    if (lane == 0) {
-      l.sum[s] = sum;
-      l.count[s] = at;
+    for (int k = v; k < end && k < v + VEC; ++k) take(x.one(k), k);
+    if (ballot(sum != 0)) {
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1)
+        sum += __shfl_xor(static_cast<unsigned long long>(sum), off);
     }
+    if (lane == 0) l.sum[s] = sum;
   }
   __syncthreads();
-  uint64_t qt = r.weight(tkey);
+
+  if (ends) {
+    const int n = static_cast<int>(l.listed);
+    const bool small = n <= kList;
+    // the sums by segment wait in registers while the searches use the bins
+    uint64_t mine = tid < nseg ? l.sum[tid] : 0;
+    auto list_keys = [&](auto f) {
+      for (int j = tid; j < n; j += kThreads)
+        f(static_cast<uint32_t>(l.list[j] >> 32));
+    };
+    auto row_keys = [&](auto f) {
+      x.each([&](float g, int) { f(key_of(g)); });
+    };
+    uint32_t kkey = 0, kties = 0;
+    if (kb >= 0) {
+      if (small)
+        kth_key(l, [&](auto f) {
+          list_keys([&](uint32_t k) { if (bin_of(k) == kb) f(k); });
+        }, k_left, kkey, kties);
+      else
+        kth_key(l, row_keys, static_cast<uint64_t>(k_raw), kkey, kties);
+      tkey = kkey;
+      ties = kties;
+    }
+    if (use_p) {
+      // the weight of all that top-k left
+      uint64_t total = 0;
+      if (kb >= 0) {
+        auto add = [&](uint32_t k) {
+          if (k > kkey && bin_of(k) == kb) total += r.weight(of_key(k));
+        };
+        if (small) list_keys(add);
+        else row_keys(add);
+        total = group_sum(total, l.part) + kties * r.weight(of_key(kkey));
+      }
+      total += k_above;
+      const uint64_t want = share(pd, total);
+      if (small)
+        pth_key(l, r, list_keys, kkey, kties, want - p_above, tkey, ties);
+      else
+        pth_key(l, r, row_keys, kkey, kties, want, tkey, ties);
+    }
+    // the kept tokens of the ends' bins, and the ties of each segment
+    __syncthreads();
+    if (tid < kSegs) {
+      l.sum[tid] = mine;
+      l.count[tid] = 0;
+    }
+    __syncthreads();
+    auto keep = [&](uint32_t k, int v) {
+      if (k < tkey || !in_list(bin_of(k))) return;
+      const int s = max(v - x.head, 0) / seg;
+      if (k == tkey) {
+        atomicAdd(&l.count[s], 1u);
+        return;
+      }
+      const uint64_t q = r.weight(of_key(k));
+      if (q >= qmin)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&l.sum[s]),
+                  static_cast<unsigned long long>(q));
+    };
+    if (small) {
+      for (int j = tid; j < n; j += kThreads)
+        keep(static_cast<uint32_t>(l.list[j] >> 32),
+             static_cast<int>(static_cast<uint32_t>(l.list[j])));
+    } else {
+      x.each([&](float f, int v) { keep(key_of(f), v); });
+    }
+    __syncthreads();
+  }
+
+  // ---- the draw
+  uint64_t qt = ends ? r.weight(of_key(tkey)) : 0;
   qt = qt >= qmin ? qt : 0;
   uint64_t total;
-  const uint32_t mine = tid < nseg ? l.count[tid] : 0;
-  const uint64_t ties_before = group_scan(mine, l.part, total);
+  const uint32_t tied = ends && tid < nseg ? l.count[tid] : 0;
+  const uint64_t ties_before = group_scan(tied, l.part, total);
   const uint64_t left = ties > ties_before ? ties - ties_before : 0;
   const uint64_t own = (tid < nseg ? l.sum[tid] : 0) +
-                       qt * (left < mine ? left : mine);
+                       qt * (left < tied ? left : tied);
   const uint64_t before = group_scan(own, l.part, total);
   float u = a.u[row];
   u = u > 0.f ? (u < 1.f ? u : 0.99999994f) : 0.f;
@@ -304,39 +577,56 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
   }
   __syncthreads();
   if (wave != 0) return;
-  // ---- the segment that holds the drawn token, one wave
-  uint64_t run = l.found_before, seen = l.found_ties;
+  // ---- the segment that holds the drawn token, one wave, a run of ids a lane
   const int s = l.found;
-  const int end = min(V, (s + 1) * a.seg);
-  for (int base = s * a.seg; base < end; base += kWave) {
-    const int v = base + lane;
-    const uint32_t k = v < end ? key_of(load<HALF>(x, v)) : 0;
-    const bool tie = v < end && k == tkey;
-    const uint64_t tm = ballot(tie);
-    const uint64_t rank = seen + __popcll(tm & ((1ull << lane) - 1));
-    uint64_t q = 0;
-    if (v < end && (k > tkey || (tie && rank < ties))) q = r.weight(k);
-    q = q >= qmin ? q : 0;
-    uint64_t c = q;
+  const int begin = s == 0 ? 0 : x.head + s * seg;
+  const int end = min(V, x.head + (s + 1) * seg);
+  const int per = (end - begin + kWave - 1) / kWave;
+  const int v0 = min(begin + lane * per, end), v1 = min(v0 + per, end);
+  uint64_t sum = 0;
+  uint32_t mine = 0;
+  for (int v = v0; v < v1; ++v) {
+    const uint32_t k = key_of(x.one(v));
+    mine += ends && k == tkey ? 1 : 0;
+    const uint64_t q = k > tkey ? r.weight(of_key(k)) : 0;
+    sum += q >= qmin ? q : 0;
+  }
+  uint64_t seen = mine;                 // ties up to this lane's last
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      const uint64_t o = __shfl_up(static_cast<unsigned long long>(c), off);
-      if (lane >= off) c += o;
+  for (int off = 1; off < kWave; off <<= 1) {
+    const uint64_t o = __shfl_up(static_cast<unsigned long long>(seen), off);
+    if (lane >= off) seen += o;
+  }
+  seen += l.found_ties - mine;          // ties before its first
+  uint64_t rest = ties > seen ? ties - seen : 0;
+  sum += qt * (rest < mine ? rest : mine);
+  uint64_t run = sum;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const uint64_t o = __shfl_up(static_cast<unsigned long long>(run), off);
+    if (lane >= off) run += o;
+  }
+  run += l.found_before - sum;          // weights before its first
+  if (!(run <= goal && run + sum > goal)) return;
+  for (int v = v0; v < v1; ++v) {
+    const uint32_t k = key_of(x.one(v));
+    uint64_t q = 0;
+    if (k > tkey) {
+      q = r.weight(of_key(k));
+      q = q >= qmin ? q : 0;
+    } else if (ends && k == tkey && rest > 0) {
+      q = qt;
+      --rest;
     }
-    const uint64_t hit = ballot(run + c > goal);
-    if (hit) {
-      if (lane == __ffsll(static_cast<unsigned long long>(hit)) - 1) {
-        a.token[row] = v;
-        if (a.logp)
-          a.logp[row] = static_cast<float>(
-              (static_cast<double>(of_key(k)) - r.max) /
-                  static_cast<double>(T) -
-              log(ldexp(static_cast<double>(total), -r.shift)));
-      }
+    run += q;
+    if (run > goal) {
+      a.token[row] = v;
+      if (a.logp)
+        a.logp[row] = static_cast<float>(
+            (static_cast<double>(of_key(k)) - r.max) / static_cast<double>(T) -
+            log(ldexp(static_cast<double>(total), -r.shift)));
       return;
     }
-    run += __shfl(static_cast<unsigned long long>(c), kWave - 1);
-    seen += __popcll(tm);
   }
 }
 
@@ -372,7 +662,7 @@ extern "C" int wedlm_sample(const void* logits, int32_t logits_type,
   int bits = 0;
   while ((1 << bits) < V) ++bits;
   a.shift = 62 - bits < 46 ? 62 - bits : 46;
-  a.seg = 256;
+  a.seg = logits_type == WEDLM_SAMPLE_BF16 ? 512 : 256;
   while ((V + a.seg - 1) / a.seg > kSegs) a.seg *= 2;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (logits_type == WEDLM_SAMPLE_BF16)
