@@ -9,15 +9,18 @@
 // are exact and the same in any order, which both the histograms' atomics and
 // the comparison of running sums with u * total need.
 // Passes over a row (the first from HBM, the others from the caches):
-//   1. the largest logit and its id;
-//   2. with top-k or top-p: a histogram over 2048 equal bins of (max - x) / T,
-//      tokens and weights per bin, which tells the bins that the ends of
-//      top-k's and top-p's runs lie in;
-//   3. the weights in the bins above them, summed by segments of consecutive
-//      ids, and the tokens of those bins collected in LDS, where a radix search
-//      over the keys finds the exact ends.  (Where they are too many, as in a
-//      flat row, the search passes over the row itself.)
-//   4. the segment that the draw falls into, walked by one wave.
+//   1. the largest logit;
+//   2. with top-k or top-p: the sum of all weights, and a histogram (tokens and
+//      weights) of the logits near the top, which tells the bins that the ends
+//      of top-k's and top-p's runs lie in.  Those logits go into a list too; a
+//      row whose list does not overflow is not read again.  (If an end lies
+//      further down, the pass is done again over all that has a weight.)
+//   3. otherwise the weights of the tokens that are surely kept, summed by
+//      segments of consecutive ids, and the tokens of the ends' bins collected.
+// The exact ends are found among the tokens of their bins: by comparing all
+// with all if they are few, else by a radix search over the keys (over the row
+// itself where they are too many for LDS, as in a flat row).  Last, one wave
+// walks the segment that the draw falls into.
 #include "common.h"
 #include "wedlm_serve.h"
 
@@ -25,7 +28,7 @@ using namespace wedlm;
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
 constexpr int kSegs = 256;              // segments of a row at most
@@ -56,24 +59,27 @@ __device__ __forceinline__ float of_key(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
+constexpr int kNear = 4096;             // tokens near the top
 constexpr int kList = 2048;             // tokens of the bins at the runs' ends
+constexpr int kPairs = 256;             // of them compared all with all
 constexpr int kFine = 256;              // steps of the table of powers
-// bins per log2 unit: bin kBins - 1 holds what is 48 units below the top and
-// more, whose weight is zero (shift <= 46)
-constexpr float kBinsPerUnit = (kBins - 1) / 48.f;
+// log2 units below the top that the histogram covers, at first and at last:
+// 48 units down every weight is zero (shift <= 46)
+constexpr float kUnits = 24.f, kAllUnits = 48.f;
 
 // 2^(i / 256), and weights from it: t = k + i / 256 + r, |r| <= 2^-9, with
 // 2^r by its series to r^4 (what is left out is below 2^-54).
 struct Row {
   double max, rate;       // largest logit; log2(e) / T
   int shift;
-  float cut;              // logits below it have a weight of zero
   const double* powers;   // LDS
-  // weight of a logit, in units of 2^-shift
+  // weight of a logit, in units of 2^-shift; without a branch: half of the
+  // work is here
   __device__ __forceinline__ uint64_t weight(float x) const {
-    if (!(x >= cut)) return 0;
-    const double t = (static_cast<double>(x) - max) * rate;
-    if (t < -48.0) return 0;
+    // 48 units down and more every weight is zero (as is that of -inf, also
+    // where the rate is zero)
+    const double t =
+        __builtin_fmax((static_cast<double>(x) - max) * rate, -48.0);
     constexpr double kMagic = 6755399441055744.0 / kFine;   // 1.5 * 2^52 / 256
     const double y = t + kMagic;
     const int n = static_cast<int>(__double2loint(y));       // round(256 t)
@@ -84,7 +90,7 @@ struct Row {
     e = __builtin_fma(e, r, 6.931471805599453e-1);
     e = __builtin_fma(e, r, 1.0);
     e *= powers[n & (kFine - 1)];
-    // (n >> 8) + shift > -2 - 46 and at most 46: whole numbers by adding 2^52
+    // a whole number below 2^47 by adding 2^52
     const double q = __builtin_amdgcn_ldexp(e, (n >> 8) + shift);
     return static_cast<uint64_t>(__double_as_longlong(q + 4503599627370496.0)) &
            ((1ull << 52) - 1);
@@ -94,12 +100,38 @@ struct Row {
 struct Lds {
   uint64_t sum[kBins];
   uint32_t count[kBins];
-  uint64_t list[kList];   // key << 32 | id
+  uint64_t near[kNear];   // key << 32 | ~id: larger is earlier in the order
+  uint64_t list[kList];
+  uint64_t weights[kPairs];
   double powers[kFine];
   uint64_t part[kWaves];
   uint64_t found_before, found_ties;
-  uint32_t found, listed;
+  uint32_t found, nears, listed, low, tied;
 };
+
+// A logit as it counts: NaN: -inf; +inf: the largest number.
+__device__ __forceinline__ float clean(float x) {
+  return fminf(fmaxf(x, kNegInf), 3.402823466e38f);
+}
+
+// Appends e of the lanes that call it to a list of `most`; false if it is
+// full, with its length then beyond that.
+__device__ __forceinline__ bool push(uint64_t* list, uint32_t* n, uint32_t most,
+                                     uint64_t e) {
+  const uint64_t m = ballot(true);
+  const int lead = __ffsll(static_cast<unsigned long long>(m)) - 1;
+  uint32_t at = 0;
+  if (lane_id() == lead)
+    at = atomicAdd(n, static_cast<uint32_t>(__popcll(m)));
+  at = __shfl(at, lead) + __popcll(m & ((1ull << lane_id()) - 1));
+  if (at < most) list[at] = e;
+  return at < most;
+}
+
+__device__ __forceinline__ uint64_t entry(float x, int id) {
+  return static_cast<uint64_t>(key_of(x)) << 32 |
+         static_cast<uint32_t>(~static_cast<uint32_t>(id));
+}
 
 // Sum over the workgroup, to all threads.
 __device__ __forceinline__ uint64_t group_sum(uint64_t v, uint64_t* part) {
@@ -141,25 +173,31 @@ __device__ __forceinline__ uint64_t group_scan(uint64_t v, uint64_t* part,
 
 // The first bin, in the order of `bin_at` (place 0 .. kBins-1 -> bin), at
 // which the running sum of `value` reaches `want` (>= 1); `before` gets the
-// sum ahead of it.  kBins if the sum of all is less.  Every thread has two
-// places.
+// sum ahead of it.  kBins if the sum of all is less.
 template <typename F, typename G>
 __device__ __forceinline__ uint32_t find_bin(Lds& l, F value, G bin_at,
                                              uint64_t want, uint64_t& before) {
-  const int p0 = 2 * static_cast<int>(threadIdx.x);
-  const uint64_t v0 = value(bin_at(p0)), v1 = value(bin_at(p0 + 1));
+  constexpr int N = kBins / kThreads;
+  const int p0 = N * static_cast<int>(threadIdx.x);
+  uint64_t v[N], own = 0;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    v[k] = value(bin_at(p0 + k));
+    own += v[k];
+  }
   uint64_t total;
-  const uint64_t at = group_scan(v0 + v1, l.part, total);
+  uint64_t at = group_scan(own, l.part, total);
   if (threadIdx.x == 0 && total < want) {
     l.found = kBins;
     l.found_before = total;
   }
-  if (at < want && at + v0 >= want) {
-    l.found = bin_at(p0);
-    l.found_before = at;
-  } else if (at + v0 < want && at + v0 + v1 >= want) {
-    l.found = bin_at(p0 + 1);
-    l.found_before = at + v0;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    if (at < want && at + v[k] >= want) {
+      l.found = bin_at(p0 + k);
+      l.found_before = at;
+    }
+    at += v[k];
   }
   __syncthreads();
   before = l.found_before;
@@ -191,12 +229,42 @@ struct Logits {
       for (int k = 0; k < 4; ++k) f[k] = v[k];
     }
   }
-  // f(logit, id) of every token, over the workgroup; four vectors of a thread
-  // under way at a time
+  // f(logits, first id) of all tokens, over the workgroup: vectors, the next
+  // one under way, and single tokens at the ends
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
     const int tid = threadIdx.x;
-    if (tid < head) f(one(tid), tid);
+    if (tid < head) {
+      const float s[1] = {one(tid)};
+      f(s, tid);
+    }
+    constexpr int kStep = kThreads * VEC;
+    int i = head + tid * VEC;
+    if (i + VEC <= V) {
+      float cur[VEC];
+      many(i, cur);
+      for (;;) {
+        const int next = i + kStep;
+        const bool more = next + VEC <= V;
+        float ahead[VEC];
+        many(more ? next : i, ahead);
+        f(cur, i);
+        i = next;
+        if (!more) break;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) cur[k] = ahead[k];
+      }
+    }
+    for (int k = i; k < V && k < i + VEC; ++k) {
+      const float s[1] = {one(k)};
+      f(s, k);
+    }
+  }
+  // the largest logit that this thread meets; four vectors under way
+  __device__ __forceinline__ float largest() const {
+    const int tid = threadIdx.x;
+    float m = tid < head ? one(tid) : kNegInf;
+    m = fmaxf(m, kNegInf);
     constexpr int kStep = kThreads * VEC;
     int i = head + tid * VEC;
     for (; i + 3 * kStep + VEC <= V; i += 4 * kStep) {
@@ -206,18 +274,25 @@ struct Logits {
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) f(v[u][k], i + u * kStep + k);
+        for (int k = 0; k < VEC; ++k) m = fmaxf(m, v[u][k]);
     }
     for (; i + VEC <= V; i += kStep) {
       float v[VEC];
       many(i, v);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) f(v[k], i + k);
+      for (int k = 0; k < VEC; ++k) m = fmaxf(m, v[k]);
     }
-    if (i < V)
-      for (int k = i; k < V; ++k) f(one(k), k);
+    for (int k = i; k < V && k < i + VEC; ++k) m = fmaxf(m, one(k));
+    return m;
   }
 };
+
+// f of each of N values
+template <int N, typename F>
+__device__ __forceinline__ void one_by_one(const float (&v)[N], int id, F f) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) f(v[k], id + k);
+}
 
 // Digits of a radix search: bits [down, up) of the key.
 __device__ __forceinline__ int digit_up(int level) {
@@ -320,55 +395,52 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
   x.head = min(V, static_cast<int>((-reinterpret_cast<uintptr_t>(x.x) & 15) /
                                    (16 / VEC)));
 
-  // ---- the largest logit and its first id
+  // ---- the largest logit
   if (tid < kFine) l.powers[tid] = exp2(tid / static_cast<double>(kFine));
-  uint32_t top = 0;
-  int first = 0x7fffffff;
-  // (a thread meets its ids in rising order, but for its last few)
-  x.each([&](float f, int v) {
-    const uint32_t k = key_of(f);
-    if (k > top || (k == top && v < first)) {
-      top = k;
-      first = v;
-    }
-  });
-  uint64_t best = static_cast<uint64_t>(top) << 32 | static_cast<uint32_t>(~first);
+  float fmax_ = x.largest();
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    const uint64_t o = __shfl_xor(static_cast<unsigned long long>(best), off);
-    best = o > best ? o : best;
+  for (int off = 32; off >= 1; off >>= 1)
+    fmax_ = fmaxf(fmax_, __shfl_xor(fmax_, off));
+  if (tid == 0) {
+    l.nears = 0;
+    l.listed = 0;
+    l.low = 0xffffffffu;
+    l.tied = 0;
   }
-  if (lane == 0) l.part[wave] = best;
+  if (lane == 0) l.part[wave] = __float_as_uint(fmax_);
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) best = l.part[w] > best ? l.part[w] : best;
-  top = static_cast<uint32_t>(best >> 32);
-  first = static_cast<int>(~static_cast<uint32_t>(best));
+  for (int w = 0; w < kWaves; ++w)
+    fmax_ = fmaxf(fmax_, __uint_as_float(static_cast<uint32_t>(l.part[w])));
+  fmax_ = clean(fmax_);
   const float T = a.temp ? a.temp[b] : 1.f;
-  if (!(T > 0.f) || of_key(top) == kNegInf) {
+  if (!(T > 0.f) || fmax_ == kNegInf) {
+    // its first id
+    uint32_t first = 0xffffffffu;
+    x.each([&](const auto& f, int v) {
+      one_by_one(f, v, [&](float g, int id) {
+        if (clean(g) == fmax_) first = min(first, static_cast<uint32_t>(id));
+      });
+    });
+    if (first != 0xffffffffu) atomicMin(&l.low, first);
+    __syncthreads();
     if (tid == 0) {
-      a.token[row] = first;
+      a.token[row] = static_cast<int>(l.low);
       if (a.logp) a.logp[row] = 0.f;
     }
     return;
   }
-  const float fmax_ = of_key(top);
   Row r;
   r.max = fmax_;
   r.rate = 1.4426950408889634 / static_cast<double>(T);
   r.shift = a.shift;
   r.powers = l.powers;
   const int k_raw = a.top_k ? a.top_k[b] : 0;
-  const bool use_k = k_raw > 0 && k_raw < V;
+  bool use_k = k_raw > 0 && k_raw < V;
   const float p = a.top_p ? a.top_p[b] : 1.f;
   const bool use_p = p < 1.f;
   const double pd = p > 0.f ? static_cast<double>(p) : 0.0;
   const float least = a.min_p ? a.min_p[b] : 0.f;
-  // weights of less than half a unit are zero: those of logits below `cut` (by
-  // a margin that its rounding to fp32 cannot reach); that of -inf always
-  r.cut = static_cast<float>(
-      fmax(r.max - (r.shift + 1.01) / r.rate - 1e-6 * fabs(r.max),
-           -3.4028234663852886e38));
   uint64_t qmin = 1;
   if (least > 0.f) {
     const double m = least < 1.f ? static_cast<double>(least) : 1.0;
@@ -376,60 +448,86 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
     qmin = q > 1 ? q : 1;
   }
 
-  // ---- the bins of the runs' ends
-  const float rate = static_cast<float>(fmin(r.rate * kBinsPerUnit, 1e30));
-  auto bin_of = [&](uint32_t key) {
-    return static_cast<int>(
-        fminf((fmax_ - of_key(key)) * rate, static_cast<float>(kBins - 1)));
-  };
-  int lo = kBins - 1, hi = lo - 1;      // bins lo .. hi and kb are collected,
-  int kb = -1;                          // those below lo are kept whole
+  // ---- the bins of the runs' ends: bins lo .. hi and kb, those below lo are
+  // kept whole
+  int lo = kBins, hi = kBins - 1, kb = -1;
   uint64_t k_left = 0, k_above = 0;     // tokens of bin kb; weights above it
   uint64_t p_above = 0;                 // weights above bin lo
-  if (use_k || use_p) {
+  float rate = 0.f;
+  // (falls with the logit, so bins are in the order of the keys; -inf last)
+  auto place = [&](float f) { return (fmax_ - f) * rate; };
+  auto bin_of = [&](uint32_t key) {
+    return static_cast<int>(fminf(place(of_key(key)), 1e6f));
+  };
+  for (float units = kUnits; use_k || use_p; units = kAllUnits) {
+    rate = static_cast<float>(fmin(r.rate * (kBins / units), 1e30));
     for (int j = tid; j < kBins; j += kThreads) {
       l.sum[j] = 0;
       l.count[j] = 0;
     }
-    if (tid == 0) l.listed = 0;
+    if (tid == 0) l.nears = 0;
     __syncthreads();
-    x.each([&](float f, int) {
-      const uint32_t k = key_of(f);
-      const int bin = bin_of(k);
-      if (bin >= kBins - 1) return;
-      if (use_k) atomicAdd(&l.count[bin], 1u);
+    uint64_t all = 0;
+    bool room = true;                   // in the list, as far as this wave saw
+    x.each([&](const auto& f, int v) {
+      constexpr int N = sizeof(f) / sizeof(float);
+      // weights of a vector side by side: each is a chain of fp64 operations
+      // and an LDS read
+      uint64_t q[N] = {};
       if (use_p) {
-        const uint64_t q = r.weight(of_key(k));
-        if (q)
-          atomicAdd(reinterpret_cast<unsigned long long*>(&l.sum[bin]),
-                    static_cast<unsigned long long>(q));
+#pragma unroll
+        for (int k = 0; k < N; ++k) q[k] = r.weight(clean(f[k]));
+#pragma unroll
+        for (int k = 0; k < N; ++k) all += q[k];
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float at = place(clean(f[k]));
+        if (at < static_cast<float>(kBins)) {
+          const int bin = static_cast<int>(at);
+          if (use_k) atomicAdd(&l.count[bin], 1u);
+          if (use_p)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&l.sum[bin]),
+                      static_cast<unsigned long long>(q[k]));
+          if (room) room = push(l.near, &l.nears, kNear, entry(f[k], v + k));
+        }
       }
     });
     __syncthreads();
     auto same = [](int j) { return j; };
     auto sums = [&](int j) { return l.sum[j]; };
+    bool below = false;                 // an end lies below the bins
     if (use_k) {
       uint64_t before;
       const uint32_t f = find_bin(
           l, [&](int j) { return static_cast<uint64_t>(l.count[j]); }, same,
           static_cast<uint64_t>(k_raw), before);
-      // (fewer tokens than k have a weight: no limit)
       if (f < kBins) {
         kb = static_cast<int>(f);
         k_left = k_raw - before;
+      } else if (units == kAllUnits) {
+        use_k = false;                  // fewer than k have a weight: no limit
+      } else {
+        below = true;
       }
     }
-    if (use_p) {
+    if (use_p && !below) {
       // what top-k leaves weighs at least the bins above kb, at most kb too
-      uint64_t most = l.sum[2 * tid] * (kb < 0 || 2 * tid <= kb) +
-                      l.sum[2 * tid + 1] * (kb < 0 || 2 * tid + 1 <= kb);
-      most = group_sum(most, l.part);
-      k_above = kb < 0 ? most : most - l.sum[kb];
-      uint64_t before;
-      lo = static_cast<int>(find_bin(l, sums, same, share(pd, k_above), before));
-      p_above = before;
-      hi = lo;
+      uint64_t most;
+      if (kb < 0) {
+        most = group_sum(all, l.part);
+        k_above = most;
+      } else {
+        uint64_t some = 0;
+        for (int j = tid; j <= kb; j += kThreads) some += l.sum[j];
+        most = group_sum(some, l.part);
+        k_above = most - l.sum[kb];
+      }
+      const uint32_t f = find_bin(l, sums, same, share(pd, k_above), p_above);
+      below = f >= kBins;
+      lo = hi = static_cast<int>(f);
       if (kb >= 0) {
+        uint64_t before;
         __syncthreads();
         hi = static_cast<int>(find_bin(l, sums, same, share(pd, most), before));
       }
@@ -437,6 +535,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
       lo = hi = kb;
     }
     __syncthreads();
+    if (!below) break;
   }
 
   // ---- sums of each segment: what is above the ends' bins; those bins' tokens
@@ -445,43 +544,76 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
   const int seg = a.seg;
   const int nseg = max(1, (V - x.head + seg - 1) / seg);
   uint32_t tkey = 0, ties = 0;
-  const bool ends = lo <= hi || kb >= 0;
+  const bool ends = use_k || use_p;
   auto in_list = [&](int bin) { return (bin >= lo && bin <= hi) || bin == kb; };
-  for (int s = wave; s < nseg; s += kWaves) {
-    uint64_t sum = 0;
-    auto take = [&](float f, int v) {
-      const uint32_t k = key_of(f);
-      if (ends) {
-        const int bin = bin_of(k);
-        if (bin >= lo) {
-          if (in_list(bin)) {
-            const uint32_t at = atomicAdd(&l.listed, 1u);
-            if (at < kList)
-              l.list[at] = static_cast<uint64_t>(k) << 32 |
-                           static_cast<uint32_t>(v);
-          }
-          return;
-        }
-      }
+  auto segment_of = [&](int v) { return max(v - x.head, 0) / seg; };
+  auto id_of = [](uint64_t e) {
+    return static_cast<int>(~static_cast<uint32_t>(e));
+  };
+  if (ends && l.nears <= kNear) {
+    // all that can be kept is in LDS
+    if (tid < kSegs) l.sum[tid] = 0;
+    __syncthreads();
+    for (uint32_t j = tid; j < l.nears; j += kThreads) {
+      const uint64_t e = l.near[j];
+      const uint32_t k = static_cast<uint32_t>(e >> 32);
+      const int bin = bin_of(k);
+      if (in_list(bin)) push(l.list, &l.listed, kList, e);
+      if (bin >= lo) continue;
       const uint64_t q = r.weight(of_key(k));
-      sum += q >= qmin ? q : 0;
-    };
-    if (s == 0 && lane < x.head) take(x.one(lane), lane);
-    const int end = min(V, x.head + (s + 1) * seg);
-    int v = x.head + s * seg + lane * VEC;
-    for (; v + VEC <= end; v += kWave * VEC) {
-      float f[VEC];
-      x.many(v, f);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) take(f[k], v + k);
+      if (q >= qmin)
+        atomicAdd(reinterpret_cast<unsigned long long*>(
+                      &l.sum[segment_of(id_of(e))]),
+                  static_cast<unsigned long long>(q));
     }
-    for (int k = v; k < end && k < v + VEC; ++k) take(x.one(k), k);
-    if (ballot(sum != 0)) {
+  } else {
+    for (int s = wave; s < nseg; s += kWaves) {
+      uint64_t sum = 0;
+      auto take = [&](const auto& f, int v) {
+        constexpr int N = sizeof(f) / sizeof(float);
+        bool whole[N], any = !ends;
 #pragma unroll
-      for (int off = 32; off >= 1; off >>= 1)
-        sum += __shfl_xor(static_cast<unsigned long long>(sum), off);
+        for (int k = 0; k < N; ++k) {
+          whole[k] = true;
+          if (ends) {
+            const float at = place(clean(f[k]));
+            whole[k] = at < static_cast<float>(lo);
+            any = any || whole[k];
+            if (!whole[k] && at < static_cast<float>(kBins) &&
+                in_list(static_cast<int>(at)))
+              push(l.list, &l.listed, kList, entry(f[k], v + k));
+          }
+        }
+        if (!any) return;
+        uint64_t q[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) q[k] = r.weight(clean(f[k]));
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          sum += whole[k] && (qmin == 1 || q[k] >= qmin) ? q[k] : 0;
+      };
+      if (s == 0 && lane < x.head) {
+        const float f[1] = {x.one(lane)};
+        take(f, lane);
+      }
+      const int end = min(V, x.head + (s + 1) * seg);
+      int v = x.head + s * seg + lane * VEC;
+      for (; v + VEC <= end; v += kWave * VEC) {
+        float f[VEC];
+        x.many(v, f);
+        take(f, v);
+      }
+      for (int k = v; k < end && k < v + VEC; ++k) {
+        const float f[1] = {x.one(k)};
+        take(f, k);
+      }
+      if (ballot(sum != 0)) {
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1)
+          sum += __shfl_xor(static_cast<unsigned long long>(sum), off);
+      }
+      if (lane == 0) l.sum[s] = sum;
     }
-    if (lane == 0) l.sum[s] = sum;
   }
   __syncthreads();
 
@@ -489,42 +621,83 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
     const int n = static_cast<int>(l.listed);
     const bool small = n <= kList;
     // the sums by segment wait in registers while the searches use the bins
-    uint64_t mine = tid < nseg ? l.sum[tid] : 0;
-    auto list_keys = [&](auto f) {
-      for (int j = tid; j < n; j += kThreads)
-        f(static_cast<uint32_t>(l.list[j] >> 32));
-    };
-    auto row_keys = [&](auto f) {
-      x.each([&](float g, int) { f(key_of(g)); });
-    };
-    uint32_t kkey = 0, kties = 0;
-    if (kb >= 0) {
-      if (small)
-        kth_key(l, [&](auto f) {
-          list_keys([&](uint32_t k) { if (bin_of(k) == kb) f(k); });
-        }, k_left, kkey, kties);
-      else
-        kth_key(l, row_keys, static_cast<uint64_t>(k_raw), kkey, kties);
-      tkey = kkey;
-      ties = kties;
-    }
-    if (use_p) {
-      // the weight of all that top-k left
-      uint64_t total = 0;
-      if (kb >= 0) {
-        auto add = [&](uint32_t k) {
-          if (k > kkey && bin_of(k) == kb) total += r.weight(of_key(k));
-        };
-        if (small) list_keys(add);
-        else row_keys(add);
-        total = group_sum(total, l.part) + kties * r.weight(of_key(kkey));
+    const uint64_t mine = tid < nseg ? l.sum[tid] : 0;
+    if (n <= kPairs) {
+      // a thread per token, which compares itself with all of them
+      uint64_t e = 0, q = 0;
+      bool kept = tid < n;
+      if (kept) {
+        e = l.list[tid];
+        const uint32_t k = static_cast<uint32_t>(e >> 32);
+        q = r.weight(of_key(k));
+        if (kb >= 0 && bin_of(k) == kb) {
+          uint64_t rank = 0;
+          for (int j = 0; j < n; ++j)
+            rank += l.list[j] > e &&
+                            bin_of(static_cast<uint32_t>(l.list[j] >> 32)) == kb
+                        ? 1 : 0;
+          kept = rank < k_left;
+        }
       }
-      total += k_above;
-      const uint64_t want = share(pd, total);
-      if (small)
-        pth_key(l, r, list_keys, kkey, kties, want - p_above, tkey, ties);
-      else
-        pth_key(l, r, row_keys, kkey, kties, want, tkey, ties);
+      if (use_p) {
+        const bool at_kb =
+            kept && kb >= 0 && bin_of(static_cast<uint32_t>(e >> 32)) == kb;
+        const uint64_t total =
+            k_above + (kb >= 0 ? group_sum(at_kb ? q : 0, l.part) : 0);
+        if (tid < n) l.weights[tid] = kept ? q : 0;
+        __syncthreads();
+        if (kept) {
+          uint64_t before = 0;
+          for (int j = 0; j < n; ++j) before += l.list[j] > e ? l.weights[j] : 0;
+          kept = before < share(pd, total) - p_above;
+        }
+      }
+      // the last kept key and its kept ties
+      if (kept) atomicMin(&l.low, static_cast<uint32_t>(e >> 32));
+      __syncthreads();
+      tkey = l.low;
+      if (kept && static_cast<uint32_t>(e >> 32) == tkey) atomicAdd(&l.tied, 1u);
+      __syncthreads();
+      ties = l.tied;
+    } else {
+      auto list_keys = [&](auto f) {
+        for (int j = tid; j < n; j += kThreads)
+          f(static_cast<uint32_t>(l.list[j] >> 32));
+      };
+      auto row_keys = [&](auto f) {
+        x.each([&](const auto& g, int v) {
+          one_by_one(g, v, [&](float h, int) { f(key_of(h)); });
+        });
+      };
+      uint32_t kkey = 0, kties = 0;
+      if (kb >= 0) {
+        if (small)
+          kth_key(l, [&](auto f) {
+            list_keys([&](uint32_t k) { if (bin_of(k) == kb) f(k); });
+          }, k_left, kkey, kties);
+        else
+          kth_key(l, row_keys, static_cast<uint64_t>(k_raw), kkey, kties);
+        tkey = kkey;
+        ties = kties;
+      }
+      if (use_p) {
+        // the weight of all that top-k left
+        uint64_t total = 0;
+        if (kb >= 0) {
+          auto add = [&](uint32_t k) {
+            if (k > kkey && bin_of(k) == kb) total += r.weight(of_key(k));
+          };
+          if (small) list_keys(add);
+          else row_keys(add);
+          total = group_sum(total, l.part) + kties * r.weight(of_key(kkey));
+        }
+        total += k_above;
+        const uint64_t want = share(pd, total);
+        if (small)
+          pth_key(l, r, list_keys, kkey, kties, want - p_above, tkey, ties);
+        else
+          pth_key(l, r, row_keys, kkey, kties, want, tkey, ties);
+      }
     }
     // the kept tokens of the ends' bins, and the ties of each segment
     __syncthreads();
@@ -535,22 +708,22 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
     __syncthreads();
     auto keep = [&](uint32_t k, int v) {
       if (k < tkey || !in_list(bin_of(k))) return;
-      const int s = max(v - x.head, 0) / seg;
       if (k == tkey) {
-        atomicAdd(&l.count[s], 1u);
+        atomicAdd(&l.count[segment_of(v)], 1u);
         return;
       }
       const uint64_t q = r.weight(of_key(k));
       if (q >= qmin)
-        atomicAdd(reinterpret_cast<unsigned long long*>(&l.sum[s]),
+        atomicAdd(reinterpret_cast<unsigned long long*>(&l.sum[segment_of(v)]),
                   static_cast<unsigned long long>(q));
     };
     if (small) {
       for (int j = tid; j < n; j += kThreads)
-        keep(static_cast<uint32_t>(l.list[j] >> 32),
-             static_cast<int>(static_cast<uint32_t>(l.list[j])));
+        keep(static_cast<uint32_t>(l.list[j] >> 32), id_of(l.list[j]));
     } else {
-      x.each([&](float f, int v) { keep(key_of(f), v); });
+      x.each([&](const auto& f, int v) {
+        one_by_one(f, v, [&](float g, int id) { keep(key_of(g), id); });
+      });
     }
     __syncthreads();
   }
