@@ -10,11 +10,13 @@
 // the comparison of running sums with u * total need.
 // Passes over a row (the first from HBM, the others from the caches):
 //   1. the largest logit;
-//   2. with top-k or top-p: the sum of all weights, and a histogram (tokens and
-//      weights) of the logits near the top, which tells the bins that the ends
-//      of top-k's and top-p's runs lie in.  Those logits go into a list too; a
-//      row whose list does not overflow is not read again.  (If an end lies
-//      further down, the pass is done again over all that has a weight.)
+//   2. with top-k: the logits that can be among the first k, into a list (the
+//      parts' maxima of pass 1 bound them from below); with top-p alone: the
+//      sum of all weights, and a histogram of the logits near the top.  A
+//      histogram (tokens and weights) tells the bins that the ends of top-k's
+//      and top-p's runs lie in.  A row whose list does not overflow is not read
+//      again.  (If an end lies below the histogram, the pass is done again over
+//      all that has a weight.)
 //   3. otherwise the weights of the tokens that are surely kept, summed by
 //      segments of consecutive ids, and the tokens of the ends' bins collected.
 // The exact ends are found among the tokens of their bins: by comparing all
@@ -260,11 +262,13 @@ struct Logits {
       f(s, k);
     }
   }
-  // the largest logit that this thread meets; four vectors under way
-  __device__ __forceinline__ float largest() const {
+  // the largest logits that this thread meets, by their place in a vector;
+  // four vectors under way
+  __device__ __forceinline__ void largest(float (&m)[VEC]) const {
     const int tid = threadIdx.x;
-    float m = tid < head ? one(tid) : kNegInf;
-    m = fmaxf(m, kNegInf);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) m[k] = kNegInf;
+    if (tid < head) m[0] = fmaxf(m[0], one(tid));
     constexpr int kStep = kThreads * VEC;
     int i = head + tid * VEC;
     for (; i + 3 * kStep + VEC <= V; i += 4 * kStep) {
@@ -274,16 +278,15 @@ struct Logits {
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) m = fmaxf(m, v[u][k]);
+        for (int k = 0; k < VEC; ++k) m[k] = fmaxf(m[k], v[u][k]);
     }
     for (; i + VEC <= V; i += kStep) {
       float v[VEC];
       many(i, v);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) m = fmaxf(m, v[k]);
+      for (int k = 0; k < VEC; ++k) m[k] = fmaxf(m[k], v[k]);
     }
-    for (int k = i; k < V && k < i + VEC; ++k) m = fmaxf(m, one(k));
-    return m;
+    for (int k = i; k < V && k < i + VEC; ++k) m[0] = fmaxf(m[0], one(k));
   }
 };
 
@@ -397,7 +400,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
 
   // ---- the largest logit
   if (tid < kFine) l.powers[tid] = exp2(tid / static_cast<double>(kFine));
-  float fmax_ = x.largest();
+  float some[VEC];        // the largest of kThreads * VEC parts of the row
+  x.largest(some);
+  float fmax_ = some[0];
+#pragma unroll
+  for (int k = 1; k < VEC; ++k) fmax_ = fmaxf(fmax_, some[k]);
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1)
     fmax_ = fmaxf(fmax_, __shfl_xor(fmax_, off));
@@ -415,13 +422,33 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
   fmax_ = clean(fmax_);
   const float T = a.temp ? a.temp[b] : 1.f;
   if (!(T > 0.f) || fmax_ == kNegInf) {
-    // its first id
+    // its first id: among the parts that it is the maximum of, a thread per
+    // vector, and the ends; over the whole row if it is that of many
     uint32_t first = 0xffffffffu;
-    x.each([&](const auto& f, int v) {
-      one_by_one(f, v, [&](float g, int id) {
-        if (clean(g) == fmax_) first = min(first, static_cast<uint32_t>(id));
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+      if (clean(some[k]) == fmax_)
+        push(l.list, &l.listed, kPairs, static_cast<uint64_t>(tid * VEC + k));
+    __syncthreads();
+    const int n = static_cast<int>(l.listed);
+    auto look = [&](int v) {
+      if (v >= 0 && v < V && clean(x.one(v)) == fmax_)
+        first = min(first, static_cast<uint32_t>(v));
+    };
+    if (n <= kPairs) {
+      for (int j = 0; j < n; ++j)
+        for (int v = x.head + static_cast<int>(l.list[j]) + tid * kThreads * VEC;
+             v < V; v += kThreads * kThreads * VEC)
+          look(v);
+      if (tid < VEC) {
+        if (tid < x.head) look(tid);
+        look(V - 1 - tid);
+      }
+    } else {
+      x.each([&](const auto& f, int v) {
+        one_by_one(f, v, [&](float, int id) { look(id); });
       });
-    });
+    }
     if (first != 0xffffffffu) atomicMin(&l.low, first);
     __syncthreads();
     if (tid == 0) {
@@ -459,14 +486,106 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
   auto bin_of = [&](uint32_t key) {
     return static_cast<int>(fminf(place(of_key(key)), 1e6f));
   };
-  for (float units = kUnits; use_k || use_p; units = kAllUnits) {
-    rate = static_cast<float>(fmin(r.rate * (kBins / units), 1e30));
+  auto same = [](int j) { return j; };
+  auto counts = [&](int j) { return static_cast<uint64_t>(l.count[j]); };
+  auto sums = [&](int j) { return l.sum[j]; };
+  auto clear = [&]() {
     for (int j = tid; j < kBins; j += kThreads) {
       l.sum[j] = 0;
       l.count[j] = 0;
     }
     if (tid == 0) l.nears = 0;
     __syncthreads();
+  };
+  // From the bins' counts and weights (`all`: this thread's part of the weight
+  // of all tokens): true if an end lies below the bins, which `last` excludes.
+  auto locate = [&](uint64_t all, bool last) {
+    if (use_k) {
+      uint64_t before;
+      const uint32_t f =
+          find_bin(l, counts, same, static_cast<uint64_t>(k_raw), before);
+      if (f < kBins) {
+        kb = static_cast<int>(f);
+        k_left = k_raw - before;
+      } else if (last) {
+        use_k = false;                  // fewer than k have a weight: no limit
+      } else {
+        return true;
+      }
+    }
+    if (use_p) {
+      // what top-k leaves weighs at least the bins above kb, at most kb too
+      uint64_t most;
+      if (kb < 0) {
+        most = group_sum(all, l.part);
+        k_above = most;
+      } else {
+        uint64_t part = 0;
+        for (int j = tid; j <= kb; j += kThreads) part += l.sum[j];
+        most = group_sum(part, l.part);
+        k_above = most - l.sum[kb];
+      }
+      const uint32_t f = find_bin(l, sums, same, share(pd, k_above), p_above);
+      lo = hi = static_cast<int>(f);
+      if (f >= kBins) return true;
+      if (kb >= 0) {
+        uint64_t before;
+        hi = static_cast<int>(find_bin(l, sums, same, share(pd, most), before));
+      }
+    } else if (kb >= 0) {
+      lo = hi = kb;
+    }
+    return false;
+  };
+  bool placed = false;
+  if (use_k && k_raw <= kThreads * VEC / 2) {
+    // The k-th largest of the parts' maxima is not above the k-th largest
+    // logit, and mostly near it: one pass collects what is above its bin.
+    rate = static_cast<float>(fmin(r.rate * (kBins / kAllUnits), 1e30));
+    clear();
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      const float at = place(clean(some[k]));
+      if (at < static_cast<float>(kBins))
+        atomicAdd(&l.count[static_cast<int>(at)], 1u);
+    }
+    __syncthreads();
+    uint64_t before;
+    const uint32_t f =
+        find_bin(l, counts, same, static_cast<uint64_t>(k_raw), before);
+    if (f < kBins) {
+      const float most = static_cast<float>(f + 1);
+      bool room = true;
+      x.each([&](const auto& g, int v) {
+        one_by_one(g, v, [&](float h, int id) {
+          if (place(clean(h)) < most && room)
+            room = push(l.near, &l.nears, kNear, entry(h, id));
+        });
+      });
+      __syncthreads();
+      const uint32_t n = l.nears;
+      if (n <= kNear) {
+        __syncthreads();
+        clear();
+        for (uint32_t j = tid; j < n; j += kThreads) {
+          const uint32_t k = static_cast<uint32_t>(l.near[j] >> 32);
+          const int bin = bin_of(k);
+          atomicAdd(&l.count[bin], 1u);
+          if (use_p)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&l.sum[bin]),
+                      static_cast<unsigned long long>(r.weight(of_key(k))));
+        }
+        if (tid == 0) l.nears = n;
+        __syncthreads();
+        locate(0, true);
+        placed = true;
+      }
+    }
+    __syncthreads();
+  }
+  for (float units = kUnits; !placed && (use_k || use_p); units = kAllUnits) {
+    rate = static_cast<float>(fmin(r.rate * (kBins / units), 1e30));
+    clear();
     uint64_t all = 0;
     bool room = true;                   // in the list, as far as this wave saw
     x.each([&](const auto& f, int v) {
@@ -494,48 +613,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
       }
     });
     __syncthreads();
-    auto same = [](int j) { return j; };
-    auto sums = [&](int j) { return l.sum[j]; };
-    bool below = false;                 // an end lies below the bins
-    if (use_k) {
-      uint64_t before;
-      const uint32_t f = find_bin(
-          l, [&](int j) { return static_cast<uint64_t>(l.count[j]); }, same,
-          static_cast<uint64_t>(k_raw), before);
-      if (f < kBins) {
-        kb = static_cast<int>(f);
-        k_left = k_raw - before;
-      } else if (units == kAllUnits) {
-        use_k = false;                  // fewer than k have a weight: no limit
-      } else {
-        below = true;
-      }
-    }
-    if (use_p && !below) {
-      // what top-k leaves weighs at least the bins above kb, at most kb too
-      uint64_t most;
-      if (kb < 0) {
-        most = group_sum(all, l.part);
-        k_above = most;
-      } else {
-        uint64_t some = 0;
-        for (int j = tid; j <= kb; j += kThreads) some += l.sum[j];
-        most = group_sum(some, l.part);
-        k_above = most - l.sum[kb];
-      }
-      const uint32_t f = find_bin(l, sums, same, share(pd, k_above), p_above);
-      below = f >= kBins;
-      lo = hi = static_cast<int>(f);
-      if (kb >= 0) {
-        uint64_t before;
-        __syncthreads();
-        hi = static_cast<int>(find_bin(l, sums, same, share(pd, most), before));
-      }
-    } else if (kb >= 0) {
-      lo = hi = kb;
-    }
+    placed = !locate(all, units == kAllUnits);
     __syncthreads();
-    if (!below) break;
   }
 
   // ---- sums of each segment: what is above the ends' bins; those bins' tokens
