@@ -232,8 +232,8 @@ struct Logits {
     }
   }
   // f(logits, first id) of all tokens, over the workgroup: vectors, the next
-  // one under way, and single tokens at the ends
-  template <typename F>
+  // AHEAD under way, and single tokens at the ends
+  template <int AHEAD, typename F>
   __device__ __forceinline__ void each(F f) const {
     const int tid = threadIdx.x;
     if (tid < head) {
@@ -243,18 +243,17 @@ struct Logits {
     constexpr int kStep = kThreads * VEC;
     int i = head + tid * VEC;
     if (i + VEC <= V) {
-      float cur[VEC];
-      many(i, cur);
-      for (;;) {
-        const int next = i + kStep;
-        const bool more = next + VEC <= V;
-        float ahead[VEC];
-        many(more ? next : i, ahead);
-        f(cur, i);
-        i = next;
-        if (!more) break;
+      const int last = i + (V - VEC - i) / kStep * kStep;
+      float v[AHEAD + 1][VEC];
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) cur[k] = ahead[k];
+      for (int u = 0; u < AHEAD; ++u) many(min(i + u * kStep, last), v[u]);
+      for (; i <= last; i += kStep) {
+        many(min(i + AHEAD * kStep, last), v[AHEAD]);
+        f(v[0], i);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) v[u][k] = v[u + 1][k];
       }
     }
     for (int k = i; k < V && k < i + VEC; ++k) {
@@ -381,8 +380,11 @@ __device__ __forceinline__ uint64_t share(double p, uint64_t total) {
   return s < 1 ? 1 : s;
 }
 
+// (registers for two workgroups a CU: one's barriers and short searches run
+// under the other's passes)
 template <bool HALF>
-__global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
   __shared__ Lds l;
   const int row = blockIdx.x, b = row / a.W, i = row - b * a.W;
   if (a.n_obs && i < a.n_obs[b]) return;
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
         look(V - 1 - tid);
       }
     } else {
-      x.each([&](const auto& f, int v) {
+      x.template each<1>([&](const auto& f, int v) {
         one_by_one(f, v, [&](float, int id) { look(id); });
       });
     }
@@ -556,7 +558,13 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
     if (f < kBins) {
       const float most = static_cast<float>(f + 1);
       bool room = true;
-      x.each([&](const auto& g, int v) {
+      x.template each<4>([&](const auto& g, int v) {
+        // (one question for a vector: few have any)
+        constexpr int N = sizeof(g) / sizeof(float);
+        float top = kNegInf;
+#pragma unroll
+        for (int k = 0; k < N; ++k) top = fmaxf(top, g[k]);
+        if (!(place(clean(top)) < most) || !room) return;
         one_by_one(g, v, [&](float h, int id) {
           if (place(clean(h)) < most && room)
             room = push(l.near, &l.nears, kNear, entry(h, id));
@@ -588,7 +596,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
     clear();
     uint64_t all = 0;
     bool room = true;                   // in the list, as far as this wave saw
-    x.each([&](const auto& f, int v) {
+    x.template each<2>([&](const auto& f, int v) {
       constexpr int N = sizeof(f) / sizeof(float);
       // weights of a vector side by side: each is a chain of fp64 operations
       // and an LDS read
@@ -744,7 +752,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
           f(static_cast<uint32_t>(l.list[j] >> 32));
       };
       auto row_keys = [&](auto f) {
-        x.each([&](const auto& g, int v) {
+        x.template each<1>([&](const auto& g, int v) {
           one_by_one(g, v, [&](float h, int) { f(key_of(h)); });
         });
       };
@@ -800,7 +808,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(Args a) {
       for (int j = tid; j < n; j += kThreads)
         keep(static_cast<uint32_t>(l.list[j] >> 32), id_of(l.list[j]));
     } else {
-      x.each([&](const auto& f, int v) {
+      x.template each<1>([&](const auto& f, int v) {
         one_by_one(f, v, [&](float g, int id) { keep(key_of(g), id); });
       });
     }
