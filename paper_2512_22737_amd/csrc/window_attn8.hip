@@ -1,11 +1,13 @@
 // The window attention over a paged cache of e4m3 codes with one power-of-two
 // scale per page and kv head (wedlm_window_attn_cache8).
 //
+// Work: a workgroup takes (sequence, kv head, query group, prefix split).
 // Query rows of one kv head are packed as in the bf16 kernel (row r = i*G + j
-// is window row i, query head kvh*G + j); a wave owns 32 of them and walks
-// 32-key tiles (two pages).  S^T = K Q^T and O^T += V^T P^T run on
-// v_mfma_f32_32x32x16_bf16: e4m3 values are exact in bf16, so the codes are
-// converted on the way into the products and nothing else is rounded than
+// is window row i, query head kvh*G + j); a wave owns 32 of them.  Up to 32
+// rows two waves share them and take every other 32-key tile; more rows go to
+// up to eight waves that all read every tile.  S^T = K Q^T and O^T += V^T P^T
+// run on v_mfma_f32_32x32x16_bf16: e4m3 values are exact in bf16, so the codes
+// are converted on the way into the products and nothing else is rounded than
 // over a bf16 cache.
 // Orders.  A lane's 16 bytes of a key row are 16 values of d: the K and Q
 // operands take d in that order (products do not care), so a lane reads whole
@@ -13,7 +15,12 @@
 // half hf with the 16 keys of page hf: its K scale is then one factor per
 // lane, folded into the softmax's, and its 16 weights meet the 16 bytes of a
 // V^T row of that page, whose scale the conversion applies.
-// Softmax, split of the prefix and its merge are those of the bf16 kernel.
+// Loads.  64 keys (four pages) are a step: 16 KB with D = 128, straight from
+// HBM into a ring of four steps in LDS, three ahead; one barrier a step.  The
+// split's page ids and exponents are staged in LDS first.
+// Softmax: log2 domain, no maximum per tile (the reference maximum is the
+// first tile's and is raised when a sum passes 2^64), split of the prefix and
+// merge as for bf16 pages.
 #include "common.h"
 #include "wedlm_serve.h"
 
@@ -22,8 +29,17 @@ using namespace wedlm;
 namespace {
 
 constexpr int kTileKeys = 32;       // keys per tile (two 16-token pages)
-// A prefix split holds at least this many tiles.
+// A prefix split holds at least this many tiles, and at most 2048 pages (their
+// ids are staged in LDS).
 constexpr int kMinSplitTiles = 8;
+constexpr int kMaxSplitPages = 2048;
+// Workgroups that a launch aims at.
+constexpr int kWorkgroups = 1024;
+constexpr int kStepPages = 4;       // pages of a step
+constexpr int kSlots = 4;           // steps in the ring, kSlots - 1 ahead
+// A column's running sum may reach this before its reference max is raised
+// (every term 2^(s - m) is then at most 2^64, far inside fp32).
+constexpr float kSumLimit = 18446744073709551616.0f;  // 2^64
 constexpr float kLn2 = 0.69314718055994530942f;
 
 struct Args {
@@ -47,23 +63,27 @@ struct Args {
 };
 
 struct Plan {
-  int nw, qgroups, rows_pad, nsplit;
+  int nw, kw;             // waves, of which kw share the rows and split the keys
+  int qgroups, rows_pad, nsplit;
   size_t ws_bytes;
 };
 
 Plan make_plan(int B, int W, int Hq, int Hkv, int D, int max_prefix) {
   Plan p{};
   const int rows = W * (Hq / Hkv);
-  const int blocks = (rows + 31) / 32;
-  p.nw = blocks < 8 ? blocks : 8;
-  p.qgroups = (blocks + p.nw - 1) / p.nw;
-  p.rows_pad = p.qgroups * p.nw * 32;
+  p.kw = rows <= 32 ? 2 : 1;
+  p.nw = rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+  const int per = 32 * p.nw / p.kw;
+  p.qgroups = (rows + per - 1) / per;
+  p.rows_pad = p.qgroups * per;
   const int tiles = (max_prefix + kTileKeys - 1) / kTileKeys;
-  const int64_t waves = static_cast<int64_t>(B) * Hkv * p.qgroups * p.nw;
-  // about eight waves a CU
-  int64_t n = (2048 + waves - 1) / waves;
+  const int64_t base = static_cast<int64_t>(B) * Hkv * p.qgroups;
+  const int64_t want = kWorkgroups;
+  int64_t n = (want + base - 1) / base;
   const int most = tiles / kMinSplitTiles;
   if (n > most) n = most;
+  const int least = (tiles + kMaxSplitPages / 2 - 1) / (kMaxSplitPages / 2);
+  if (n < least) n = least;
   if (n < 1) n = 1;
   p.nsplit = static_cast<int>(n);
   if (p.nsplit > 1) {
@@ -121,12 +141,37 @@ __device__ __forceinline__ float scale_of(int e) {
   return __uint_as_float(static_cast<uint32_t>(e) << 23);
 }
 
+// LDS of one workgroup: the ring (K and V^T of each step), the pages' ids and
+// exponents.
+//   K    [4 pages][16 rows][D]: 16-byte chunk c of row r of page g sits in
+//        slot c ^ swz(r, g & 1), so that the 16 lanes of a read pass (rows 4a
+//        .. 4a+7 of two pages) meet 64 different banks
+//   V^T  [4 pages][D rows][16]
 template <int D>
-__global__ __launch_bounds__(8 * kWave)
+struct Lds {
+  static constexpr int kPageBytes = kPage * D;
+  static constexpr int kHalf = kStepPages * kPageBytes;   // K or V^T of a step
+  static constexpr int kStep = 2 * kHalf;
+  __device__ static __forceinline__ int swz(int r, int g) {
+    return D == 128 ? ((r >> 1) & 3) | (g << 2) : ((r >> 2) & 1) | (g << 1);
+  }
+};
+
+template <int D, int NW, int KW>
+__global__ __launch_bounds__(NW * kWave)
+__attribute__((amdgpu_waves_per_eu(NW == 2 ? 1 : 2)))
 void window_attn8_kernel(Args a) {
+  using L = Lds<D>;
   constexpr int NJ = D / 32;          // 16-byte pieces of a key row per half
   constexpr int NK = D / 16;          // k-steps of the score MFMA
   constexpr int NM = D / 32;          // 32-row blocks of O^T
+  constexpr int NQ = NW / KW;         // query blocks of a workgroup
+  constexpr int NT = NW * kWave;
+  constexpr int kLoads = L::kStep / 1024 / NW;   // of a wave per step
+  static_assert(L::kStep % (1024 * NW) == 0, "whole loads");
+  __shared__ __attribute__((aligned(1024))) char ring[kSlots * L::kStep];
+  __shared__ int32_t pg[kMaxSplitPages + kStepPages];
+  __shared__ uint16_t ex[kMaxSplitPages + kStepPages];
 
   int wg = blockIdx.x;
   const int split = wg % a.nsplit;
@@ -137,23 +182,11 @@ void window_attn8_kernel(Args a) {
   const int b = wg / a.Hkv;
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int nw = blockDim.x / kWave;
   const int lane = lane_id();
   const int col = lane & 31, hf = lane >> 5;
+  const int kw = KW == 1 ? 0 : wave / NQ;
   const int rows = a.W * a.G;
-  const int rb = (qg * nw + wave) * 32;
-
-  const int c = a.plen[b];
-  if (!len_ok(a, c)) {
-    if (a.status && threadIdx.x == 0 && split == 0 && qg == 0 && kvh == 0)
-      atomicOr(a.status + b, WEDLM_SEQ_BAD_LEN);
-    return;
-  }
-  const SeqSplit ss = seq_split(c, a.nsplit);
-  if (split >= ss.n || rb >= rows) return;
-  const int k0 = split * ss.len;
-  const int k1 = min(c, k0 + ss.len);
-  const bool last = split == ss.n - 1;
+  const int rb = (qg * NQ + wave % NQ) * 32;
 
   // ---- queries
   const int r = rb + col;
@@ -170,6 +203,76 @@ void window_attn8_kernel(Args a) {
       qf[2 * j + i] = __builtin_bit_cast(
           bf16x8_t,
           *reinterpret_cast<const u16x8_t*>(qp + 32 * j + 16 * hf + 8 * i));
+
+  const int c = a.plen[b];
+  if (!len_ok(a, c)) {
+    if (a.status && threadIdx.x == 0 && split == 0 && qg == 0 && kvh == 0)
+      atomicOr(a.status + b, WEDLM_SEQ_BAD_LEN);
+    return;
+  }
+  const SeqSplit ss = seq_split(c, a.nsplit);
+  if (split >= ss.n) return;
+  const int k0 = split * ss.len;
+  const int k1 = min(c, k0 + ss.len);
+  const bool last = split == ss.n - 1;
+  const int pages = (k1 - k0 + kPage - 1) / kPage;
+  const int steps = (pages + kStepPages - 1) / kStepPages;
+
+  // ---- the split's pages; an id outside the cache becomes page 0 (in bounds)
+  // and is told.  The last step is filled up with the last page.
+  const int32_t* btb = a.bt + static_cast<int64_t>(b) * a.max_pages + k0 / kPage;
+  for (int i = threadIdx.x; i < steps * kStepPages; i += NT) {
+    int id = btb[min(i, pages - 1)];
+    if (id < 0 || id >= a.num_pages) {
+      if (a.status) atomicOr(a.status + b, WEDLM_SEQ_BAD_PAGE);
+      id = 0;
+    }
+    pg[i] = id;
+  }
+  __syncthreads();
+  // the queries have arrived by now: taken here, once, so that no later use
+  // waits for loads that are under way then
+#pragma unroll
+  for (int kk = 0; kk < NK; ++kk) asm volatile("" : "+v"(qf[kk]));
+
+  // ---- loads of a step: piece u of this wave is kilobyte wave * kLoads + u of
+  // the step's K, then of its V^T.  Lane l's 16 bytes land at byte 16 l of it,
+  // so K's swizzle is in the lane's address.
+  constexpr int kPerPage = L::kPageBytes / 1024;          // kilobytes
+  const uint32_t lds0 =
+      static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void_t*)ring));
+  auto load_step = [&](int t) {
+    const int slot = t & (kSlots - 1);
+    t = min(t, steps - 1);            // (as many loads in every step)
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int kb = wave * kLoads + u;
+      const bool isv = kb >= L::kHalf / 1024;
+      const int p = kb % (L::kHalf / 1024) / kPerPage;    // page of the step
+      const int at = kb % kPerPage * 64 + lane;           // chunk of the page
+      int off = at * 16;
+      if (!isv) {
+        const int row = at / (D / 16), s = at % (D / 16);
+        off = row * D + ((s ^ L::swz(row, p & 1)) << 4);
+      }
+      const int id = __builtin_amdgcn_readfirstlane(pg[t * kStepPages + p]);
+      const uint8_t* base =
+          (isv ? a.v8 : a.k8) +
+          (static_cast<int64_t>(id) * a.Hkv + kvh) * L::kPageBytes;
+      load_to_lds16(buffer_rsrc(base, L::kPageBytes), off,
+                    __builtin_amdgcn_readfirstlane(
+                        lds0 + slot * L::kStep + kb * 1024));
+    }
+  };
+  if (steps > 0) {
+#pragma unroll
+    for (int t = 0; t < kSlots - 1; ++t) load_step(t);
+    // the exponents, under the first loads
+    for (int i = threadIdx.x; i < steps * kStepPages; i += NT) {
+      const int64_t at = static_cast<int64_t>(pg[i]) * a.Hkv + kvh;
+      ex[i] = static_cast<uint16_t>(a.ke[at] | a.ve[at] << 8);
+    }
+  }
 
   floatx16_t o[NM];
 #pragma unroll
@@ -188,29 +291,38 @@ void window_attn8_kernel(Args a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[m][e] *= alpha;
   };
-  // one tile's weights and products; x: scores in log2 units
-  auto finish = [&](float (&x)[16], const bf16x8_t (&vf)[2][NM], bool first) {
+  // largest of a column's 32 scores
+  auto col_max = [&](const floatx16_t& x) {
     float mx = x[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
     float x0, x1;
     xor32_pair(mx, x0, x1);
-    mx = fmaxf(x0, x1);
+    return fmaxf(x0, x1);
+  };
+  // weights 2^(x f - m2) in bf16 and l_run with their sum added
+  auto weigh = [&](const floatx16_t& x, float f, bf16x8_t (&pf)[2]) {
+    const float mc = m2 == kNegInf ? 0.f : m2;
+    float p[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, -mc));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = static_cast<__bf16>(p[e]);
+    float s[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      s[g] = (p[4 * g] + p[4 * g + 1]) + (p[4 * g + 2] + p[4 * g + 3]);
+    return l_run + ((s[0] + s[1]) + (s[2] + s[3]));
+  };
+  auto raise = [&](float mx) {
     if (ballot(mx > m2)) {
       const float m_new = fmaxf(m2, mx);
       rescale(m2 == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m2 - m_new));
       m2 = m_new;
     }
-    const float mc = m2 == kNegInf ? 0.f : m2;
-    bf16x8_t pf[2];
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float p = __builtin_amdgcn_exp2f(x[e] - mc);
-      sum += p;
-      pf[e >> 3][e & 7] = static_cast<__bf16>(p);
-    }
-    l_run += sum;
+  };
+  auto product = [&](const bf16x8_t (&vf)[2][NM], const bf16x8_t (&pf)[2]) {
 #pragma unroll
     for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
@@ -219,69 +331,11 @@ void window_attn8_kernel(Args a) {
                                                        0, 0, 0);
   };
 
-  // ---- the prefix
-  const int32_t* btb = a.bt + static_cast<int64_t>(b) * a.max_pages;
-  bool pages_ok = true;
-  for (int base = k0; base < k1; base += kTileKeys) {
-    int id[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int p = base / kPage + h;
-      id[h] = base + h * kPage < k1 ? btb[p] : 0;
-      const bool ok = id[h] >= 0 && id[h] < a.num_pages;
-      pages_ok = pages_ok && ok;
-      id[h] = ok ? id[h] : 0;
-    }
-    const int64_t kpage =
-        static_cast<int64_t>(id[(col >> 2) & 1]) * a.Hkv + kvh;
-    const int64_t vpage = static_cast<int64_t>(id[hf]) * a.Hkv + kvh;
-    u32x4_t kr[NJ], vr[NM];
-    const uint8_t* kp = a.k8 + (kpage * kPage + (key & 15)) * D + 16 * hf;
-    const uint8_t* vp = a.v8 + (vpage * D + col) * kPage;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-      kr[j] = *reinterpret_cast<const u32x4_t*>(kp + 32 * j);
-#pragma unroll
-    for (int m = 0; m < NM; ++m)
-      vr[m] = *reinterpret_cast<const u32x4_t*>(vp + 32 * m * kPage);
-    // keys of this lane's page that are in the prefix
-    const int n = min(max(k1 - base - 16 * hf, 0), kPage);
-    // (a page without any may hold any scale)
-    const float ks = n > 0 ? scale_of(a.ke[vpage]) : 1.f;
-    const float vs = n > 0 ? scale_of(a.ve[vpage]) : 1.f;
-    floatx16_t s = {};
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            widen(kr[j][2 * i], kr[j][2 * i + 1], 1.f), qf[2 * j + i], s, 0, 0,
-            0);
-    float x[16];
-    const float f = a.scale_log2 * ks;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = e < n ? s[e] * f : kNegInf;
-    // codes behind the prefix count as zero
-    uint32_t mask[4];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const int k = min(max(n - 4 * w, 0), 4);
-      mask[w] = k == 4 ? ~0u : (1u << (8 * k)) - 1;
-    }
-    bf16x8_t vf[2][NM];
-#pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-      for (int m = 0; m < NM; ++m)
-        vf[h2][m] = widen(vr[m][2 * h2] & mask[2 * h2],
-                          vr[m][2 * h2 + 1] & mask[2 * h2 + 1], vs);
-    finish(x, vf, false);
-  }
-
-  // ---- the window, with the last split
-  if (last) {
+  // ---- the window, with the last split (its tiles dealt to the key waves):
+  // under the first loads
+  if (last && rb < rows) {
     const int64_t wrow = static_cast<int64_t>(b) * a.W;
-    for (int base = 0; base < a.W; base += kTileKeys) {
+    for (int base = kw * kTileKeys; base < a.W; base += KW * kTileKeys) {
       const int kk = base + key;
       const uint16_t* kp = a.kw + ((wrow + min(kk, a.W - 1)) * a.Hkv + kvh) * D;
       floatx16_t s = {};
@@ -294,12 +348,10 @@ void window_attn8_kernel(Args a) {
                                  *reinterpret_cast<const u16x8_t*>(
                                      kp + 32 * j + 16 * hf + 8 * i)),
               qf[2 * j + i], s, 0, 0, 0);
-      float x[16];
       const int at = base + 16 * hf;
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        x[e] = at + e <= qi ? s[e] * a.scale_log2 : kNegInf;
-      bf16x8_t vf[2][NM];
+      for (int e = 0; e < 16; ++e) s[e] = at + e <= qi ? s[e] : kNegInf;
+      bf16x8_t vf[2][NM], pf[2];
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
@@ -314,12 +366,121 @@ void window_attn8_kernel(Args a) {
           }
           vf[h2][m] = __builtin_bit_cast(bf16x8_t, v);
         }
-      finish(x, vf, false);
+      raise(col_max(s) * a.scale_log2);
+      l_run = weigh(s, a.scale_log2, pf);
+      product(vf, pf);
     }
   }
 
-  if (!pages_ok && a.status && lane == 0)
-    atomicOr(a.status + b, WEDLM_SEQ_BAD_PAGE);
+  // ---- the prefix
+  // offsets in a tile: page (col >> 2) & 1 of its two, row key & 15
+  const int kpg = (col >> 2) & 1, krow = key & 15;
+  const int k_lane = kpg * L::kPageBytes + krow * D;
+  const int k_swz = L::swz(krow, kpg);
+  const int v_lane = L::kHalf + hf * L::kPageBytes + col * kPage;
+  for (int t = 0; t < steps; ++t) {
+    // this wave's loads of step t are done, and with the barrier everyone's;
+    // nobody reads the slot of step t - 1 any more
+    wait_vmcnt<kLoads * (kSlots - 2)>();
+    __syncthreads();
+    load_step(t + kSlots - 1);
+    const char* step = ring + (t & (kSlots - 1)) * L::kStep;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      if (KW == 2 && g != kw) continue;
+      const int base = k0 + t * 64 + g * kTileKeys;
+      if (base >= k1) continue;
+      const char* tile = step + g * 2 * L::kPageBytes;
+      u32x4_t kr[NJ], vr[NM];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        kr[j] = *reinterpret_cast<const u32x4_t*>(
+            tile + k_lane + (((2 * j + hf) ^ k_swz) << 4));
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+        vr[m] = *reinterpret_cast<const u32x4_t*>(tile + v_lane +
+                                                  m * 32 * kPage);
+      const int e2 = ex[t * kStepPages + g * 2 + hf];
+      float ks = scale_of(e2 & 0xff), vs = scale_of(e2 >> 8);
+      floatx16_t s = {};
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              widen(kr[j][2 * i], kr[j][2 * i + 1], 1.f), qf[2 * j + i], s, 0,
+              0, 0);
+      bf16x8_t vf[2][NM], pf[2];
+      if (base + kTileKeys <= k1) {
+        const float f = a.scale_log2 * ks;
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+          for (int m = 0; m < NM; ++m)
+            vf[h2][m] = widen(vr[m][2 * h2], vr[m][2 * h2 + 1], vs);
+        if (ballot(m2 == kNegInf)) raise(col_max(s * f));
+        float sum = weigh(s, f, pf);
+        if (ballot(sum > kSumLimit)) {
+          raise(col_max(s * f));
+          sum = weigh(s, f, pf);
+        }
+        l_run = sum;
+      } else {
+        // the prefix ends inside: keys of this lane's page that are in it.
+        // Codes behind count as zero, and a page without any has any scale
+        const int n = min(max(k1 - base - 16 * hf, 0), kPage);
+        ks = n > 0 ? ks : 1.f;
+        vs = n > 0 ? vs : 1.f;
+        const float f = a.scale_log2 * ks;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = e < n ? s[e] * f : kNegInf;
+        uint32_t mask[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int k = min(max(n - 4 * w, 0), 4);
+          mask[w] = k == 4 ? ~0u : (1u << (8 * k)) - 1;
+        }
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+          for (int m = 0; m < NM; ++m)
+            vf[h2][m] = widen(vr[m][2 * h2] & mask[2 * h2],
+                              vr[m][2 * h2 + 1] & mask[2 * h2 + 1], vs);
+        raise(col_max(s));
+        l_run = weigh(s, 1.f, pf);
+      }
+      product(vf, pf);
+    }
+  }
+  wait_vmcnt<0>();        // surplus loads have landed before LDS is used again
+
+  // ---- the key waves' parts joined, in the first one
+  if constexpr (KW == 2) {
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(ring);      // [NM * 16 + 2][64]
+    if (kw == 1) {
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) part[(m * 16 + e) * kWave + lane] = o[m][e];
+      part[NM * 16 * kWave + lane] = m2;
+      part[(NM * 16 + 1) * kWave + lane] = l_run;
+    }
+    __syncthreads();
+    if (kw == 1) return;
+    const float mo = part[NM * 16 * kWave + lane];
+    const float m_new = fmaxf(m2, mo);
+    const float base = m_new == kNegInf ? 0.f : m_new;
+    rescale(__builtin_amdgcn_exp2f(m2 - base));
+    const float w = __builtin_amdgcn_exp2f(mo - base);
+    l_run += w * part[(NM * 16 + 1) * kWave + lane];
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        o[m][e] += w * part[(m * 16 + e) * kWave + lane];
+    m2 = m_new;
+  }
 
   float l0, l1;
   xor32_pair(l_run, l0, l1);
@@ -394,6 +555,21 @@ __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
   if (a.lse && d == 0) a.lse[orow] = (M + __log2f(L)) * kLn2;
 }
 
+template <int D>
+int launch(const Args& a, const Plan& p, int64_t grid, hipStream_t st) {
+  const dim3 g(static_cast<unsigned>(grid)), n(p.nw * kWave);
+  if (p.kw == 2)
+    hipLaunchKernelGGL((window_attn8_kernel<D, 2, 2>), g, n, 0, st, a);
+  else if (p.nw == 2)
+    hipLaunchKernelGGL((window_attn8_kernel<D, 2, 1>), g, n, 0, st, a);
+  else if (p.nw == 4)
+    hipLaunchKernelGGL((window_attn8_kernel<D, 4, 1>), g, n, 0, st, a);
+  else
+    hipLaunchKernelGGL((window_attn8_kernel<D, 8, 1>), g, n, 0, st, a);
+  WEDLM_LAUNCH_CHECK();
+  return WEDLM_OK;
+}
+
 bool shape_ok(int B, int W, int Hq, int Hkv, int D, int max_prefix) {
   if (!(B >= 1 && W >= 1 && W <= WEDLM_MAX_WINDOW && Hkv >= 1 && Hq >= Hkv &&
         Hq % Hkv == 0 && (D == 64 || D == 128) && max_prefix >= 0))
@@ -457,15 +633,9 @@ extern "C" int wedlm_window_attn_cache8(
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int64_t grid = static_cast<int64_t>(p.nsplit) * B * Hkv * p.qgroups;
-  if (D == 128)
-    hipLaunchKernelGGL(window_attn8_kernel<128>,
-                       dim3(static_cast<unsigned>(grid)), dim3(p.nw * kWave),
-                       0, st, a);
-  else
-    hipLaunchKernelGGL(window_attn8_kernel<64>,
-                       dim3(static_cast<unsigned>(grid)), dim3(p.nw * kWave),
-                       0, st, a);
-  WEDLM_LAUNCH_CHECK();
+  const int e = D == 128 ? launch<128>(a, p, grid, st)
+                         : launch<64>(a, p, grid, st);
+  if (e != WEDLM_OK) return e;
   if (p.nsplit > 1) {
     const int64_t threads = static_cast<int64_t>(B) * W * Hq * (D / 8);
     const dim3 mg(static_cast<unsigned>((threads + kMergeThreads - 1) /
