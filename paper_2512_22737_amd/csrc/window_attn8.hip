@@ -4,8 +4,8 @@
 // Work: a workgroup takes (sequence, kv head, query group, prefix split).
 // Query rows of one kv head are packed as in the bf16 kernel (row r = i*G + j
 // is window row i, query head kvh*G + j); a wave owns 32 of them.  Up to 32
-// rows two waves share them and take every other 32-key tile; more rows go to
-// up to eight waves that all read every tile.  S^T = K Q^T and O^T += V^T P^T
+// rows four waves share them and take every fourth 32-key tile, up to 64 two
+// do; more rows go to up to eight waves that all read every tile.  S^T = K Q^T and O^T += V^T P^T
 // run on v_mfma_f32_32x32x16_bf16: e4m3 values are exact in bf16, so the codes
 // are converted on the way into the products and nothing else is rounded than
 // over a bf16 cache.
@@ -15,9 +15,10 @@
 // half hf with the 16 keys of page hf: its K scale is then one factor per
 // lane, folded into the softmax's, and its 16 weights meet the 16 bytes of a
 // V^T row of that page, whose scale the conversion applies.
-// Loads.  64 keys (four pages) are a step: 16 KB with D = 128, straight from
-// HBM into a ring of four steps in LDS, three ahead; one barrier a step.  The
-// split's page ids and exponents are staged in LDS first.
+// Loads go straight from HBM into LDS.  Waves that share keys: 64 keys (four
+// pages) are a step, 16 KB with D = 128, in a ring of four steps, three ahead;
+// one barrier a step.  Waves with keys of their own: a ring of two tiles each,
+// no barrier.  The split's page ids and exponents are staged in LDS first.
 // Softmax: log2 domain, no maximum per tile (the reference maximum is the
 // first tile's and is raised when a sum passes 2^64), split of the prefix and
 // merge as for bf16 pages.
@@ -33,8 +34,10 @@ constexpr int kTileKeys = 32;       // keys per tile (two 16-token pages)
 // ids are staged in LDS).
 constexpr int kMinSplitTiles = 8;
 constexpr int kMaxSplitPages = 2048;
-// Workgroups that a launch aims at.
-constexpr int kWorkgroups = 1024;
+constexpr int kMaxSplitTiles = kMaxSplitPages / 2;
+// A launch has this many times the workgroups that its splits should come to:
+// a sequence can have that many times its share of them.
+constexpr int kSpare = 4;
 constexpr int kStepPages = 4;       // pages of a step
 constexpr int kSlots = 4;           // steps in the ring, kSlots - 1 ahead
 // A column's running sum may reach this before its reference max is raised
@@ -59,30 +62,33 @@ struct Args {
   float2* ws_ml;          // [B, Hkv, rows_pad, nsplit]
   int num_pages, B, W, Hq, Hkv, G, max_pages, max_prefix, nsplit, qgroups,
       rows_pad;
+  int want;               // workgroups that the splits should come to
   float scale_log2;       // softmax_scale * log2(e)
 };
 
 struct Plan {
   int nw, kw;             // waves, of which kw share the rows and split the keys
-  int qgroups, rows_pad, nsplit;
+  int qgroups, rows_pad, nsplit, want;
   size_t ws_bytes;
 };
 
 Plan make_plan(int B, int W, int Hq, int Hkv, int D, int max_prefix) {
   Plan p{};
   const int rows = W * (Hq / Hkv);
-  p.kw = rows <= 32 ? 2 : 1;
-  p.nw = rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+  p.kw = rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
+  p.nw = rows <= 128 ? 4 : 8;
   const int per = 32 * p.nw / p.kw;
   p.qgroups = (rows + per - 1) / per;
   p.rows_pad = p.qgroups * per;
+  // two workgroups of four waves are on a CU, or one of eight
+  p.want = p.nw == 4 ? 512 : 256;
   const int tiles = (max_prefix + kTileKeys - 1) / kTileKeys;
   const int64_t base = static_cast<int64_t>(B) * Hkv * p.qgroups;
-  const int64_t want = kWorkgroups;
-  int64_t n = (want + base - 1) / base;
+  // room for a long prefix among short ones
+  int64_t n = (kSpare * p.want + base - 1) / base;
   const int most = tiles / kMinSplitTiles;
   if (n > most) n = most;
-  const int least = (tiles + kMaxSplitPages / 2 - 1) / (kMaxSplitPages / 2);
+  const int least = (tiles + kMaxSplitTiles - 1) / kMaxSplitTiles;
   if (n < least) n = least;
   if (n < 1) n = 1;
   p.nsplit = static_cast<int>(n);
@@ -99,22 +105,36 @@ __device__ __forceinline__ bool len_ok(const Args& a, int c) {
          static_cast<int64_t>(c) <= static_cast<int64_t>(a.max_pages) * kPage;
 }
 
-// Split of one sequence's prefix of c positions over the launch's nsplit
-// slots: as many splits as keep kMinSplitTiles tiles each (one for an empty
-// prefix), each of the same whole number of tiles.  From the sequence's own c,
-// so that a max_prefix_len far above it leaves no split empty.
-struct SeqSplit {
-  int n, len;             // splits in use, positions per split
-};
+// Tiles of a split: such that the splits of all sequences come to `want`
+// workgroups, within the limits and the launch's nsplit a sequence.  From the
+// sequences' own lengths, so neither a max_prefix_len far above them nor
+// uneven ones leave CUs idle.  Every lane takes part and gets it.
+__device__ __forceinline__ int split_tiles(const Args& a) {
+  if (a.nsplit == 1) return 1 << 30;
+  int most = 0;
+  int64_t total = 0;
+  for (int i = lane_id(); i < a.B; i += kWave) {
+    const int c = a.plen[i];
+    const int t = len_ok(a, c) ? (c + kTileKeys - 1) / kTileKeys : 0;
+    most = max(most, t);
+    total += t;
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    most = max(most, __shfl_xor(most, off));
+    total += __shfl_xor(static_cast<long long>(total), off);
+  }
+  const int64_t share =
+      (total * a.Hkv * a.qgroups + a.want - 1) / a.want;
+  const int64_t per = max(max(share, static_cast<int64_t>(kMinSplitTiles)),
+                          static_cast<int64_t>((most + a.nsplit - 1) / a.nsplit));
+  return static_cast<int>(min(per, static_cast<int64_t>(kMaxSplitTiles)));
+}
 
-__device__ __forceinline__ SeqSplit seq_split(int c, int nsplit) {
+// Splits in use by a prefix of c positions (one if it is empty).
+__device__ __forceinline__ int splits_of(int c, int per) {
   const int tiles = c / kTileKeys + (c % kTileKeys != 0 ? 1 : 0);
-  const int n = max(1, min(tiles / kMinSplitTiles, nsplit));
-  const int per = max(1, (tiles + n - 1) / n);
-  SeqSplit r;
-  r.len = per * kTileKeys;
-  r.n = c > 0 ? (tiles + per - 1) / per : 1;
-  return r;
+  return max(1, (tiles + per - 1) / per);
 }
 
 // Values of x in this lane and in the lane 32 away.
@@ -159,7 +179,7 @@ struct Lds {
 
 template <int D, int NW, int KW>
 __global__ __launch_bounds__(NW * kWave)
-__attribute__((amdgpu_waves_per_eu(NW == 2 ? 1 : 2)))
+__attribute__((amdgpu_waves_per_eu(2)))
 void window_attn8_kernel(Args a) {
   using L = Lds<D>;
   constexpr int NJ = D / 32;          // 16-byte pieces of a key row per half
@@ -167,19 +187,25 @@ void window_attn8_kernel(Args a) {
   constexpr int NM = D / 32;          // 32-row blocks of O^T
   constexpr int NQ = NW / KW;         // query blocks of a workgroup
   constexpr int NT = NW * kWave;
-  constexpr int kLoads = L::kStep / 1024 / NW;   // of a wave per step
+  constexpr bool kOwn = KW == NW;     // waves with keys (and a ring) of their own
+  constexpr int kTile = L::kStep / 2;
+  // loads of a wave per step, or per tile of its own
+  constexpr int kLoads = kOwn ? kTile / 1024 : L::kStep / 1024 / NW;
   static_assert(L::kStep % (1024 * NW) == 0, "whole loads");
+  static_assert(!kOwn || NW * 2 * kTile == kSlots * L::kStep, "the same LDS");
   __shared__ __attribute__((aligned(1024))) char ring[kSlots * L::kStep];
   __shared__ int32_t pg[kMaxSplitPages + kStepPages];
   __shared__ uint16_t ex[kMaxSplitPages + kStepPages];
 
+  // the first splits of all sequences, then the second ones, ...: those that
+  // are not in use come last
   int wg = blockIdx.x;
-  const int split = wg % a.nsplit;
-  wg /= a.nsplit;
   const int qg = wg % a.qgroups;
   wg /= a.qgroups;
   const int kvh = wg % a.Hkv;
-  const int b = wg / a.Hkv;
+  wg /= a.Hkv;
+  const int b = wg % a.B;
+  const int split = wg / a.B;
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = lane_id();
@@ -210,11 +236,12 @@ void window_attn8_kernel(Args a) {
       atomicOr(a.status + b, WEDLM_SEQ_BAD_LEN);
     return;
   }
-  const SeqSplit ss = seq_split(c, a.nsplit);
-  if (split >= ss.n) return;
-  const int k0 = split * ss.len;
-  const int k1 = min(c, k0 + ss.len);
-  const bool last = split == ss.n - 1;
+  const int per = split_tiles(a);
+  const int nsplit = splits_of(c, per);
+  if (split >= nsplit) return;
+  const int k0 = nsplit == 1 ? 0 : split * per * kTileKeys;
+  const int k1 = split == nsplit - 1 ? c : k0 + per * kTileKeys;
+  const bool last = split == nsplit - 1;
   const int pages = (k1 - k0 + kPage - 1) / kPage;
   const int steps = (pages + kStepPages - 1) / kStepPages;
 
@@ -235,38 +262,50 @@ void window_attn8_kernel(Args a) {
 #pragma unroll
   for (int kk = 0; kk < NK; ++kk) asm volatile("" : "+v"(qf[kk]));
 
-  // ---- loads of a step: piece u of this wave is kilobyte wave * kLoads + u of
-  // the step's K, then of its V^T.  Lane l's 16 bytes land at byte 16 l of it,
-  // so K's swizzle is in the lane's address.
+  // ---- loads.  Kilobyte kb of a step is one of its K, then of its V^T; lane
+  // l's 16 bytes land at byte 16 l of it, so K's swizzle is in the lane's
+  // address.  A tile of a wave's own is laid out alike, with half the pages.
   constexpr int kPerPage = L::kPageBytes / 1024;          // kilobytes
+  constexpr int kHalfKb = (kOwn ? kTile : L::kStep) / 2048;
   const uint32_t lds0 =
       static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void_t*)ring));
-  auto load_step = [&](int t) {
-    const int slot = t & (kSlots - 1);
-    t = min(t, steps - 1);            // (as many loads in every step)
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const int kb = wave * kLoads + u;
-      const bool isv = kb >= L::kHalf / 1024;
-      const int p = kb % (L::kHalf / 1024) / kPerPage;    // page of the step
-      const int at = kb % kPerPage * 64 + lane;           // chunk of the page
-      int off = at * 16;
-      if (!isv) {
-        const int row = at / (D / 16), s = at % (D / 16);
-        off = row * D + ((s ^ L::swz(row, p & 1)) << 4);
-      }
-      const int id = __builtin_amdgcn_readfirstlane(pg[t * kStepPages + p]);
-      const uint8_t* base =
-          (isv ? a.v8 : a.k8) +
-          (static_cast<int64_t>(id) * a.Hkv + kvh) * L::kPageBytes;
-      load_to_lds16(buffer_rsrc(base, L::kPageBytes), off,
-                    __builtin_amdgcn_readfirstlane(
-                        lds0 + slot * L::kStep + kb * 1024));
+  auto load_kb = [&](int first_page, int kb, uint32_t dst) {
+    const bool isv = kb >= kHalfKb;
+    const int p = kb % kHalfKb / kPerPage;                // page of the step
+    const int at = kb % kPerPage * 64 + lane;             // chunk of the page
+    int off = at * 16;
+    if (!isv) {
+      const int row = at / (D / 16), s = at % (D / 16);
+      off = row * D + ((s ^ L::swz(row, p & 1)) << 4);
     }
+    const int id = __builtin_amdgcn_readfirstlane(pg[first_page + p]);
+    const uint8_t* base = (isv ? a.v8 : a.k8) +
+                          (static_cast<int64_t>(id) * a.Hkv + kvh) *
+                              L::kPageBytes;
+    load_to_lds16(buffer_rsrc(base, L::kPageBytes), off,
+                  __builtin_amdgcn_readfirstlane(dst + kb * 1024));
+  };
+  // (indices past the end load the last pages again: as many loads each time)
+  auto load_step = [&](int t) {
+    const uint32_t dst = lds0 + (t & (kSlots - 1)) * L::kStep;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+      load_kb(min(t, steps - 1) * kStepPages, wave * kLoads + u, dst);
+  };
+  const int tiles = (pages + 1) / 2;
+  auto load_own = [&](int i) {
+    const uint32_t dst = lds0 + (wave * 2 + (i & 1)) * kTile;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+      load_kb(min(i * KW + kw, tiles - 1) * 2, u, dst);
   };
   if (steps > 0) {
+    if constexpr (kOwn) {
+      load_own(0);
+    } else {
 #pragma unroll
-    for (int t = 0; t < kSlots - 1; ++t) load_step(t);
+      for (int t = 0; t < kSlots - 1; ++t) load_step(t);
+    }
     // the exponents, under the first loads
     for (int i = threadIdx.x; i < steps * kStepPages; i += NT) {
       const int64_t at = static_cast<int64_t>(pg[i]) * a.Hkv + kvh;
@@ -377,30 +416,19 @@ void window_attn8_kernel(Args a) {
   const int kpg = (col >> 2) & 1, krow = key & 15;
   const int k_lane = kpg * L::kPageBytes + krow * D;
   const int k_swz = L::swz(krow, kpg);
-  const int v_lane = L::kHalf + hf * L::kPageBytes + col * kPage;
-  for (int t = 0; t < steps; ++t) {
-    // this wave's loads of step t are done, and with the barrier everyone's;
-    // nobody reads the slot of step t - 1 any more
-    wait_vmcnt<kLoads * (kSlots - 2)>();
-    __syncthreads();
-    load_step(t + kSlots - 1);
-    const char* step = ring + (t & (kSlots - 1)) * L::kStep;
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      if (KW == 2 && g != kw) continue;
-      const int base = k0 + t * 64 + g * kTileKeys;
-      if (base >= k1) continue;
-      const char* tile = step + g * 2 * L::kPageBytes;
+  const int v_lane = hf * L::kPageBytes + col * kPage;
+  // one tile: its K and V^T pages in LDS, its number in the split
+  auto tile_of = [&](const char* kt, const char* vt, int n32) {
+      const int base = k0 + n32 * kTileKeys;
       u32x4_t kr[NJ], vr[NM];
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
         kr[j] = *reinterpret_cast<const u32x4_t*>(
-            tile + k_lane + (((2 * j + hf) ^ k_swz) << 4));
+            kt + k_lane + (((2 * j + hf) ^ k_swz) << 4));
 #pragma unroll
       for (int m = 0; m < NM; ++m)
-        vr[m] = *reinterpret_cast<const u32x4_t*>(tile + v_lane +
-                                                  m * 32 * kPage);
-      const int e2 = ex[t * kStepPages + g * 2 + hf];
+        vr[m] = *reinterpret_cast<const u32x4_t*>(vt + v_lane + m * 32 * kPage);
+      const int e2 = ex[n32 * 2 + hf];
       float ks = scale_of(e2 & 0xff), vs = scale_of(e2 >> 8);
       floatx16_t s = {};
 #pragma unroll
@@ -450,36 +478,70 @@ void window_attn8_kernel(Args a) {
         l_run = weigh(s, 1.f, pf);
       }
       product(vf, pf);
+  };
+  if constexpr (kOwn) {
+    __syncthreads();      // the exponents are there
+    for (int i = 0; i * KW + kw < tiles; ++i) {
+      // every read of the other slot has returned; its next tile is loaded, and
+      // the loads before that have arrived
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      load_own(i + 1);
+      wait_vmcnt<kLoads>();
+      asm volatile("" ::: "memory");
+      const char* at = ring + (wave * 2 + (i & 1)) * kTile;
+      tile_of(at, at + kTile / 2, i * KW + kw);
+    }
+  } else {
+    for (int t = 0; t < steps; ++t) {
+      // this wave's loads of step t are done, and with the barrier everyone's;
+      // nobody reads the slot of step t - 1 any more
+      wait_vmcnt<kLoads * (kSlots - 2)>();
+      __syncthreads();
+      load_step(t + kSlots - 1);
+      const char* at = ring + (t & (kSlots - 1)) * L::kStep;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        if (KW == 2 && g != kw) continue;
+        if (2 * t + g < tiles)
+          tile_of(at + g * 2 * L::kPageBytes,
+                  at + L::kHalf + g * 2 * L::kPageBytes, 2 * t + g);
+      }
     }
   }
   wait_vmcnt<0>();        // surplus loads have landed before LDS is used again
 
-  // ---- the key waves' parts joined, in the first one
-  if constexpr (KW == 2) {
+  // ---- the key waves' parts joined, in the first ones
+  if constexpr (KW > 1) {
+    constexpr int kPart = (NM * 16 + 2) * kWave;
+    static_assert((KW - 1) * NQ * kPart * 4 <= kSlots * L::kStep, "parts in LDS");
     __syncthreads();
-    float* part = reinterpret_cast<float*>(ring);      // [NM * 16 + 2][64]
-    if (kw == 1) {
+    float* part = reinterpret_cast<float*>(ring) + lane;
+    if (kw > 0) {
+      part += ((kw - 1) * NQ + wave % NQ) * kPart;
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) part[(m * 16 + e) * kWave + lane] = o[m][e];
-      part[NM * 16 * kWave + lane] = m2;
-      part[(NM * 16 + 1) * kWave + lane] = l_run;
+        for (int e = 0; e < 16; ++e) part[(m * 16 + e) * kWave] = o[m][e];
+      part[NM * 16 * kWave] = m2;
+      part[(NM * 16 + 1) * kWave] = l_run;
     }
     __syncthreads();
-    if (kw == 1) return;
-    const float mo = part[NM * 16 * kWave + lane];
-    const float m_new = fmaxf(m2, mo);
-    const float base = m_new == kNegInf ? 0.f : m_new;
-    rescale(__builtin_amdgcn_exp2f(m2 - base));
-    const float w = __builtin_amdgcn_exp2f(mo - base);
-    l_run += w * part[(NM * 16 + 1) * kWave + lane];
+    if (kw > 0) return;
+    part += wave % NQ * kPart;
+#pragma unroll 1
+    for (int w = 1; w < KW; ++w, part += NQ * kPart) {
+      const float mo = part[NM * 16 * kWave];
+      const float m_new = fmaxf(m2, mo);
+      const float base = m_new == kNegInf ? 0.f : m_new;
+      rescale(__builtin_amdgcn_exp2f(m2 - base));
+      const float f = __builtin_amdgcn_exp2f(mo - base);
+      l_run += f * part[(NM * 16 + 1) * kWave];
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+      for (int m = 0; m < NM; ++m)
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        o[m][e] += w * part[(m * 16 + e) * kWave + lane];
-    m2 = m_new;
+        for (int e = 0; e < 16; ++e) o[m][e] += f * part[(m * 16 + e) * kWave];
+      m2 = m_new;
+    }
   }
 
   float l0, l1;
@@ -491,7 +553,7 @@ void window_attn8_kernel(Args a) {
       ((static_cast<int64_t>(b) * a.Hkv + kvh) * a.rows_pad + r) * a.nsplit +
       split;
   const int64_t orow = (static_cast<int64_t>(b) * a.W + qi) * a.Hq + qh;
-  uint16_t* op = a.nsplit == 1 ? a.out + orow * D : a.ws_o + part * D;
+  uint16_t* op = nsplit == 1 ? a.out + orow * D : a.ws_o + part * D;
 #pragma unroll
   for (int m = 0; m < NM; ++m)
 #pragma unroll
@@ -503,14 +565,14 @@ void window_attn8_kernel(Args a) {
       *reinterpret_cast<u16x4_t*>(op + m * 32 + g * 8 + hf * 4) = v;
     }
   if (hf == 0) {
-    if (a.nsplit > 1)
+    if (nsplit > 1)
       a.ws_ml[part] = make_float2(m2, l_tot);
     else if (a.lse)
       a.lse[orow] = (m2 + __log2f(l_tot)) * kLn2;
   }
 }
 
-// Merge of the splits' outputs: O = sum_s 2^(m_s - M) l_s O_s / sum_s
+// Merge of the outputs of sequences with several splits: O = sum_s 2^(m_s - M) l_s O_s / sum_s
 // 2^(m_s - M) l_s, O_s normalised by l_s.  D/8 threads a row, 16 bytes of a
 // split each; a row's threads take its splits in order.
 constexpr int kMergeThreads = 256;
@@ -519,6 +581,7 @@ template <int D>
 __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
   constexpr int TPR = D / 8;
   const int rows = a.W * a.G;
+  const int per = split_tiles(a);
   const int64_t gr = (static_cast<int64_t>(blockIdx.x) * kMergeThreads +
                       threadIdx.x) / TPR;
   if (gr >= static_cast<int64_t>(a.B) * a.Hkv * rows) return;
@@ -528,7 +591,8 @@ __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
   const int d = (threadIdx.x % TPR) * 8;
   const int c = a.plen[b];
   if (!len_ok(a, c)) return;
-  const int n = seq_split(c, a.nsplit).n;
+  const int n = splits_of(c, per);
+  if (n == 1) return;                 // written already
   const int64_t part = (bk * a.rows_pad + r) * a.nsplit;
   const float2* ml = a.ws_ml + part;
   const uint16_t* op = a.ws_o + part * D + d;
@@ -558,10 +622,10 @@ __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
 template <int D>
 int launch(const Args& a, const Plan& p, int64_t grid, hipStream_t st) {
   const dim3 g(static_cast<unsigned>(grid)), n(p.nw * kWave);
-  if (p.kw == 2)
-    hipLaunchKernelGGL((window_attn8_kernel<D, 2, 2>), g, n, 0, st, a);
-  else if (p.nw == 2)
-    hipLaunchKernelGGL((window_attn8_kernel<D, 2, 1>), g, n, 0, st, a);
+  if (p.kw == 4)
+    hipLaunchKernelGGL((window_attn8_kernel<D, 4, 4>), g, n, 0, st, a);
+  else if (p.kw == 2)
+    hipLaunchKernelGGL((window_attn8_kernel<D, 4, 2>), g, n, 0, st, a);
   else if (p.nw == 4)
     hipLaunchKernelGGL((window_attn8_kernel<D, 4, 1>), g, n, 0, st, a);
   else
@@ -623,6 +687,7 @@ extern "C" int wedlm_window_attn_cache8(
   a.B = B; a.W = W; a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv;
   a.max_pages = max_pages; a.max_prefix = max_prefix_len;
   a.nsplit = p.nsplit; a.qgroups = p.qgroups; a.rows_pad = p.rows_pad;
+  a.want = p.want;
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   if (p.nsplit > 1) {
     const size_t n = static_cast<size_t>(B) * Hkv * p.rows_pad * p.nsplit;
