@@ -285,12 +285,16 @@ void window_attn8_kernel(Args a) {
     load_to_lds16(buffer_rsrc(base, L::kPageBytes), off,
                   __builtin_amdgcn_readfirstlane(dst + kb * 1024));
   };
+  // the step of the split that is taken as the t-th one
+  auto step_of = [&](int t) {
+    return KW > 1 ? t : t == 0 ? steps - 1 : t - 1;
+  };
   // (indices past the end load the last pages again: as many loads each time)
   auto load_step = [&](int t) {
     const uint32_t dst = lds0 + (t & (kSlots - 1)) * L::kStep;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u)
-      load_kb(min(t, steps - 1) * kStepPages, wave * kLoads + u, dst);
+      load_kb(step_of(min(t, steps - 1)) * kStepPages, wave * kLoads + u, dst);
   };
   const int tiles = (pages + 1) / 2;
   auto load_own = [&](int i) {
@@ -417,38 +421,87 @@ void window_attn8_kernel(Args a) {
   const int k_lane = kpg * L::kPageBytes + krow * D;
   const int k_swz = L::swz(krow, kpg);
   const int v_lane = hf * L::kPageBytes + col * kPage;
+  auto read_k = [&](const char* kt, u32x4_t (&kr)[NJ]) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+      kr[j] = *reinterpret_cast<const u32x4_t*>(
+          kt + k_lane + (((2 * j + hf) ^ k_swz) << 4));
+  };
+  auto read_v = [&](const char* vt, u32x4_t (&vr)[NM]) {
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+      vr[m] = *reinterpret_cast<const u32x4_t*>(vt + v_lane + m * 32 * kPage);
+  };
+  auto scores = [&](const u32x4_t (&kr)[NJ]) {
+    floatx16_t s = {};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            widen(kr[j][2 * i], kr[j][2 * i + 1], 1.f), qf[2 * j + i], s, 0, 0,
+            0);
+    return s;
+  };
+  auto add_values = [&](const u32x4_t (&vr)[NM], float vs,
+                        const bf16x8_t (&pf)[2]) {
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+        o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            widen(vr[m][2 * h2], vr[m][2 * h2 + 1], vs), pf[h2], o[m], 0, 0, 0);
+  };
+  // A whole tile whose K is in registers already (kr, exponents e), with the
+  // next one's K read meanwhile.  One block of code, but for the rare raise:
+  // under each score MFMA the conversions of the next one's keys and of an
+  // eighth of the values.
+  auto whole_tile = [&](const char* vt, u32x4_t (&kr)[NJ], int& e,
+                        const char* next_kt, int next_n32) {
+    u32x4_t vr[NM], kn[NJ];
+    read_v(vt, vr);
+    read_k(next_kt, kn);
+    const int en = ex[next_n32 * 2 + hf];
+    const float f = a.scale_log2 * scale_of(e & 0xff), vs = scale_of(e >> 8);
+    const floatx16_t s = scores(kr);
+    bf16x8_t vf[2][NM], pf[2];
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+        vf[h2][m] = widen(vr[m][2 * h2], vr[m][2 * h2 + 1], vs);
+    __builtin_amdgcn_sched_group_barrier(0x100, NM + NJ + 1, 0);  // LDS reads
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);          // VALU
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // MFMA
+    }
+    float sum = weigh(s, f, pf);
+    if (ballot(!(sum <= kSumLimit))) {
+      raise(col_max(s * f));
+      sum = weigh(s, f, pf);
+    }
+    l_run = sum;
+    product(vf, pf);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) kr[j] = kn[j];
+    e = en;
+  };
   // one tile: its K and V^T pages in LDS, its number in the split
   auto tile_of = [&](const char* kt, const char* vt, int n32) {
       const int base = k0 + n32 * kTileKeys;
       u32x4_t kr[NJ], vr[NM];
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        kr[j] = *reinterpret_cast<const u32x4_t*>(
-            kt + k_lane + (((2 * j + hf) ^ k_swz) << 4));
-#pragma unroll
-      for (int m = 0; m < NM; ++m)
-        vr[m] = *reinterpret_cast<const u32x4_t*>(vt + v_lane + m * 32 * kPage);
+      read_k(kt, kr);
+      read_v(vt, vr);
       const int e2 = ex[n32 * 2 + hf];
       float ks = scale_of(e2 & 0xff), vs = scale_of(e2 >> 8);
-      floatx16_t s = {};
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              widen(kr[j][2 * i], kr[j][2 * i + 1], 1.f), qf[2 * j + i], s, 0,
-              0, 0);
-      bf16x8_t vf[2][NM], pf[2];
+      floatx16_t s = scores(kr);
+      bf16x8_t pf[2];
       if (base + kTileKeys <= k1) {
         const float f = a.scale_log2 * ks;
-#pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-          for (int m = 0; m < NM; ++m)
-            vf[h2][m] = widen(vr[m][2 * h2], vr[m][2 * h2 + 1], vs);
         if (ballot(m2 == kNegInf)) raise(col_max(s * f));
         float sum = weigh(s, f, pf);
-        if (ballot(sum > kSumLimit)) {
+        if (ballot(!(sum <= kSumLimit))) {
           raise(col_max(s * f));
           sum = weigh(s, f, pf);
         }
@@ -469,15 +522,13 @@ void window_attn8_kernel(Args a) {
           mask[w] = k == 4 ? ~0u : (1u << (8 * k)) - 1;
         }
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2)
+        for (int m = 0; m < NM; ++m)
 #pragma unroll
-          for (int m = 0; m < NM; ++m)
-            vf[h2][m] = widen(vr[m][2 * h2] & mask[2 * h2],
-                              vr[m][2 * h2 + 1] & mask[2 * h2 + 1], vs);
+          for (int w = 0; w < 4; ++w) vr[m][w] &= mask[w];
         raise(col_max(s));
         l_run = weigh(s, 1.f, pf);
       }
-      product(vf, pf);
+      add_values(vr, vs, pf);
   };
   if constexpr (kOwn) {
     __syncthreads();      // the exponents are there
@@ -492,20 +543,42 @@ void window_attn8_kernel(Args a) {
       tile_of(at, at + kTile / 2, i * KW + kw);
     }
   } else {
-    for (int t = 0; t < steps; ++t) {
-      // this wave's loads of step t are done, and with the barrier everyone's;
-      // nobody reads the slot of step t - 1 any more
-      wait_vmcnt<kLoads * (kSlots - 2)>();
+    // this wave's loads of step t (and the next, where K is read ahead) are
+    // done, and with the barrier everyone's; nobody reads the slot of step
+    // t - 1 any more
+    auto begin = [&](int t) {
+      wait_vmcnt<kLoads * (kSlots - (KW == 1 ? 3 : 2))>();
       __syncthreads();
       load_step(t + kSlots - 1);
-      const char* at = ring + (t & (kSlots - 1)) * L::kStep;
+      return ring + (t & (kSlots - 1)) * L::kStep;
+    };
+    auto by_tile = [&](const char* at, int n32) {
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         if (KW == 2 && g != kw) continue;
-        if (2 * t + g < tiles)
+        if (n32 + g < tiles)
           tile_of(at + g * 2 * L::kPageBytes,
-                  at + L::kHalf + g * 2 * L::kPageBytes, 2 * t + g);
+                  at + L::kHalf + g * 2 * L::kPageBytes, n32 + g);
       }
+    };
+    if constexpr (KW == 1) {
+      // the last step first, tile by tile: it may end inside, and gives the
+      // reference maxima; all others are whole
+      if (steps > 0) by_tile(begin(0), 2 * (steps - 1));
+      u32x4_t kr[NJ];
+      int e = 0;
+      if (steps > 1) {
+        read_k(ring + L::kStep, kr);
+        e = ex[hf];
+      }
+      for (int t = 1; t < steps; ++t) {
+        const char* at = begin(t);
+        const char* next = ring + ((t + 1) & (kSlots - 1)) * L::kStep;
+        whole_tile(at + L::kHalf, kr, e, at + 2 * L::kPageBytes, 2 * t - 1);
+        whole_tile(at + L::kHalf + 2 * L::kPageBytes, kr, e, next, 2 * t);
+      }
+    } else {
+      for (int t = 0; t < steps; ++t) by_tile(begin(t), 2 * t);
     }
   }
   wait_vmcnt<0>();        // surplus loads have landed before LDS is used again
