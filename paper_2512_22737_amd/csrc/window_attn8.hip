@@ -156,6 +156,18 @@ __device__ __forceinline__ bf16x8_t widen(uint32_t lo, uint32_t hi,
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// 16 bytes per lane from a raw buffer straight into LDS (lane l's at lds_addr +
+// 16 l).  A vector memory instruction must not read a scalar register within
+// five wait states of a vector instruction that wrote it (as readfirstlane
+// does), nor M0 within one of its write; the compiler does not see the load
+// in this text, so the states are part of it.
+__device__ __forceinline__ void load_lds16(i32x4_t rsrc, int voff,
+                                           uint32_t lds_addr) {
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen nt lds"
+               :
+               : "v"(voff), "s"(rsrc), "{m0}"(lds_addr));
+}
+
 // 2^(e - 127) of a scale's exponent (1 .. 254).
 __device__ __forceinline__ float scale_of(int e) {
   return __uint_as_float(static_cast<uint32_t>(e) << 23);
@@ -202,7 +214,7 @@ void window_attn8_kernel(Args a) {
   int wg = blockIdx.x;
   const int qg = wg % a.qgroups;
   wg /= a.qgroups;
-  const int kvh = wg % a.Hkv;
+  const int kvh = __builtin_amdgcn_readfirstlane(wg % a.Hkv);
   wg /= a.Hkv;
   const int b = wg % a.B;
   const int split = wg / a.B;
@@ -269,47 +281,58 @@ void window_attn8_kernel(Args a) {
   constexpr int kHalfKb = (kOwn ? kTile : L::kStep) / 2048;
   const uint32_t lds0 =
       static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void_t*)ring));
-  auto load_kb = [&](int first_page, int kb, uint32_t dst) {
+  // page of a step that kilobyte kb is of
+  auto page_of = [](int kb) { return kb % kHalfKb / kPerPage; };
+  auto load_kb = [&](int id, int kb, uint32_t dst) {
     const bool isv = kb >= kHalfKb;
-    const int p = kb % kHalfKb / kPerPage;                // page of the step
     const int at = kb % kPerPage * 64 + lane;             // chunk of the page
     int off = at * 16;
     if (!isv) {
       const int row = at / (D / 16), s = at % (D / 16);
-      off = row * D + ((s ^ L::swz(row, p & 1)) << 4);
+      off = row * D + ((s ^ L::swz(row, page_of(kb) & 1)) << 4);
     }
-    const int id = __builtin_amdgcn_readfirstlane(pg[first_page + p]);
     const uint8_t* base = (isv ? a.v8 : a.k8) +
                           (static_cast<int64_t>(id) * a.Hkv + kvh) *
                               L::kPageBytes;
-    load_to_lds16(buffer_rsrc(base, L::kPageBytes), off,
-                  __builtin_amdgcn_readfirstlane(dst + kb * 1024));
+    load_lds16(buffer_rsrc(base, L::kPageBytes), off,
+               __builtin_amdgcn_readfirstlane(dst + kb * 1024));
   };
   // the step of the split that is taken as the t-th one
   auto step_of = [&](int t) {
     return KW > 1 ? t : t == 0 ? steps - 1 : t - 1;
   };
-  // (indices past the end load the last pages again: as many loads each time)
-  auto load_step = [&](int t) {
-    const uint32_t dst = lds0 + (t & (kSlots - 1)) * L::kStep;
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u)
-      load_kb(step_of(min(t, steps - 1)) * kStepPages, wave * kLoads + u, dst);
-  };
   const int tiles = (pages + 1) / 2;
-  auto load_own = [&](int i) {
-    const uint32_t dst = lds0 + (wave * 2 + (i & 1)) * kTile;
+  // Loads of this wave's part of step t, or of its i-th own tile (indices past
+  // the end load the last pages again: as many loads each time).  Their page
+  // ids are read from LDS one call ahead.
+  int ids[kLoads];
+  auto read_ids = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      if constexpr (kOwn)
+        ids[u] = pg[min(t * KW + kw, tiles - 1) * 2 + page_of(u)];
+      else
+        ids[u] = pg[step_of(min(t, steps - 1)) * kStepPages +
+                    page_of(wave * kLoads + u)];
+    }
+  };
+  auto load = [&](int t) {
+    const uint32_t dst =
+        lds0 + (kOwn ? (wave * 2 + (t & 1)) * kTile
+                     : (t & (kSlots - 1)) * L::kStep);
+    int now[kLoads];
 #pragma unroll
     for (int u = 0; u < kLoads; ++u)
-      load_kb(min(i * KW + kw, tiles - 1) * 2, u, dst);
+      now[u] = __builtin_amdgcn_readfirstlane(ids[u]);
+    read_ids(t + 1);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+      load_kb(now[u], kOwn ? u : wave * kLoads + u, dst);
   };
   if (steps > 0) {
-    if constexpr (kOwn) {
-      load_own(0);
-    } else {
+    read_ids(0);
 #pragma unroll
-      for (int t = 0; t < kSlots - 1; ++t) load_step(t);
-    }
+    for (int t = 0; t < (kOwn ? 1 : kSlots - 1); ++t) load(t);
     // the exponents, under the first loads
     for (int i = threadIdx.x; i < steps * kStepPages; i += NT) {
       const int64_t at = static_cast<int64_t>(pg[i]) * a.Hkv + kvh;
@@ -536,7 +559,7 @@ void window_attn8_kernel(Args a) {
       // every read of the other slot has returned; its next tile is loaded, and
       // the loads before that have arrived
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      load_own(i + 1);
+      load(i + 1);
       wait_vmcnt<kLoads>();
       asm volatile("" ::: "memory");
       const char* at = ring + (wave * 2 + (i & 1)) * kTile;
@@ -549,7 +572,7 @@ void window_attn8_kernel(Args a) {
     auto begin = [&](int t) {
       wait_vmcnt<kLoads * (kSlots - (KW == 1 ? 3 : 2))>();
       __syncthreads();
-      load_step(t + kSlots - 1);
+      load(t + kSlots - 1);
       return ring + (t & (kSlots - 1)) * L::kStep;
     };
     auto by_tile = [&](const char* at, int n32) {
@@ -669,18 +692,35 @@ __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
   const int64_t part = (bk * a.rows_pad + r) * a.nsplit;
   const float2* ml = a.ws_ml + part;
   const uint16_t* op = a.ws_o + part * D + d;
-  float M = kNegInf;
-  for (int s = 0; s < n; ++s) M = fmaxf(M, ml[s].x);
-  const float base = M == kNegInf ? 0.f : M;
-  float L = 0.f, acc[8] = {};
-#pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const float w = __builtin_amdgcn_exp2f(ml[s].x - base) * ml[s].y;
-    const u16x8_t v =
-        *reinterpret_cast<const u16x8_t*>(op + static_cast<int64_t>(s) * D);
-    L += w;
+  // four splits' loads under way at a time
+  constexpr int kAtOnce = 4;
+  float M = kNegInf, L = 0.f, acc[8] = {};
+  for (int s0 = 0; s0 < n; s0 += kAtOnce) {
+    float2 x[kAtOnce];
+    u16x8_t v[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) acc[k] += w * bf16_to_f32(v[k]);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int s = min(s0 + i, n - 1);
+      x[i] = ml[s];
+      v[i] = *reinterpret_cast<const u16x8_t*>(op + static_cast<int64_t>(s) * D);
+    }
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, x[i].x);
+    const float base = top == kNegInf ? 0.f : top;
+    const float old = __builtin_amdgcn_exp2f(M - base);
+    L *= old;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[k] *= old;
+    M = top;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float w =
+          s0 + i < n ? __builtin_amdgcn_exp2f(x[i].x - base) * x[i].y : 0.f;
+      L += w;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc[k] += w * bf16_to_f32(v[i][k]);
+    }
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
   u16x8_t v;
