@@ -1,7 +1,7 @@
 // Rows appended to the 8-bit paged cache: e4m3 codes, one power-of-two scale
 // per page and kv head (wedlm_cache8_append, wedlm_commit_cache8).
 //
-// One wave per (layer, sequence, page, kv head).  Its rows' largest finite
+// One wave per (layer, sequence, kv head) and page, or window.  The rows' largest finite
 // magnitude is an integer maximum over the bf16 patterns without their sign;
 // the exponent is read off that pattern, so the scale is exact and does not
 // depend on any rounding.  x * 2^(127 - e) is exact in fp32 and rounded once,
@@ -33,6 +33,7 @@ struct AppendArgs {
   int64_t num_pages;
   int L, B, T, Hkv, max_pages;
   int spans;              // pages that a sequence's rows can touch
+  int run, runs;          // pages of a wave; waves for them
   uint32_t units;         // waves
   int behind;             // start is the position behind the last row
 };
@@ -96,41 +97,57 @@ __device__ __forceinline__ uint32_t byte_mask(int word, int lo, int hi) {
   return below_b & ~below_a;
 }
 
-template <int D>
-__global__ __launch_bounds__(kWavesPerGroup * kWave) void append8_kernel(
-    AppendArgs a) {
-  constexpr int LPR = D / 8;            // lanes per row, 8 values each
-  constexpr int RPI = kWave / LPR;      // rows per load
-  constexpr int NI = kPage / RPI;       // loads per page
-  // a page's V^T, bytes, per wave.  Rows of 16 bytes: a lane's 8 stores go to
-  // 8 consecutive rows
-  __shared__ __attribute__((aligned(16))) uint8_t vt[kWavesPerGroup][D * kPage];
-  const int wave = threadIdx.x / kWave, lane = lane_id();
-  const uint32_t unit = blockIdx.x * kWavesPerGroup + wave;
-  if (unit >= a.units) return;
-  const int h = unit % a.Hkv;
-  uint32_t w = unit / a.Hkv;
-  const int span = w % a.spans;
-  w /= a.spans;
-  const int l = w % a.L, b = w / a.L;
+// The four words of a 4 x 4 transpose of bytes: byte j of word i is byte i of
+// word j.
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400);
+  const uint32_t b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400);
+  const uint32_t c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);
+  const uint32_t d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+  w[0] = __builtin_amdgcn_perm(b, a, 0x05040100);
+  w[1] = __builtin_amdgcn_perm(b, a, 0x07060302);
+  w[2] = __builtin_amdgcn_perm(d, c, 0x05040100);
+  w[3] = __builtin_amdgcn_perm(d, c, 0x07060302);
+}
 
-  const int n = a.count[b];
-  int64_t s0 = a.start[b];
-  if (a.behind) s0 -= n;
-  const bool tell = a.status && l == 0 && h == 0 && lane == 0;
-  if (n < 0 || n > a.T || s0 < 0) {
-    if (tell && span == 0) atomicOr(a.status + b, WEDLM_SEQ_BAD_LEN);
-    return;
-  }
+// 16-byte row dd of V^T in LDS: its eight neighbours' order is changed from one
+// group of eight to the next, so that lanes that write row k of their groups
+// meet different banks.
+__device__ __forceinline__ int vt_row(int dd) { return dd ^ (dd >> 3 & 7); }
+
+// The page `span` of sequence b's rows, layer l, head h: one wave.
+template <int D>
+__device__ __forceinline__ void append_page(const AppendArgs& a, int l, int b,
+                                            int h, int span, int n, int64_t s0,
+                                            uint8_t* vt) {
+  constexpr int LPR = D / 8;            // lanes per row, 8 values each
+  constexpr int NI = kPage * LPR / kWave;   // rows of a lane: NI r .. NI r+NI-1
+  const int lane = lane_id();
   const int64_t page0 = (s0 / kPage + span) * kPage;     // its first position
   const int r0 = static_cast<int>(max(s0 - page0, static_cast<int64_t>(0)));
   const int r1 = static_cast<int>(
       min(s0 + n - page0, static_cast<int64_t>(kPage)));
   if (r1 <= r0) return;
+  const bool tell = a.status && l == 0 && h == 0 && lane == 0;
   const int64_t entry = page0 / kPage;
   if (entry >= a.max_pages) {
     if (tell) atomicOr(a.status + b, WEDLM_SEQ_CAPACITY);
     return;
+  }
+  // ---- the new rows, under the table's round trip
+  const int row = lane / LPR * NI, d = (lane % LPR) * 8;
+  u16x8_t xk[NI], xv[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const u16x8_t z = {0, 0, 0, 0, 0, 0, 0, 0};
+    xk[i] = xv[i] = z;
+    if (row + i >= r0 && row + i < r1) {
+      const int64_t src =
+          (((static_cast<int64_t>(l) * a.B + b) * a.T + (page0 + row + i - s0)) *
+               a.Hkv + h) * D + d;
+      xk[i] = *reinterpret_cast<const u16x8_t*>(a.k + src);
+      xv[i] = *reinterpret_cast<const u16x8_t*>(a.v + src);
+    }
   }
   const int64_t id = a.bt[static_cast<int64_t>(b) * a.max_pages + entry];
   if (id < 0 || id >= a.num_pages) {
@@ -140,31 +157,27 @@ __global__ __launch_bounds__(kWavesPerGroup * kWave) void append8_kernel(
   const int64_t ph = (l * a.num_pages + id) * a.Hkv + h;
   uint8_t* kp = a.k8 + ph * (kPage * D);
   uint8_t* vp = a.v8 + ph * (kPage * D);
-
-  // ---- the new rows
-  const int row = lane / LPR, d = (lane % LPR) * 8;
-  u16x8_t xk[NI], xv[NI];
+  // what the page holds, where not all 16 rows are new
+  constexpr int NV = D / kWave;
+  u32x4_t old[NV];
+  if (r1 - r0 < kPage) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      old[i] = *reinterpret_cast<const u32x4_t*>(vp + (i * kWave + lane) * kPage);
+  }
+  int ek0 = 0, ev0 = 0;
+  if (r0 > 0) {
+    ek0 = a.ke[ph];
+    ev0 = a.ve[ph];
+  }
   int mk = 0, mv = 0;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    const int r = row + i * RPI;
-    u16x8_t z = {0, 0, 0, 0, 0, 0, 0, 0};
-    xk[i] = xv[i] = z;
-    if (r >= r0 && r < r1) {
-      const int64_t src =
-          (((static_cast<int64_t>(l) * a.B + b) * a.T + (page0 + r - s0)) *
-               a.Hkv + h) * D + d;
-      xk[i] = *reinterpret_cast<const u16x8_t*>(a.k + src);
-      xv[i] = *reinterpret_cast<const u16x8_t*>(a.v + src);
-    }
     mk = mag_max(xk[i], mk);
     mv = mag_max(xv[i], mv);
   }
   int ek = need_exp(wave_max_int(mk)), ev = need_exp(wave_max_int(mv));
-  int ek0 = ek, ev0 = ev;
   if (r0 > 0) {
-    ek0 = a.ke[ph];
-    ev0 = a.ve[ph];
     ek = max(ek, ek0);
     ev = max(ev, ev0);
   }
@@ -176,7 +189,7 @@ __global__ __launch_bounds__(kWavesPerGroup * kWave) void append8_kernel(
   // ---- keys: rows are contiguous
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    const int r = row + i * RPI;
+    const int r = row + i;
     uint2* dst = reinterpret_cast<uint2*>(kp + r * D + d);
     if (r >= r0 && r < r1) {
       *dst = pack8(xk[i], 127 - ek);
@@ -188,39 +201,73 @@ __global__ __launch_bounds__(kWavesPerGroup * kWave) void append8_kernel(
     }
   }
 
-  // ---- values: transposed through LDS, then whole 16-byte rows of the page,
-  // merged with what the page holds where not all 16 rows are new
+  // ---- values: transposed, a lane's rows as one word (or half of one) of each
+  // of its 8 d, through LDS to whole 16-byte rows of the page, merged with what
+  // it holds
+  uint2 c[NI];
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int r = row + i * RPI;
-    const uint2 c = pack8(xv[i], 127 - ev);
+  for (int i = 0; i < NI; ++i) c[i] = pack8(xv[i], 127 - ev);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      vt[wave][(d + k) * kPage + r] =
-          static_cast<uint8_t>((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
+  for (int half = 0; half < 2; ++half) {
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int i = 0; i < NI; ++i) w[i] = half ? c[i].y : c[i].x;
+    transpose4(w);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint8_t* at = vt + vt_row(d + 4 * half + k) * kPage + row;
+      if constexpr (NI == 4) *reinterpret_cast<uint32_t*>(at) = w[k];
+      else *reinterpret_cast<uint16_t*>(at) = static_cast<uint16_t>(w[k]);
+    }
   }
   // the wave's own LDS writes are complete before its reads (in order)
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int i = 0; i < D / kWave; ++i) {
+  for (int i = 0; i < NV; ++i) {
     const int dd = i * kWave + lane;
-    u32x4_t c = *reinterpret_cast<const u32x4_t*>(&vt[wave][dd * kPage]);
-    u32x4_t* dst = reinterpret_cast<u32x4_t*>(vp + dd * kPage);
+    u32x4_t v = *reinterpret_cast<const u32x4_t*>(vt + vt_row(dd) * kPage);
     if (r1 - r0 < kPage) {
-      const u32x4_t old = *dst;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const uint32_t fresh = byte_mask(q, r0, r1);
-        uint32_t o = old[q];
-        if (ev > ev0) {
+        uint32_t o = old[i][q];
+        if (r0 > 0 && ev > ev0) {
           const uint32_t before = byte_mask(q, 0, r0);
           o = (again4(o, ev0 - ev) & before) | (o & ~before);
         }
-        c[q] = (c[q] & fresh) | (o & ~fresh);
+        v[q] = (v[q] & fresh) | (o & ~fresh);
       }
     }
-    *dst = c;
+    *reinterpret_cast<u32x4_t*>(vp + dd * kPage) = v;
   }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// One wave per (sequence, layer, run of pages, kv head), kv heads fastest.
+template <int D>
+__global__ __launch_bounds__(kWavesPerGroup * kWave) void append8_kernel(
+    AppendArgs a) {
+  // a page's V^T, bytes, per wave
+  __shared__ __attribute__((aligned(16))) uint8_t vt[kWavesPerGroup][D * kPage];
+  const int wave = threadIdx.x / kWave;
+  const uint32_t unit = blockIdx.x * kWavesPerGroup + wave;
+  if (unit >= a.units) return;
+  const int h = unit % a.Hkv;
+  uint32_t w = unit / a.Hkv;
+  const int run = w % a.runs;
+  w /= a.runs;
+  const int l = w % a.L, b = w / a.L;
+  const int n = a.count[b];
+  int64_t s0 = a.start[b];
+  if (a.behind) s0 -= n;
+  if (n < 0 || n > a.T || s0 < 0) {
+    if (a.status && l == 0 && h == 0 && run == 0 && lane_id() == 0)
+      atomicOr(a.status + b, WEDLM_SEQ_BAD_LEN);
+    return;
+  }
+  const int end = min((run + 1) * a.run, a.spans);
+  for (int span = run * a.run; span < end; ++span)
+    append_page<D>(a, l, b, h, span, n, s0, vt[wave]);
 }
 
 bool aligned(const void* p, size_t n) {
@@ -247,6 +294,12 @@ int append_shape(int64_t L, int64_t B, int64_t T, int64_t Hkv, int32_t D,
 
 int launch_append(AppendArgs& a, int D, int64_t units, hipStream_t st) {
   a.spans = (a.T + kPage - 1) / kPage + 1;
+  // A window's rows (at most five pages, mostly one that gets a few rows) are
+  // one wave's: fewer waves that find nothing to do.  Longer ones take a wave
+  // a page.
+  a.run = a.T <= WEDLM_MAX_WINDOW ? a.spans : 1;
+  a.runs = (a.spans + a.run - 1) / a.run;
+  units = units / a.spans * a.runs;
   a.units = static_cast<uint32_t>(units);
   const dim3 grid(static_cast<unsigned>((units + kWavesPerGroup - 1) /
                                         kWavesPerGroup));
