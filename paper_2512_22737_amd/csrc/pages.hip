@@ -286,28 +286,23 @@ __device__ __forceinline__ void copy_pages(const CopyArgs& a, int which,
   const int64_t words = bytes >> shift;
   const int lanes = words <= 4 ? 4 : words <= 32 ? 32 : 256;
   const int at = threadIdx.x % lanes, many = 256 / lanes;
-  for (int64_t m = static_cast<int64_t>(first) * many + threadIdx.x / lanes;
-       m < n; m += static_cast<int64_t>(step) * many) {
-    int64_t from, to;
-    if (!pair(static_cast<int>(m), from, to)) continue;
-    const char* s = base + from * bytes;
-    char* d = base + to * bytes;
+  const int64_t by = static_cast<int64_t>(step) * many;
+  int64_t m = static_cast<int64_t>(first) * many + threadIdx.x / lanes;
+  int64_t from = 0, to = 0;
+  bool have = m < n && pair(static_cast<int>(m), from, to);
+  while (m < n) {
+    // the next pair is read under this copy
+    const int64_t s_at = from * bytes, d_at = to * bytes;
+    const bool now = have;
+    m += by;
+    have = m < n && pair(static_cast<int>(m), from, to);
+    if (!now) continue;
+    const char* s = base + s_at;
+    char* d = base + d_at;
     if (shift == 4) copy_words<u32x4_t>(s, d, words, at, lanes);
     else if (shift == 2) copy_words<uint32_t>(s, d, words, at, lanes);
     else copy_words<uint8_t>(s, d, words, at, lanes);
   }
-}
-
-// x: workgroups that share the moves, y: arrays and layers
-__global__ __launch_bounds__(256) void copy_pages_kernel(CopyArgs a,
-                                                         const int32_t* moves,
-                                                         const int32_t* count) {
-  copy_pages(a, blockIdx.y % a.n_arrays, blockIdx.y / a.n_arrays, *count,
-             blockIdx.x, gridDim.x, [&](int m, int64_t& from, int64_t& to) {
-               from = moves[2 * m];
-               to = moves[2 * m + 1];
-               return true;
-             });
 }
 
 // Tables and counts of request i, a workgroup.
@@ -453,11 +448,25 @@ __global__ __launch_bounds__(kThreads) void compact_plan_kernel(CompactArgs a) {
   }
 }
 
-__global__ __launch_bounds__(256) void compact_table_kernel(CompactArgs a) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= a.entries) return;
-  const int id = a.bt[i];
-  a.new_bt[i] = id >= 0 && id < a.num_pages ? a.name[id] : -1;
+// y = 0: the table's new numbers.  y > 0: the moves, shared by the workgroups
+// of one array and layer.
+__global__ __launch_bounds__(256) void compact_apply_kernel(CompactArgs a,
+                                                            CopyArgs c) {
+  if (blockIdx.y > 0) {
+    copy_pages(c, (blockIdx.y - 1) % c.n_arrays, (blockIdx.y - 1) / c.n_arrays,
+               *a.count, blockIdx.x, gridDim.x,
+               [&](int m, int64_t& from, int64_t& to) {
+                 from = a.moves[2 * m];
+                 to = a.moves[2 * m + 1];
+                 return true;
+               });
+    return;
+  }
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+       i < a.entries; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int id = a.bt[i];
+    a.new_bt[i] = id >= 0 && id < a.num_pages ? a.name[id] : -1;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -487,9 +496,12 @@ int check_arrays(const wedlm_page_array* arrays, int32_t n_arrays,
 }
 
 // Workgroups that share `most` copies of one array and layer: about eight a CU
-// in all.
-unsigned sharers(int most, int64_t arrays) {
-  const int64_t x = (2048 + arrays - 1) / (arrays > 0 ? arrays : 1);
+// on the pages of more than a few words, 16 KB under way in each
+unsigned sharers(int64_t most, const CopyArgs& c, int n_layers) {
+  int64_t wide = 0;
+  for (int i = 0; i < c.n_arrays; ++i)
+    wide += (c.array[i].bytes >> c.array[i].shift) > 32 ? n_layers : 0;
+  const int64_t x = wide > 0 ? (2048 + wide - 1) / wide : 256;
   return static_cast<unsigned>(x < most ? x : most);
 }
 
@@ -563,7 +575,7 @@ extern "C" int wedlm_cache_fork(
   WEDLM_LAUNCH_CHECK();
   const int64_t copies = static_cast<int64_t>(n_arrays) * n_layers;
   hipLaunchKernelGGL(fork_assign_kernel,
-                     dim3(sharers(n, copies + 1),
+                     dim3(sharers(n, c, n_layers),
                           static_cast<unsigned>(copies + 1)),
                      dim3(256), 0, st, a, c);
   WEDLM_LAUNCH_CHECK();
@@ -605,18 +617,14 @@ extern "C" int wedlm_cache_compact(
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kThreads), 0, st, a);
   WEDLM_LAUNCH_CHECK();
-  hipLaunchKernelGGL(compact_table_kernel,
-                     dim3(static_cast<unsigned>((entries + 255) / 256)),
-                     dim3(256), 0, st, a);
-  WEDLM_LAUNCH_CHECK();
   c.num_pages = num_pages;
-  const int64_t copies = static_cast<int64_t>(n_arrays) * n_layers;
-  if (copies > 0 && num_pages > 1) {
-    hipLaunchKernelGGL(copy_pages_kernel,
-                       dim3(sharers(static_cast<int>(num_pages / 2), copies),
-                            static_cast<unsigned>(copies)),
-                       dim3(256), 0, st, c, a.moves, a.count);
-    WEDLM_LAUNCH_CHECK();
-  }
+  // (the copies of one page need none, but the table does)
+  const int64_t copies =
+      num_pages > 1 ? static_cast<int64_t>(n_arrays) * n_layers : 0;
+  hipLaunchKernelGGL(compact_apply_kernel,
+                     dim3(sharers(1 << 20, c, n_layers),
+                          static_cast<unsigned>(copies + 1)),
+                     dim3(256), 0, st, a, c);
+  WEDLM_LAUNCH_CHECK();
   return WEDLM_OK;
 }

@@ -60,6 +60,7 @@ struct Args {
   int32_t* status;        // [B] or null
   uint16_t* ws_o;         // [B, Hkv, rows_pad, nsplit, D]
   float2* ws_ml;          // [B, Hkv, rows_pad, nsplit]
+  int32_t* ws_n;          // [B] splits in use (0: a bad length)
   int num_pages, B, W, Hq, Hkv, G, max_pages, max_prefix, nsplit, qgroups,
       rows_pad;
   int want;               // workgroups that the splits should come to
@@ -95,7 +96,7 @@ Plan make_plan(int B, int W, int Hq, int Hkv, int D, int max_prefix) {
   if (p.nsplit > 1) {
     const size_t r = static_cast<size_t>(B) * Hkv * p.rows_pad * p.nsplit;
     p.ws_bytes = ((r * D * sizeof(uint16_t) + 255) & ~static_cast<size_t>(255)) +
-                 r * sizeof(float2);
+                 r * sizeof(float2) + static_cast<size_t>(B) * sizeof(int32_t);
   }
   return p;
 }
@@ -243,13 +244,15 @@ void window_attn8_kernel(Args a) {
           *reinterpret_cast<const u16x8_t*>(qp + 32 * j + 16 * hf + 8 * i));
 
   const int c = a.plen[b];
+  const bool tells = threadIdx.x == 0 && split == 0 && qg == 0 && kvh == 0;
   if (!len_ok(a, c)) {
-    if (a.status && threadIdx.x == 0 && split == 0 && qg == 0 && kvh == 0)
-      atomicOr(a.status + b, WEDLM_SEQ_BAD_LEN);
+    if (tells && a.status) atomicOr(a.status + b, WEDLM_SEQ_BAD_LEN);
+    if (tells && a.nsplit > 1) a.ws_n[b] = 0;
     return;
   }
   const int per = split_tiles(a);
   const int nsplit = splits_of(c, per);
+  if (tells && a.nsplit > 1) a.ws_n[b] = nsplit;
   if (split >= nsplit) return;
   const int k0 = nsplit == 1 ? 0 : split * per * kTileKeys;
   const int k1 = split == nsplit - 1 ? c : k0 + per * kTileKeys;
@@ -677,7 +680,6 @@ template <int D>
 __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
   constexpr int TPR = D / 8;
   const int rows = a.W * a.G;
-  const int per = split_tiles(a);
   const int64_t gr = (static_cast<int64_t>(blockIdx.x) * kMergeThreads +
                       threadIdx.x) / TPR;
   if (gr >= static_cast<int64_t>(a.B) * a.Hkv * rows) return;
@@ -685,10 +687,8 @@ __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
   const int64_t bk = gr / rows;
   const int kvh = static_cast<int>(bk % a.Hkv), b = static_cast<int>(bk / a.Hkv);
   const int d = (threadIdx.x % TPR) * 8;
-  const int c = a.plen[b];
-  if (!len_ok(a, c)) return;
-  const int n = splits_of(c, per);
-  if (n == 1) return;                 // written already
+  const int n = a.ws_n[b];
+  if (n <= 1) return;                 // written already, or not at all
   const int64_t part = (bk * a.rows_pad + r) * a.nsplit;
   const float2* ml = a.ws_ml + part;
   const uint16_t* op = a.ws_o + part * D + d;
@@ -808,6 +808,7 @@ extern "C" int wedlm_window_attn_cache8(
     a.ws_o = reinterpret_cast<uint16_t*>(base);
     a.ws_ml = reinterpret_cast<float2*>(
         base + ((n * D * sizeof(uint16_t) + 255) & ~static_cast<size_t>(255)));
+    a.ws_n = reinterpret_cast<int32_t*>(a.ws_ml + n);
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int64_t grid = static_cast<int64_t>(p.nsplit) * B * Hkv * p.qgroups;
