@@ -46,7 +46,7 @@ struct Args {
   const float* min_p;
   int32_t* token;
   float* logp;
-  int W, V, shift;
+  int B, W, V, shift;
   int seg;                // tokens per segment, whole vectors of a wave
 };
 
@@ -64,6 +64,7 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 constexpr int kNear = 4096;             // tokens near the top
 constexpr int kList = 2048;             // tokens of the bins at the runs' ends
 constexpr int kPairs = 256;             // of them compared all with all
+constexpr int kBlocks = 2 * kList;      // blocks of a row at most
 constexpr int kFine = 256;              // steps of the table of powers
 // log2 units below the top that the histogram covers, at first and at last:
 // 48 units down every weight is zero (shift <= 46)
@@ -103,7 +104,10 @@ struct Lds {
   uint64_t sum[kBins];
   uint32_t count[kBins];
   uint64_t near[kNear];   // key << 32 | ~id: larger is earlier in the order
-  uint64_t list[kList];
+  union {
+    uint64_t list[kList];
+    float blocks[2 * kList];   // largest logit of each (before the list)
+  };
   uint64_t weights[kPairs];
   double powers[kFine];
   uint64_t part[kWaves];
@@ -114,6 +118,20 @@ struct Lds {
 // A logit as it counts: NaN: -inf; +inf: the largest number.
 __device__ __forceinline__ float clean(float x) {
   return fminf(fmaxf(x, kNegInf), 3.402823466e38f);
+}
+
+// Largest of a value over the wave, in lane 63: rows of 16 lanes shifted by 1,
+// 2, 4 and 8, then lane 15 of each row to the next row and lane 31 to the upper
+// half.
+template <int CTRL>
+__device__ __forceinline__ float dpp_top(float v) {
+  const int x = __float_as_int(v);
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(x, x, CTRL, 0xf,
+                                                             0xf, false)));
+}
+__device__ __forceinline__ float wave_top(float v) {
+  v = dpp_top<0x118>(dpp_top<0x114>(dpp_top<0x112>(dpp_top<0x111>(v))));
+  return dpp_top<0x143>(dpp_top<0x142>(v));
 }
 
 // Appends e of the lanes that call it to a list of `most`; false if it is
@@ -261,31 +279,122 @@ struct Logits {
       f(s, k);
     }
   }
-  // the largest logits that this thread meets, by their place in a vector;
-  // four vectors under way
-  __device__ __forceinline__ void largest(float (&m)[VEC]) const {
-    const int tid = threadIdx.x;
+  // Rounds of the workgroup's whole vectors, and the rounds of one block: a
+  // block is a wave's vectors of `fold` rounds in a row, as many blocks as fit.
+  __device__ __forceinline__ int rounds() const {
+    return (V - head) / VEC / kThreads +
+           ((V - head) / VEC % kThreads != 0 ? 1 : 0);
+  }
+  __device__ __forceinline__ int fold() const {
+    return (rounds() * kWaves + kBlocks - 1) / kBlocks;
+  }
+  // The largest logits that this thread meets, by their place in a vector, and
+  // if wanted of each block (blocks[block round * kWaves + wave]); four vectors
+  // under way.  What is not in whole vectors counts in m alone.
+  template <bool BLOCKS>
+  __device__ __forceinline__ void largest(float (&m)[VEC], float* blocks) const {
+    const int tid = threadIdx.x, n = rounds(), f = fold();
 #pragma unroll
     for (int k = 0; k < VEC; ++k) m[k] = kNegInf;
     if (tid < head) m[0] = fmaxf(m[0], one(tid));
     constexpr int kStep = kThreads * VEC;
-    int i = head + tid * VEC;
-    for (; i + 3 * kStep + VEC <= V; i += 4 * kStep) {
+    float top = kNegInf;
+    int left = f, block = tid / kWave;
+    auto round = [&](const float (&v)[VEC], bool whole) {
+      float t = kNegInf;
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        m[k] = fmaxf(m[k], whole ? v[k] : kNegInf);
+        t = fmaxf(t, v[k]);
+      }
+      top = fmaxf(top, whole ? t : kNegInf);
+      if (BLOCKS && --left == 0) {
+        top = wave_top(top);
+        if (lane_id() == kWave - 1) blocks[block] = top;
+        top = kNegInf;
+        left = f;
+        block += kWaves;
+      }
+    };
+    int i = head + tid * VEC, j = 0;
+    for (; j + 4 <= n && i - tid * VEC + 4 * kStep <= V; j += 4, i += 4 * kStep) {
       float v[4][VEC];
 #pragma unroll
       for (int u = 0; u < 4; ++u) many(i + u * kStep, v[u]);
+      if (BLOCKS && f == 1) {
+        // (four reductions side by side)
+        float t[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u) {
+          t[u] = kNegInf;
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) m[k] = fmaxf(m[k], v[u][k]);
+          for (int k = 0; k < VEC; ++k) {
+            m[k] = fmaxf(m[k], v[u][k]);
+            t[u] = fmaxf(t[u], v[u][k]);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) t[u] = wave_top(t[u]);
+        if (lane_id() == kWave - 1)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) blocks[block + u * kWaves] = t[u];
+        block += 4 * kWaves;
+        continue;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) round(v[u], true);
     }
-    for (; i + VEC <= V; i += kStep) {
+    for (; j < n; ++j, i += kStep) {
+      const bool whole = i + VEC <= V;
       float v[VEC];
-      many(i, v);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) m[k] = fmaxf(m[k], v[k]);
+      for (int k = 0; k < VEC; ++k) v[k] = kNegInf;
+      if (whole) many(i, v);
+      round(v, whole);
     }
-    for (int k = i; k < V && k < i + VEC; ++k) m[0] = fmaxf(m[0], one(k));
+    if (BLOCKS && left < f) {
+      top = wave_top(top);
+      if (lane_id() == kWave - 1) blocks[block] = top;
+    }
+    // the last, not whole, vector is the one after all whole ones
+    const int rest = head + (V - head) / VEC * VEC + tid;
+    if (rest < V) m[0] = fmaxf(m[0], one(rest));
+  }
+  // f(logits, first id) of the blocks that want(largest) says, each by the wave
+  // that has it, and of the tokens that are in no whole vector
+  template <typename W, typename F>
+  __device__ __forceinline__ void each_block(const float* blocks, W want,
+                                             F f) const {
+    const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
+    const int n = rounds(), fo = fold();
+    const int mine = (n + fo - 1) / fo;        // block rounds
+    for (int b0 = 0; b0 < mine; b0 += kWave) {
+      uint64_t todo = ballot(b0 + lane < mine &&
+                             want(blocks[(b0 + lane) * kWaves + wave]));
+      while (todo) {
+        const int b = b0 + __ffsll(static_cast<unsigned long long>(todo)) - 1;
+        todo &= todo - 1;
+        for (int j = b * fo; j < min((b + 1) * fo, n); ++j) {
+          const int i = head + (j * kThreads + tid) * VEC;
+          if (i + VEC <= V) {
+            float v[VEC];
+            many(i, v);
+            f(v, i);
+          }
+        }
+      }
+    }
+    const int rest = head + (V - head) / VEC * VEC + tid;
+    if (tid < head || rest < V) {
+      if (tid < head) {
+        const float s[1] = {one(tid)};
+        f(s, tid);
+      }
+      if (rest < V) {
+        const float s[1] = {one(rest)};
+        f(s, rest);
+      }
+    }
   }
 };
 
@@ -386,6 +495,8 @@ template <bool HALF>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
   __shared__ Lds l;
+  // neighbours take rows of different sequences: settings, and so the rows'
+  // times, go by sequence
   const int row = blockIdx.x, b = row / a.W, i = row - b * a.W;
   if (a.n_obs && i < a.n_obs[b]) return;
   Logits<HALF> x;
@@ -403,7 +514,14 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
   // ---- the largest logit
   if (tid < kFine) l.powers[tid] = exp2(tid / static_cast<double>(kFine));
   float some[VEC];        // the largest of kThreads * VEC parts of the row
-  x.largest(some);
+  const float T = a.temp ? a.temp[b] : 1.f;
+  const int k_raw = a.top_k ? a.top_k[b] : 0;
+  // with few k the blocks' maxima too (1280 rows of 151936, k = 50: 189 us with
+  // them, 281 without; other rows' first pass takes up to 7 us longer with them)
+  const int blocks = (x.rounds() + x.fold() - 1) / max(x.fold(), 1) * kWaves;
+  const bool few = T > 0.f && k_raw > 0 && k_raw < V && k_raw <= blocks / 4;
+  if (few) x.template largest<true>(some, l.blocks);
+  else x.template largest<false>(some, l.blocks);
   float fmax_ = some[0];
 #pragma unroll
   for (int k = 1; k < VEC; ++k) fmax_ = fmaxf(fmax_, some[k]);
@@ -422,7 +540,6 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
   for (int w = 0; w < kWaves; ++w)
     fmax_ = fmaxf(fmax_, __uint_as_float(static_cast<uint32_t>(l.part[w])));
   fmax_ = clean(fmax_);
-  const float T = a.temp ? a.temp[b] : 1.f;
   if (!(T > 0.f) || fmax_ == kNegInf) {
     // its first id: among the parts that it is the maximum of, a thread per
     // vector, and the ends; over the whole row if it is that of many
@@ -464,7 +581,6 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
   r.rate = 1.4426950408889634 / static_cast<double>(T);
   r.shift = a.shift;
   r.powers = l.powers;
-  const int k_raw = a.top_k ? a.top_k[b] : 0;
   bool use_k = k_raw > 0 && k_raw < V;
   const float p = a.top_p ? a.top_p[b] : 1.f;
   const bool use_p = p < 1.f;
@@ -542,14 +658,20 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
   bool placed = false;
   if (use_k && k_raw <= kThreads * VEC / 2) {
     // The k-th largest of the parts' maxima is not above the k-th largest
-    // logit, and mostly near it: one pass collects what is above its bin.
+    // logit, and mostly near it: what is above its bin is collected.  With few
+    // k the parts are the blocks, and only those with something are read again.
     rate = static_cast<float>(fmin(r.rate * (kBins / kAllUnits), 1e30));
     clear();
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const float at = place(clean(some[k]));
+    auto mark = [&](float f) {
+      const float at = place(clean(f));
       if (at < static_cast<float>(kBins))
         atomicAdd(&l.count[static_cast<int>(at)], 1u);
+    };
+    if (few) {
+      for (int j = tid; j < blocks; j += kThreads) mark(l.blocks[j]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) mark(some[k]);
     }
     __syncthreads();
     uint64_t before;
@@ -558,7 +680,7 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
     if (f < kBins) {
       const float most = static_cast<float>(f + 1);
       bool room = true;
-      x.template each<4>([&](const auto& g, int v) {
+      auto take = [&](const auto& g, int v) {
         // (one question for a vector: few have any)
         constexpr int N = sizeof(g) / sizeof(float);
         float top = kNegInf;
@@ -569,7 +691,12 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
           if (place(clean(h)) < most && room)
             room = push(l.near, &l.nears, kNear, entry(h, id));
         });
-      });
+      };
+      if (few)
+        x.each_block(l.blocks,
+                     [&](float top) { return place(clean(top)) < most; }, take);
+      else
+        x.template each<4>(take);
       __syncthreads();
       const uint32_t n = l.nears;
       if (n <= kNear) {
@@ -917,7 +1044,7 @@ extern "C" int wedlm_sample(const void* logits, int32_t logits_type,
   Args a{};
   a.x = logits; a.stride = row_stride; a.u = u; a.n_obs = n_obs;
   a.temp = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
-  a.token = token; a.logp = logp; a.W = W; a.V = V;
+  a.token = token; a.logp = logp; a.B = B; a.W = W; a.V = V;
   // V weights of at most 2^shift each stay below 2^63
   int bits = 0;
   while ((1 << bits) < V) ++bits;
