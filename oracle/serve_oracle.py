@@ -117,8 +117,7 @@ def attention(q, kw, vw, kp, vp, scale):
     D] -> out, lse and elementwise bounds of their errors.
 
     With A = sum p |v|: the weights enter the product in bf16 (half a step of
-    A), a split's output and the result are rounded to bf16 (another half step
-    of A each, |out| <= A).  A score is a sum of D products and carries
+    A) and the result is rounded to bf16 (another half step of A, |out| <= A).  A score is a sum of D products and carries
     (D + 2) fp32 roundings of S = sum |q k| scale, which move every weight by
     that much relatively and A by twice it; sums over n keys carry n / 16
     roundings (16 are added as a tree per tile) and the exponentials 4."""
@@ -144,7 +143,7 @@ def attention(q, kw, vw, kp, vp, scale):
         A = p @ np.abs(v)
         ds = (D + 2) * F32 * S + 4 * F32
         sums = ((c + W) / 16 + 16) * F32
-        bo[:, h] = A * (3 * BF16 * (1 + BF16) ** 2 +
+        bo[:, h] = A * (2 * BF16 * (1 + BF16) +
                         (2 * ds + 2 * sums)[:, None] * 1.1)
         bl[:, h] = ds + sums + 4 * F32 * (np.abs(lse[:, h]) + 32)
     return out, lse, bo, bl

@@ -58,7 +58,8 @@ struct Args {
   uint16_t* out;          // [B, W, Hq, D]
   float* lse;             // [B, W, Hq] or null
   int32_t* status;        // [B] or null
-  uint16_t* ws_o;         // [B, Hkv, rows_pad, nsplit, D]
+  float* ws_o;            // [B, Hkv, rows_pad, nsplit, D]: a split's sums of
+                          // p v, not normalised (bf16 would round once more)
   float2* ws_ml;          // [B, Hkv, rows_pad, nsplit]
   int32_t* ws_n;          // [B] splits in use (0: a bad length)
   int num_pages, B, W, Hq, Hkv, G, max_pages, max_prefix, nsplit, qgroups,
@@ -71,6 +72,18 @@ struct Plan {
   int nw, kw;             // waves, of which kw share the rows and split the keys
   int qgroups, rows_pad, nsplit, want;
   size_t ws_bytes;
+};
+
+// Byte offsets of a workspace's parts (see Args): the sums, from 0, the
+// (m, l) pairs, the splits in use.
+struct Layout {
+  size_t ml, n, bytes;
+  Layout(int B, int Hkv, const Plan& p, int D) {
+    const size_t rows = static_cast<size_t>(B) * Hkv * p.rows_pad * p.nsplit;
+    ml = rows * D * sizeof(float);
+    n = ml + rows * sizeof(float2);
+    bytes = n + static_cast<size_t>(B) * sizeof(int32_t);
+  }
 };
 
 Plan make_plan(int B, int W, int Hq, int Hkv, int D, int max_prefix) {
@@ -93,11 +106,7 @@ Plan make_plan(int B, int W, int Hq, int Hkv, int D, int max_prefix) {
   if (n < least) n = least;
   if (n < 1) n = 1;
   p.nsplit = static_cast<int>(n);
-  if (p.nsplit > 1) {
-    const size_t r = static_cast<size_t>(B) * Hkv * p.rows_pad * p.nsplit;
-    p.ws_bytes = ((r * D * sizeof(uint16_t) + 255) & ~static_cast<size_t>(255)) +
-                 r * sizeof(float2) + static_cast<size_t>(B) * sizeof(int32_t);
-  }
+  if (p.nsplit > 1) p.ws_bytes = Layout(B, Hkv, p, D).bytes;
   return p;
 }
 
@@ -652,17 +661,30 @@ void window_attn8_kernel(Args a) {
       ((static_cast<int64_t>(b) * a.Hkv + kvh) * a.rows_pad + r) * a.nsplit +
       split;
   const int64_t orow = (static_cast<int64_t>(b) * a.W + qi) * a.Hq + qh;
-  uint16_t* op = nsplit == 1 ? a.out + orow * D : a.ws_o + part * D;
+  // (both branches store 4 consecutive d of an accumulator's quarter)
+  if (nsplit == 1) {
+    uint16_t* op = a.out + orow * D;
 #pragma unroll
-  for (int m = 0; m < NM; ++m)
+    for (int m = 0; m < NM; ++m)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const u16x4_t v = {to_bf16(o[m][4 * g] * inv),
-                         to_bf16(o[m][4 * g + 1] * inv),
-                         to_bf16(o[m][4 * g + 2] * inv),
-                         to_bf16(o[m][4 * g + 3] * inv)};
-      *reinterpret_cast<u16x4_t*>(op + m * 32 + g * 8 + hf * 4) = v;
-    }
+      for (int g = 0; g < 4; ++g) {
+        const u16x4_t v = {to_bf16(o[m][4 * g] * inv),
+                           to_bf16(o[m][4 * g + 1] * inv),
+                           to_bf16(o[m][4 * g + 2] * inv),
+                           to_bf16(o[m][4 * g + 3] * inv)};
+        *reinterpret_cast<u16x4_t*>(op + m * 32 + g * 8 + hf * 4) = v;
+      }
+  } else {
+    float* op = a.ws_o + part * D;
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx4_t v = {o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2],
+                             o[m][4 * g + 3]};
+        *reinterpret_cast<floatx4_t*>(op + m * 32 + g * 8 + hf * 4) = v;
+      }
+  }
   if (hf == 0) {
     if (nsplit > 1)
       a.ws_ml[part] = make_float2(m2, l_tot);
@@ -671,9 +693,9 @@ void window_attn8_kernel(Args a) {
   }
 }
 
-// Merge of the outputs of sequences with several splits: O = sum_s 2^(m_s - M) l_s O_s / sum_s
-// 2^(m_s - M) l_s, O_s normalised by l_s.  D/8 threads a row, 16 bytes of a
-// split each; a row's threads take its splits in order.
+// Merge of the outputs of sequences with several splits: O = sum_s 2^(m_s - M)
+// O_s / sum_s 2^(m_s - M) l_s, in fp32, the splits in order.  D/8 threads a
+// row, 32 bytes of a split each.
 constexpr int kMergeThreads = 256;
 
 template <int D>
@@ -691,18 +713,21 @@ __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
   if (n <= 1) return;                 // written already, or not at all
   const int64_t part = (bk * a.rows_pad + r) * a.nsplit;
   const float2* ml = a.ws_ml + part;
-  const uint16_t* op = a.ws_o + part * D + d;
+  const float* op = a.ws_o + part * D + d;
   // four splits' loads under way at a time
   constexpr int kAtOnce = 4;
   float M = kNegInf, L = 0.f, acc[8] = {};
   for (int s0 = 0; s0 < n; s0 += kAtOnce) {
     float2 x[kAtOnce];
-    u16x8_t v[kAtOnce];
+    floatx4_t v[kAtOnce][2];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const int s = min(s0 + i, n - 1);
       x[i] = ml[s];
-      v[i] = *reinterpret_cast<const u16x8_t*>(op + static_cast<int64_t>(s) * D);
+      const floatx4_t* at =
+          reinterpret_cast<const floatx4_t*>(op + static_cast<int64_t>(s) * D);
+      v[i][0] = at[0];
+      v[i][1] = at[1];
     }
     float top = M;
 #pragma unroll
@@ -716,10 +741,10 @@ __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const float w =
-          s0 + i < n ? __builtin_amdgcn_exp2f(x[i].x - base) * x[i].y : 0.f;
-      L += w;
+          s0 + i < n ? __builtin_amdgcn_exp2f(x[i].x - base) : 0.f;
+      L += w * x[i].y;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] += w * bf16_to_f32(v[i][k]);
+      for (int k = 0; k < 8; ++k) acc[k] += w * v[i][k / 4][k % 4];
     }
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -803,12 +828,11 @@ extern "C" int wedlm_window_attn_cache8(
   a.want = p.want;
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   if (p.nsplit > 1) {
-    const size_t n = static_cast<size_t>(B) * Hkv * p.rows_pad * p.nsplit;
+    const Layout at(B, Hkv, p, D);
     char* base = static_cast<char*>(workspace);
-    a.ws_o = reinterpret_cast<uint16_t*>(base);
-    a.ws_ml = reinterpret_cast<float2*>(
-        base + ((n * D * sizeof(uint16_t) + 255) & ~static_cast<size_t>(255)));
-    a.ws_n = reinterpret_cast<int32_t*>(a.ws_ml + n);
+    a.ws_o = reinterpret_cast<float*>(base);
+    a.ws_ml = reinterpret_cast<float2*>(base + at.ml);
+    a.ws_n = reinterpret_cast<int32_t*>(base + at.n);
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int64_t grid = static_cast<int64_t>(p.nsplit) * B * Hkv * p.qgroups;

@@ -41,8 +41,12 @@ def test_attention_refusals():
     lib = _lib()
     size = lib.wedlm_window_attn_cache8_workspace_size
     assert size(1, 16, 4, 2, 64, 100) == 0              # one split
+    # 2 kv heads of 32 rows, 16 splits of at least 256 keys: fp32 sums of 64
+    # values and two floats each, and how many splits there are
     need = size(1, 16, 4, 2, 64, 4096)
-    assert need > 0
+    assert need == 2 * 32 * 16 * (64 + 2) * 4 + 4
+    # 3 sequences, 8 heads, 128 rows, 16 splits at most
+    assert size(3, 32, 32, 8, 128, 4096) == 3 * 8 * 128 * 16 * 130 * 4 + 12
     for bad in ((0, 16, 4, 2, 64, 9), (1, 65, 4, 2, 64, 9),
                 (1, 16, 5, 2, 64, 9), (1, 16, 4, 2, 96, 9),
                 (1, 16, 4, 2, 64, -1), (1 << 30, 64, 4, 2, 64, 9)):
