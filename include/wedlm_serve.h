@@ -80,9 +80,11 @@ size_t wedlm_window_attn_cache8_workspace_size(int32_t B, int32_t W,
  * window's own keys and values stay bf16.  Arguments, outputs, limits and
  * errors are those of wedlm_window_attn with k8, v8, k_exp, v_exp in the
  * place of k_cache, v_cache; D = 64 or 128, W = 1 (single tokens) to 64.
- * Codes behind a sequence's prefix are not used, whatever they hold.  bf16
- * arrays, k8 and v8 on 16-byte boundaries, the workspace on a 256-byte one
- * (WEDLM_E_ARG).
+ * Codes behind a sequence's prefix are not used, whatever they hold.  The
+ * splits' sums are merged in fp32; their number goes by the batch's own prefix
+ * lengths, and nothing depends on the run.  bf16 arrays, k8 and v8 on 16-byte
+ * boundaries, the workspace on a 256-byte one (WEDLM_E_ARG); a max_prefix_len
+ * whose splits pass one launch is refused (WEDLM_E_SHAPE).
  */
 int wedlm_window_attn_cache8(
     const uint16_t* q_phys, const uint16_t* k_phys, const uint16_t* v_phys,
@@ -220,9 +222,6 @@ int wedlm_cache_compact(const int32_t* block_table, int32_t B,
 #define WEDLM_SAMPLE_F32 0
 #define WEDLM_SAMPLE_BF16 1
 
-/* Bytes of workspace wedlm_sample needs (0: none, or an unsupported shape). */
-size_t wedlm_sample_workspace_size(int32_t B, int32_t W, int32_t V);
-
 /*
  * wedlm_sample -- one token per masked row from given random numbers, in the
  * place of wedlm_score's greedy token (a decoder without windows calls it
@@ -253,18 +252,14 @@ size_t wedlm_sample_workspace_size(int32_t B, int32_t W, int32_t V);
  *   min_p [B] fp32, or NULL: <= 0 or NaN: no limit; above 1 as 1
  * Out: token [B, W] int32, logp [B, W] fp32 or NULL; entries of observed rows
  *   are left untouched.
- * B, W >= 1, B * W < 2^22, 1 <= V <= 2^22 (WEDLM_E_SHAPE).  Rows on 16-byte
- * boundaries are read faster.
- * workspace: wedlm_sample_workspace_size() bytes on a 16-byte boundary
- * (WEDLM_E_ARG; NULL when that is 0); its contents on entry do not matter.
- * Two calls that overlap in time must not share a workspace.
+ * B, W >= 1, B * W < 2^22, 1 <= V <= 2^22 (WEDLM_E_SHAPE).  Rows may start
+ * anywhere (row_stride of any size); no workspace is needed.
  */
 int wedlm_sample(const void* logits, int32_t logits_type, int64_t row_stride,
                  const float* u, const int32_t* n_obs,
                  const float* temperature, const int32_t* top_k,
                  const float* top_p, const float* min_p, int32_t B, int32_t W,
-                 int32_t V, int32_t* token, float* logp, void* workspace,
-                 size_t workspace_bytes, void* stream);
+                 int32_t V, int32_t* token, float* logp, void* stream);
 
 #ifdef __cplusplus
 }

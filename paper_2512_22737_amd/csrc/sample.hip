@@ -1019,21 +1019,13 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
 
 }  // namespace
 
-extern "C" size_t wedlm_sample_workspace_size(int32_t B, int32_t W,
-                                              int32_t V) {
-  (void)B; (void)W; (void)V;
-  return 0;
-}
-
 extern "C" int wedlm_sample(const void* logits, int32_t logits_type,
                             int64_t row_stride, const float* u,
                             const int32_t* n_obs, const float* temperature,
                             const int32_t* top_k, const float* top_p,
                             const float* min_p, int32_t B, int32_t W,
                             int32_t V, int32_t* token, float* logp,
-                            void* workspace, size_t workspace_bytes,
                             void* stream) {
-  (void)workspace; (void)workspace_bytes;
   if (!logits || !u || !token) return WEDLM_E_ARG;
   if (logits_type != WEDLM_SAMPLE_F32 && logits_type != WEDLM_SAMPLE_BF16)
     return WEDLM_E_ARG;

@@ -68,6 +68,11 @@ struct Args {
   float scale_log2;       // softmax_scale * log2(e)
 };
 
+// Tiles of a prefix (up to 2^31 - 1 positions).
+__host__ __device__ __forceinline__ int tiles_of(int c) {
+  return c / kTileKeys + (c % kTileKeys != 0 ? 1 : 0);
+}
+
 struct Plan {
   int nw, kw;             // waves, of which kw share the rows and split the keys
   int qgroups, rows_pad, nsplit, want;
@@ -96,7 +101,7 @@ Plan make_plan(int B, int W, int Hq, int Hkv, int D, int max_prefix) {
   p.rows_pad = p.qgroups * per;
   // two workgroups of four waves are on a CU, or one of eight
   p.want = p.nw == 4 ? 512 : 256;
-  const int tiles = (max_prefix + kTileKeys - 1) / kTileKeys;
+  const int tiles = tiles_of(max_prefix);
   const int64_t base = static_cast<int64_t>(B) * Hkv * p.qgroups;
   // room for a long prefix among short ones
   int64_t n = (kSpare * p.want + base - 1) / base;
@@ -125,7 +130,7 @@ __device__ __forceinline__ int split_tiles(const Args& a) {
   int64_t total = 0;
   for (int i = lane_id(); i < a.B; i += kWave) {
     const int c = a.plen[i];
-    const int t = len_ok(a, c) ? (c + kTileKeys - 1) / kTileKeys : 0;
+    const int t = len_ok(a, c) ? tiles_of(c) : 0;
     most = max(most, t);
     total += t;
   }
@@ -143,8 +148,7 @@ __device__ __forceinline__ int split_tiles(const Args& a) {
 
 // Splits in use by a prefix of c positions (one if it is empty).
 __device__ __forceinline__ int splits_of(int c, int per) {
-  const int tiles = c / kTileKeys + (c % kTileKeys != 0 ? 1 : 0);
-  return max(1, (tiles + per - 1) / per);
+  return max(1, (tiles_of(c) + per - 1) / per);
 }
 
 // Values of x in this lane and in the lane 32 away.
@@ -778,7 +782,11 @@ bool shape_ok(int B, int W, int Hq, int Hkv, int D, int max_prefix) {
     return false;
   // rows, padded to whole workgroups, and their workgroups fit 31 bits
   const int64_t rows = static_cast<int64_t>(W) * (Hq / Hkv) + 255;
-  return rows < (1ll << 31) / Hkv && rows * Hkv < (1ll << 31) / B;
+  if (rows >= (1ll << 31) / Hkv || rows * Hkv >= (1ll << 31) / B) return false;
+  // and so do the launch's threads 32
+  const Plan p = make_plan(B, W, Hq, Hkv, D, max_prefix);
+  return static_cast<int64_t>(p.nsplit) * B * Hkv * p.qgroups <
+         (1ll << 32) / (p.nw * kWave);
 }
 
 bool aligned(const void* p, size_t n) {

@@ -146,10 +146,7 @@ def _load():
     lib.wedlm_cache_compact.argtypes = [P, I32, I32, P, I64, P, I32, I32, P,
                                         P, P, P, SZ, P]
     lib.wedlm_cache_compact.restype = ctypes.c_int
-    lib.wedlm_sample_workspace_size.argtypes = [I32] * 3
-    lib.wedlm_sample_workspace_size.restype = SZ
-    lib.wedlm_sample.argtypes = [P, I32, I64] + [P] * 6 + [I32] * 3 + [
-        P, P, P, SZ, P]
+    lib.wedlm_sample.argtypes = [P, I32, I64] + [P] * 6 + [I32] * 3 + [P] * 3
     lib.wedlm_sample.restype = ctypes.c_int
     lib.wedlm_strerror.argtypes = [ctypes.c_int]
     lib.wedlm_strerror.restype = ctypes.c_char_p
@@ -184,8 +181,7 @@ EXPORTED = ["wedlm_reorder", "wedlm_window_attn_workspace_size",
             "wedlm_window_attn_cache8", "wedlm_commit_cache8",
             "wedlm_cache_free", "wedlm_cache_fork_workspace_size",
             "wedlm_cache_fork", "wedlm_cache_compact_workspace_size",
-            "wedlm_cache_compact", "wedlm_sample_workspace_size",
-            "wedlm_sample"]
+            "wedlm_cache_compact", "wedlm_sample"]
 
 # decoding rules of wedlm_commit_rule (include/wedlm.h)
 RULE_STREAMING, RULE_BLOCK, RULE_ONE_TOKEN = 0, 1, 2
@@ -1199,25 +1195,18 @@ def wedlm_cache_compact(block_table, ref, arrays, new_table, new_ref, n_used,
 SAMPLE_F32, SAMPLE_BF16 = 0, 1
 
 
-def wedlm_sample_workspace_size(B, W, V) -> int:
-    return _size("wedlm_sample_workspace_size", B, W, V)
-
-
 def wedlm_sample(logits, u, token, temperature=None, top_k=None, top_p=None,
-                 min_p=None, n_obs=None, logp=None, workspace=None,
+                 min_p=None, n_obs=None, logp=None,
                  V: Optional[int] = None) -> None:
     """logits [B, W, row_stride] fp32 or bf16, u [B, W] fp32 in [0, 1) ->
     token [B, W] int32 and logp [B, W] fp32 (optional) of rows i >= n_obs[b]
     (all without n_obs).  temperature, top_p, min_p [B] fp32 and top_k [B]
-    int32 are optional.  V defaults to the last dimension.  A workspace is
-    allocated here if one is needed and none is given."""
+    int32 are optional.  V defaults to the last dimension."""
     B, W, stride = logits.shape
     V = stride if V is None else V
     _sizes("wedlm_sample", B, W, V)
     half = logits.dtype == torch.bfloat16
     types = (torch.bfloat16,) if half else _F32
-    held, ws, nbytes = _workspace(workspace, logits.device,
-                                  wedlm_sample_workspace_size, B, W, V)
     code = _load().wedlm_sample(
         _t(logits, "logits", types), SAMPLE_BF16 if half else SAMPLE_F32,
         stride, _t(u, "u", _F32, (B, W)),
@@ -1227,6 +1216,5 @@ def wedlm_sample(logits, u, token, temperature=None, top_k=None, top_p=None,
         _t(top_p, "top_p", _F32, (B,), allow_none=True),
         _t(min_p, "min_p", _F32, (B,), allow_none=True), B, W, V,
         _t(token, "token", _I32, (B, W)),
-        _t(logp, "logp", _F32, (B, W), allow_none=True), ws, nbytes,
-        _stream())
+        _t(logp, "logp", _F32, (B, W), allow_none=True), _stream())
     _check(code, "wedlm_sample")

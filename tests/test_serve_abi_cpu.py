@@ -45,11 +45,14 @@ def test_attention_refusals():
     # values and two floats each, and how many splits there are
     need = size(1, 16, 4, 2, 64, 4096)
     assert need == 2 * 32 * 16 * (64 + 2) * 4 + 4
+    # the longest prefix of one sequence: splits of 32768 keys
+    assert size(1, 1, 1, 1, 64, 2**31 - 1) == 65536 * 32 * (64 + 2) * 4 + 4
     # 3 sequences, 8 heads, 128 rows, 16 splits at most
     assert size(3, 32, 32, 8, 128, 4096) == 3 * 8 * 128 * 16 * 130 * 4 + 12
     for bad in ((0, 16, 4, 2, 64, 9), (1, 65, 4, 2, 64, 9),
                 (1, 16, 5, 2, 64, 9), (1, 16, 4, 2, 96, 9),
-                (1, 16, 4, 2, 64, -1), (1 << 30, 64, 4, 2, 64, 9)):
+                (1, 16, 4, 2, 64, -1), (1 << 30, 64, 4, 2, 64, 9),
+                (64, 64, 32, 8, 128, 2**31 - 1)):
         assert size(*bad) == 0, bad
     args = [F] * 7 + [300, F, 256, F, 1, 16, 4, 2, 64, 4096, 0.125, F, None,
                       None, F, need, None]
@@ -122,12 +125,8 @@ def test_compact_refusals():
 
 
 def test_sample_refusals():
-    lib = _lib()
-    size = lib.wedlm_sample_workspace_size
-    assert size(0, 1, 10) == size(1, 1, 0) == size(1, 1, (1 << 22) + 1) == 0
-    args = [F, 0, 64, F, None, None, None, None, None, 2, 3, 64, F, None, F,
-            1 << 30, None]
-    refusals(lib.wedlm_sample, args,
+    args = [F, 0, 64, F, None, None, None, None, None, 2, 3, 64, F, None, None]
+    refusals(_lib().wedlm_sample, args,
              [(i, None, -1) for i in (0, 3, 12)] +
              [(1, 2, -1), (1, -1, -1), (2, 63, -2), (9, 0, -2), (10, 0, -2),
               (11, 0, -2), (11, (1 << 22) + 1, -2), (9, 1 << 22, -2)])
@@ -138,7 +137,6 @@ def test_binding_refusals():
     tensor is refused; here the sizes are)."""
     import torch
     from paper_2512_22737_amd import wedlm
-    assert wedlm.wedlm_sample_workspace_size(1 << 33, 1, 10) == 0
     assert wedlm.wedlm_cache_compact_workspace_size(1 << 33) == 0
     x = torch.zeros(2, 3)
     with pytest.raises(wedlm.WedlmError, match="arrays"):
