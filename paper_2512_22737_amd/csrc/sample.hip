@@ -23,6 +23,11 @@
 // with all if they are few, else by a radix search over the keys (over the row
 // itself where they are too many for LDS, as in a flat row).  Last, one wave
 // walks the segment that the draw falls into.
+// Bounds, 1280 rows of 151936 fp32 logits: greedy 136 us (HBM, 5.7 TB/s), k = 50
+// 194, k = 1000 328 (the second pass), no limit 377 (fp64 weights: 15 fp64
+// operations and an LDS read a token), top-p alone 0.68 ms (the histogram's
+// 64-bit LDS additions beside that).  One row: 8 to 165 us, its workgroup's
+// own time; rows are not split over workgroups.
 #include "common.h"
 #include "wedlm_serve.h"
 
@@ -30,6 +35,8 @@ using namespace wedlm;
 
 namespace {
 
+// (1024 threads: 762 us in place of 669 for 1280 rows with top-p alone, and 125
+// in place of 155 for one row)
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;

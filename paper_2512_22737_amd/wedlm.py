@@ -1116,15 +1116,15 @@ def _page_arrays(arrays, P):
     if not arrays:
         return None, 0, 1
     L = arrays[0].shape[0]
-    made = (PageArray * len(arrays))()
+    pairs = []                    # the fields of PageArray, one after another
     for i, x in enumerate(arrays):
         if not x.is_cuda or not x.is_contiguous():
             raise WedlmError(f"arrays[{i}] must be a contiguous device tensor")
-        if x.dim() < 2 or x.shape[:2] != (L, P):
+        if x.dim() < 2 or x.shape[0] != L or x.shape[1] != P:
             raise WedlmError(f"arrays[{i}]: shape {tuple(x.shape)} is not "
                              f"[{L}, {P}, ...]")
-        made[i] = PageArray(x.data_ptr(), x.nbytes // (L * P) if L * P else 0)
-    return made, len(arrays), L
+        pairs += (x.data_ptr(), x.nbytes // (L * P) if L * P else 0)
+    return (ctypes.c_int64 * len(pairs))(*pairs), len(arrays), L
 
 
 def wedlm_cache_free(rows, block_table, ref, prefix_len=None) -> None:
