@@ -5,7 +5,7 @@
 // falling order, so it is described by a key (the order-preserving pattern of
 // a logit) and a number of ties: tokens above the key, and the first m ids at
 // it.  Weights w = 2^((x - max) log2(e) / T) are fp64 values rounded to whole
-// multiples of 2^-shift (shift >= 41, so that V of them fit 64 bits): sums
+// multiples of 2^-shift (shift >= 40, so that V of them fit 64 bits): sums
 // are exact and the same in any order, which both the histograms' atomics and
 // the comparison of running sums with u * total need.
 // Passes over a row (the first from HBM, the others from the caches):
