@@ -9,7 +9,7 @@
 // pages are aligned.  No result depends on an order of atomics: they only add
 // integers.
 // Bound by latency where little is copied (8 samples of one prompt, 36 layers:
-// free 2.4, plan 6.1, tables and copies 5.3 us); by HBM where much is
+// free 2.3, plan 6.8, tables and copies 5.4 us); by HBM where much is
 // (compaction of 8192 pages, 1.03 GB read and written: 211 us, 4.9 TB/s, and
 // 16 us of plan).
 #include "common.h"
@@ -26,26 +26,28 @@ constexpr int kWaves = kThreads / kWave;
 // sums over a workgroup
 // ---------------------------------------------------------------------------
 
-__device__ __forceinline__ int wave_scan(int v) {      // inclusive
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v) {          // inclusive
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
-    const int u = __shfl_up(v, off);
+    const T u = __shfl_up(v, off);
     if (lane_id() >= off) v += u;
   }
   return v;
 }
 
 // Exclusive sums over the workgroup's threads; `total` to all of them.
-__device__ __forceinline__ int group_scan(int v, int* lds, int& total) {
+template <typename T>
+__device__ __forceinline__ T group_scan(T v, T* lds, T& total) {
   const int wave = threadIdx.x / kWave;
-  const int s = wave_scan(v);
+  const T s = wave_scan(v);
   __syncthreads();                      // lds is free again
   if (lane_id() == kWave - 1) lds[wave] = s;
   __syncthreads();
-  int before = 0, all = 0;
+  T before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    const int t = lds[w];
+    const T t = lds[w];
     before += w < wave ? t : 0;
     all += t;
   }
@@ -184,11 +186,13 @@ __global__ __launch_bounds__(256) void fork_check_kernel(ForkArgs a) {
 
 // First pages of the requests (in order, as far as the free pages reach) and
 // the list of the lowest free pages, one workgroup.  Up to as many requests as
-// it has waves are checked here too, which saves a launch (8 requests: 6.1 us
+// it has waves are checked here too, which saves a launch (8 requests: 6.8 us
 // for both; the check alone takes 4.2 and a gap before the next kernel).
 __global__ __launch_bounds__(kThreads) void fork_plan_kernel(ForkArgs a) {
   __shared__ int lds[kWaves];
+  __shared__ long long sums[kWaves];
   int total;
+  long long wanted;       // a few requests can ask for 2^31 pages together
   if (a.n <= kWaves) {
     const int i = threadIdx.x / kWave;
     if (i < a.n) {
@@ -204,8 +208,8 @@ __global__ __launch_bounds__(kThreads) void fork_plan_kernel(ForkArgs a) {
   int64_t want = 0;
   for (int base = 0; base < a.n; base += kThreads) {
     const int i = base + threadIdx.x;
-    group_scan(i < a.n ? a.first[i] : 0, lds, total);
-    want += total;
+    group_scan<long long>(i < a.n ? a.first[i] : 0, sums, wanted);
+    want += wanted;
   }
   // the lowest free pages, until there are enough
   int found = 0;
@@ -235,12 +239,12 @@ __global__ __launch_bounds__(kThreads) void fork_plan_kernel(ForkArgs a) {
   for (int base = 0; base < a.n; base += kThreads) {
     const int i = base + threadIdx.x;
     const int need = i < a.n ? a.first[i] : 0;
-    const int64_t at = given + group_scan(need, lds, total);
+    const int64_t at = given + group_scan<long long>(need, sums, wanted);
     if (i < a.n) {
       if (need > 0 && at + need > found) a.status[i] = WEDLM_SEQ_CAPACITY;
       a.first[i] = static_cast<int>(min(at, static_cast<int64_t>(found)));
     }
-    given += total;
+    given += wanted;
   }
 }
 

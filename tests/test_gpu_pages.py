@@ -128,6 +128,27 @@ def test_fork_many_requests():
          [rng.integers(0, 9, (1, 9000, 4)).astype(np.uint8)])
 
 
+def test_fork_wants_2_31_pages_together():
+    """1024 requests for 2^21 pages each, a pool that holds one of them and
+    five pages: the sum of the needs passes 32 bits."""
+    from paper_2512_22737_amd import wedlm
+    n, maxp = 1024, 1 << 21
+    i32 = dict(dtype=torch.int32, device="cuda")
+    bt = torch.full((n, maxp), -1, **i32)
+    ref = torch.zeros(maxp + 5, **i32)
+    ref[7] = 1
+    status = torch.full((n,), -1, **i32)
+    wedlm.wedlm_cache_fork(
+        torch.full((n,), -1, **i32), torch.arange(n, **i32),
+        torch.full((n,), 16 * maxp, **i32), torch.zeros(n, **i32), bt, ref, [],
+        status)
+    assert host(status).tolist() == [0] + [O.CAPACITY] * (n - 1)
+    ids = torch.arange(maxp + 1, **i32)
+    assert torch.equal(bt[0], ids[ids != 7])
+    assert all(bool((bt[b] == -1).all()) for b in range(1, n))
+    assert bool((ref[:maxp + 1] == 1).all()) and not ref[maxp + 1:].any()
+
+
 def test_fork_without_arrays_and_with_any_workspace():
     from paper_2512_22737_amd import wedlm
     rng = np.random.default_rng(4)
