@@ -493,7 +493,7 @@ class DecodeStep:
 
     def _pages(self, k_exp, v_exp):
         """Whether the calls are those of an 8-bit cache."""
-        if self.eight_bits != (k_exp is not None and v_exp is not None):
+        if any((x is not None) != self.eight_bits for x in (k_exp, v_exp)):
             raise WedlmError("exponents go with cache='e4m3', and only there")
         return self.eight_bits
 
@@ -540,13 +540,14 @@ class DecodeStep:
 
     def __call__(self, win_tok, win_start, qkv_in, logits, k_cache, v_cache,
                  block_table, k_exp=None, v_exp=None, u=None, **settings):
+        self._pages(k_exp, v_exp)
+        if settings and u is None:
+            raise WedlmError("sampling needs random numbers u")
         self.reorder(win_tok, win_start, qkv_in)
         self.attn(k_cache, v_cache, block_table, win_start, k_exp, v_exp)
         self.score(logits)
         if u is not None:
             self.sample(logits, u, **settings)
-        elif settings:
-            raise WedlmError("sampling needs random numbers u")
         self.commit(win_tok, win_start, k_cache, v_cache, block_table, k_exp,
                     v_exp)
 

@@ -144,3 +144,20 @@ def test_binding_refusals():
     t = torch.zeros(2, 4, dtype=torch.int32)
     with pytest.raises(wedlm.WedlmError, match="device"):
         wedlm.wedlm_cache_free(t[0], t, t[0])
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_step_refuses_a_mix_before_it_starts(cache):
+    """One exponent alone is no 8-bit cache and no bf16 one; settings need
+    random numbers."""
+    import torch
+    from paper_2512_22737_amd import wedlm
+    step = wedlm.DecodeStep(1, 2, 2, 1, 64, 8, 16, device="cpu", cache=cache)
+    e = torch.zeros(1, 1, dtype=torch.uint8)
+    wrong = [(e, None), (None, e), (None, None) if step.eight_bits else (e, e)]
+    for k, v in wrong:
+        with pytest.raises(wedlm.WedlmError, match="exponents"):
+            step(*[None] * 7, k_exp=k, v_exp=v)
+    good = (e, e) if step.eight_bits else (None, None)
+    with pytest.raises(wedlm.WedlmError, match="random"):
+        step(*[None] * 7, *good, top_k=e)
