@@ -236,9 +236,11 @@ int wedlm_cache_compact(const int32_t* block_table, int32_t B,
  *   token = the lowest id t for which the weights of the remaining ids <= t
  *           sum up to more than u times their total
  *   logp  = ln(w_t / total)
- * Weights are fixed-point numbers of at least 40 bits after the point, from
- * fp64; their sums are exact, so the result does not depend on an order of
- * summation.
+ * Weights are fixed-point numbers with f = min(46, 62 - ceil(log2 V)) bits
+ * after the point, from fp64; their sums are exact, so the result does not
+ * depend on an order of summation.  The total is at least 1 and each weight is
+ * off by at most half a unit, logp therefore by at most V 2^-(f+1) beside its
+ * rounding to fp32: one that is nearer to 0 is not resolved.
  * In:
  *   logits [B, W, row_stride] of logits_type (WEDLM_SAMPLE_*), row_stride >=
  *     V; NaN counts as -inf (a token that is ruled out), +inf as the largest
