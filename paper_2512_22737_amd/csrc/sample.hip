@@ -590,7 +590,7 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
   r.powers = l.powers;
   bool use_k = k_raw > 0 && k_raw < V;
   const float p = a.top_p ? a.top_p[b] : 1.f;
-  const bool use_p = p < 1.f;
+  bool use_p = p < 1.f;
   const double pd = p > 0.f ? static_cast<double>(p) : 0.0;
   const float least = a.min_p ? a.min_p[b] : 0.f;
   uint64_t qmin = 1;
@@ -606,8 +606,15 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
   uint64_t k_left = 0, k_above = 0;     // tokens of bin kb; weights above it
   uint64_t p_above = 0;                 // weights above bin lo
   float rate = 0.f;
-  // (falls with the logit, so bins are in the order of the keys; -inf last)
-  auto place = [&](float f) { return (fmax_ - f) * rate; };
+  // (fmax_ - f) * rate / 2: falls with the logit, so bins are in the order of
+  // the keys; -inf has none.  Half of each, since the difference of two fp32
+  // numbers can pass the largest one: a token would have a weight and no bin
+  // where T is that large too.
+  const float half = 0.5f * fmax_;
+  auto place = [&](float f) { return __builtin_fmaf(-0.5f, f, half) * rate; };
+  auto rate_of = [&](float units) {
+    return static_cast<float>(fmin(r.rate * (kBins / units), 1e30) * 2.0);
+  };
   auto bin_of = [&](uint32_t key) {
     return static_cast<int>(fminf(place(of_key(key)), 1e6f));
   };
@@ -623,7 +630,8 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
     __syncthreads();
   };
   // From the bins' counts and weights (`all`: this thread's part of the weight
-  // of all tokens): true if an end lies below the bins, which `last` excludes.
+  // of all tokens): true if an end lies below the bins; never with `last`, so
+  // that the passes end whatever the bins hold.
   auto locate = [&](uint64_t all, bool last) {
     if (use_k) {
       uint64_t before;
@@ -651,15 +659,19 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
         k_above = most - l.sum[kb];
       }
       const uint32_t f = find_bin(l, sums, same, share(pd, k_above), p_above);
-      lo = hi = static_cast<int>(f);
-      if (f >= kBins) return true;
-      if (kb >= 0) {
-        uint64_t before;
-        hi = static_cast<int>(find_bin(l, sums, same, share(pd, most), before));
+      if (f < kBins) {
+        lo = hi = static_cast<int>(f);
+        if (kb >= 0) {
+          uint64_t before;
+          hi = static_cast<int>(
+              find_bin(l, sums, same, share(pd, most), before));
+        }
+        return false;
       }
-    } else if (kb >= 0) {
-      lo = hi = kb;
+      if (!last) return true;
+      use_p = false;                    // what has no bin then has no weight
     }
+    if (kb >= 0) lo = hi = kb;
     return false;
   };
   bool placed = false;
@@ -667,7 +679,7 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
     // The k-th largest of the parts' maxima is not above the k-th largest
     // logit, and mostly near it: what is above its bin is collected.  With few
     // k the parts are the blocks, and only those with something are read again.
-    rate = static_cast<float>(fmin(r.rate * (kBins / kAllUnits), 1e30));
+    rate = rate_of(kAllUnits);
     clear();
     auto mark = [&](float f) {
       const float at = place(clean(f));
@@ -726,7 +738,7 @@ __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(Args a) {
     __syncthreads();
   }
   for (float units = kUnits; !placed && (use_k || use_p); units = kAllUnits) {
-    rate = static_cast<float>(fmin(r.rate * (kBins / units), 1e30));
+    rate = rate_of(units);
     clear();
     uint64_t all = 0;
     bool room = true;                   // in the list, as far as this wave saw
