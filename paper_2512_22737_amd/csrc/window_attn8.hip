@@ -546,7 +546,7 @@ void window_attn8_kernel(Args a) {
       float ks = scale_of(e2 & 0xff), vs = scale_of(e2 >> 8);
       floatx16_t s = scores(kr);
       bf16x8_t pf[2];
-      if (base + kTileKeys <= k1) {
+      if (k1 - base >= kTileKeys) {     // (base + kTileKeys may pass 2^31 - 1)
         const float f = a.scale_log2 * ks;
         if (ballot(m2 == kNegInf)) raise(col_max(s * f));
         float sum = weigh(s, f, pf);
