@@ -149,7 +149,9 @@ __device__ Request check_request(const ForkArgs& a, int i) {
     for (int off = 32; off >= 1; off >>= 1) have += __shfl_xor(have, off);
     need = q.upto - have;
   } else {
-    for (int j = lane; j < a.max_pages; j += kWave)
+    // (unsigned: the step behind the last of 2^31 - 1 entries counts on)
+#pragma unroll 8
+    for (uint32_t j = lane; j < static_cast<uint32_t>(a.max_pages); j += kWave)
       if (own[j] >= 0) clash = true;
   }
   if (ballot(clash)) {
