@@ -161,7 +161,8 @@ __device__ Request check_request(const ForkArgs& a, int i) {
   if (!q.extend && q.p >= 0) {
     const int32_t* from = a.bt + static_cast<int64_t>(q.p) * a.max_pages;
     bool bad = false;
-    const int pages = (q.c + kPage - 1) / kPage;
+    const int pages = q.c / kPage + (q.c % kPage != 0 ? 1 : 0);
+#pragma unroll 8
     for (int j = lane; j < pages; j += kWave) {
       const int id = from[j];
       if (id < 0 || id >= a.num_pages) bad = true;
