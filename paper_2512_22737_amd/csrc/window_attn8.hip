@@ -754,8 +754,9 @@ __global__ __launch_bounds__(kMergeThreads) void merge8_kernel(Args a) {
     M = top;
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      const float w =
-          s0 + i < n ? __builtin_amdgcn_exp2f(x[i].x - base) : 0.f;
+      if (s0 + i >= n) break;         // (a weight of 0 would not do: sums that
+                                      // are infinite stay so)
+      const float w = __builtin_amdgcn_exp2f(x[i].x - base);
       L += w * x[i].y;
 #pragma unroll
       for (int k = 0; k < 8; ++k) acc[k] += w * v[i][k / 4][k % 4];
