@@ -85,6 +85,12 @@ size_t wedlm_window_attn_cache8_workspace_size(int32_t B, int32_t W,
  * lengths, and nothing depends on the run.  bf16 arrays, k8 and v8 on 16-byte
  * boundaries, the workspace on a 256-byte one (WEDLM_E_ARG); a max_prefix_len
  * whose splits pass one launch is refused (WEDLM_E_SHAPE).
+ * What is not finite: a NaN code in a key of the prefix makes the outputs and
+ * lse of its kv head's rows NaN, one in a value its element of their outputs; in
+ * the window a query its own row, a key the rows that see it, a value its
+ * element of all the window's rows (NaN, or infinite).  Weights are summed
+ * before their maximum is known: with values of 2^44 and more a sum can become
+ * infinite where the result is not.
  */
 int wedlm_window_attn_cache8(
     const uint16_t* q_phys, const uint16_t* k_phys, const uint16_t* v_phys,

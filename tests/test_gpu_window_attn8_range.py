@@ -75,7 +75,36 @@ def near_but(got, want, bound, reached):
 
 
 @pytest.mark.parametrize("W,Hq,Hkv,D", SHAPES)
-@pytest.mark.parametrize("bad", [float("inf")])
+def test_codes_of_the_prefix(W, Hq, Hkv, D):
+    """One NaN code at the first, a middle and the last position of each
+    sequence, in keys or values."""
+    s = state(W, Hq, Hkv, D)
+    out, lse = call(s)
+    assert bool(out.isfinite().all()) and bool(lse.isfinite().all())
+    G = Hq // Hkv
+    for b, n in enumerate(LENS):
+        for j in sorted({0, 31, n // 2, n // 32 * 32 - 1, n - 1}):
+            p, h, d = s["bt"][b, j // 16], j % Hkv, (5 * j) % D
+            print(f"NaN at sequence {b} position {j} head {h}", flush=True)
+            heads = slice(h * G, (h + 1) * G)
+            k8 = s["k8"].copy()
+            k8[p, h, j % 16, d] = 0x7f
+            o, l = call(dict(s, k8=k8))
+            hit = torch.zeros_like(lse, dtype=torch.bool)
+            hit[b, :, heads] = True
+            same_but(l, lse, hit)
+            same_but(o, out, hit[..., None].expand_as(out))
+            v8 = s["v8"].copy()
+            v8[p, h, d, j % 16] = 0xff
+            o, l = call(dict(s, v8=v8))
+            assert torch.equal(l, lse)
+            hit = torch.zeros_like(out, dtype=torch.bool)
+            hit[b, :, heads, d] = True
+            same_but(o, out, hit)
+
+
+@pytest.mark.parametrize("W,Hq,Hkv,D", SHAPES)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_rows_of_the_window(W, Hq, Hkv, D, bad):
     """A query reaches its own row; a key the rows that see it; a value its
     element of all rows."""
@@ -112,3 +141,19 @@ def test_rows_of_the_window(W, Hq, Hkv, D, bad):
             want[b, i:, h * G:(h + 1) * G, d] = bad
             hit &= (rows < i)[None, :, None, None]
         same_but(o, want, hit)
+
+
+@pytest.mark.parametrize("W,Hq,Hkv,D", SHAPES)
+def test_large_values(W, Hq, Hkv, D):
+    """Values up to 2^43 at keys that outgrow every earlier one: the outputs
+    are those of values 2^42 times smaller, times 2^42."""
+    s = state(W, Hq, Hkv, D)
+    for b in range(len(LENS)):
+        for j in range(-(-LENS[b] // 16)):
+            s["ke"][s["bt"][b, j]] = 112 + j // 12
+    s["ve"] = np.full_like(s["ve"], 119)                  # |v| <= 448 * 2^-8
+    s["vw"] = s["vw"] * 0.25
+    out, lse = call(s)
+    o, l = call(dict(s, ve=s["ve"] + 42, vw=s["vw"] * 2.0 ** 42))
+    assert bool(o.isfinite().all()) and torch.equal(l, lse)
+    assert torch.equal(o, out * 2.0 ** 42)
