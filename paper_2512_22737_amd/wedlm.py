@@ -1109,6 +1109,8 @@ def wedlm_commit_cache8(win_tok, win_start, argmax, entropy, tau: float,
 
 
 class PageArray(ctypes.Structure):
+    """wedlm_page_array.  (_page_arrays writes the same two words of each array
+    without it, in half the time.)"""
     _fields_ = [("base", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
 
 
@@ -1116,7 +1118,7 @@ def _page_arrays(arrays, P):
     """The library's list of a pool's arrays [L, P, ...], and their L."""
     if not arrays:
         return None, 0, 1
-    L = arrays[0].shape[0]
+    L = arrays[0].shape[0] if arrays[0].dim() else 0
     pairs = []                    # the fields of PageArray, one after another
     for i, x in enumerate(arrays):
         if not x.is_cuda or not x.is_contiguous():
