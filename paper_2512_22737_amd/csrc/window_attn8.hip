@@ -37,8 +37,8 @@ using namespace wedlm;
 namespace {
 
 constexpr int kTileKeys = 32;       // keys per tile (two 16-token pages)
-// A prefix split holds at least this many tiles, and at most 2048 pages (their
-// ids are staged in LDS).
+// A prefix split but a sequence's last one, which has what is left, holds at
+// least this many tiles, and at most 2048 pages (their ids are staged in LDS).
 constexpr int kMinSplitTiles = 8;
 constexpr int kMaxSplitPages = 2048;
 constexpr int kMaxSplitTiles = kMaxSplitPages / 2;
