@@ -493,7 +493,8 @@ class DecodeStep:
 
     def _pages(self, k_exp, v_exp):
         """Whether the calls are those of an 8-bit cache."""
-        if any((x is not None) != self.eight_bits for x in (k_exp, v_exp)):
+        if ((k_exp is None) == self.eight_bits or
+                (v_exp is None) == self.eight_bits):
             raise WedlmError("exponents go with cache='e4m3', and only there")
         return self.eight_bits
 
