@@ -80,9 +80,11 @@ size_t wedlm_window_attn_cache8_workspace_size(int32_t B, int32_t W,
  * window's own keys and values stay bf16.  Arguments, outputs, limits and
  * errors are those of wedlm_window_attn with k8, v8, k_exp, v_exp in the
  * place of k_cache, v_cache; D = 64 or 128, W = 1 (single tokens) to 64.
- * Codes behind a sequence's prefix are not used, whatever they hold.  The
- * splits' sums are merged in fp32; their number goes by the batch's own prefix
- * lengths, and nothing depends on the run.  bf16 arrays, k8 and v8 on 16-byte
+ * Codes behind a sequence's prefix are not used, whatever they hold.  Weights
+ * enter their product with the values in bf16 (as over bf16 pages; half a step
+ * of 2^-8, as much as the result's own rounding), sums are fp32, also where
+ * splits are merged; their number goes by the batch's own prefix lengths, and
+ * nothing depends on the run.  bf16 arrays, k8 and v8 on 16-byte
  * boundaries, the workspace on a 256-byte one (WEDLM_E_ARG); a max_prefix_len
  * whose splits pass one launch is refused (WEDLM_E_SHAPE).
  * What is not finite: a NaN code in a key of the prefix makes the outputs and
@@ -246,7 +248,8 @@ int wedlm_cache_compact(const int32_t* block_table, int32_t B,
  * after the point, from fp64; their sums are exact, so the result does not
  * depend on an order of summation.  The total is at least 1 and each weight is
  * off by at most half a unit, logp therefore by at most V 2^-(f+1) beside its
- * rounding to fp32: one that is nearer to 0 is not resolved.
+ * rounding to fp32: one that is nearer to 0 is not resolved.  A weight below
+ * 2^-(f+1) is 0, and its token is not drawn.
  * In:
  *   logits [B, W, row_stride] of logits_type (WEDLM_SAMPLE_*), row_stride >=
  *     V; NaN counts as -inf (a token that is ruled out), +inf as the largest

@@ -9,7 +9,9 @@
 // Bound by HBM where rows are many (4 x 1024 rows of 8 layers, 8 heads of 128:
 // 169 MB in 33 us, 5.1 TB/s); by latency where a step commits a few tokens (16 x
 // 4 rows of 36 layers: 12 us): the chain is start/count, block table with the
-// rows, the page's old bytes with its exponents, stores.
+// rows, the page's old V bytes with its exponents, K's old codes where the
+// scale grows, stores; from the block table on once more for a run that crosses
+// into the next page.
 #include "common.h"
 #include "internal.h"
 #include "wedlm_serve.h"

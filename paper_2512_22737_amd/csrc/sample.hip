@@ -24,10 +24,11 @@
 // itself where they are too many for LDS, as in a flat row).  Last, one wave
 // walks the segment that the draw falls into.
 // Bounds, 1280 rows of 151936 fp32 logits: greedy 136 us (HBM, 5.7 TB/s), k = 50
-// 194, k = 1000 328 (the second pass), no limit 377 (fp64 weights: 15 fp64
+// 191, k = 1000 328 (the second pass), no limit 375 (fp64 weights: 15 fp64
 // operations and an LDS read a token), top-p alone 0.68 ms (the histogram's
-// 64-bit LDS additions beside that).  One row: 8 to 165 us, its workgroup's
-// own time; rows are not split over workgroups.
+// 64-bit LDS additions beside that).  bf16 logits: 71, 132, 247, 282 and 587
+// us (8 registers of the vectors under way spill).  One row: 8 to 165 us, its
+// workgroup's own time; rows are not split over workgroups.
 #include "common.h"
 #include "wedlm_serve.h"
 
